@@ -61,6 +61,7 @@ typedef int32_t huge_status;
 #define HUGE_ERR_BAD_COUNT (-3)       /* a negative co_count                       */
 #define HUGE_ERR_WORKSPACE (-4)       /* workspace smaller than huge_workspace_bytes */
 #define HUGE_ERR_HIP (-5)             /* a HIP runtime call failed                 */
+#define HUGE_ERR_NOT_FINITE (-6)      /* an optimiser state would not be finite    */
 
 /* Negative distribution: uniform over the vocabulary (Sec. 3.3.2), or an
    alias table over caller weights (e.g. degree^0.75). */
@@ -447,6 +448,148 @@ huge_status huge_eval_recall(const int64_t* d_offsets, const int32_t* d_neighbor
                              int64_t num_nodes, int64_t num_edges, const int32_t* d_queries,
                              int32_t n_queries, const int32_t* d_ids, int32_t k,
                              double* d_recall, int32_t* d_status, void* stream);
+
+/* ------------------------------------------------------------------------
+   A softmax head on embedding rows: layer norm, the exact softmax loss over
+   every row of an output table (the classes: all nodes, as in DeepWalk's
+   objective that negative sampling stands in for, or the labels of the
+   downstream classifier of Sec. 4.2) with its gradient, and AdamW for the
+   dense gradients.  The calls take no handle.  Rows are `dim` elements of
+   HUGE_DTYPE_F32 or HUGE_DTYPE_BF16 at a row stride of ld >= dim elements;
+   pointers need the alignment of their element type only (16 bytes, with ld
+   and dim multiples of 4, take the vector loads of layer norm and AdamW).
+   Everything is computed in fp32 from the stored values and rounded once to
+   the type of the output.  All calls are asynchronous on `stream`; argument
+   errors return before any launch.  Results are bitwise reproducible.
+   d_status (device int32) is sticky: a call writes an error to it where it
+   holds 0 and never clears it, so that one word serves any number of calls. */
+
+/* Layer norm of n rows, 1 <= dim <= 8192 (variance over the row, biased):
+     mean = sum x / dim, rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps),
+     y = (x - mean) rstd gamma + beta.
+     d_x, d_y           : rows of `dtype`, which may be the same array
+     d_gamma, d_beta    : dim floats each
+     d_mean, d_rstd     : n floats each, or both NULL
+   eps > 0. */
+huge_status huge_layer_norm(const void* d_x, int64_t ld_x, int64_t n, int32_t dim, int32_t dtype,
+                            const float* d_gamma, const float* d_beta, float eps, void* d_y,
+                            int64_t ld_y, float* d_mean, float* d_rstd, void* stream);
+
+/* Its gradient, with xh = (x - mean) rstd and a = dy gamma:
+     dx = rstd (a - sum a / dim - xh sum (a xh) / dim),
+     dgamma = sum over rows of dy xh, dbeta = sum over rows of dy.
+   d_dx or both of d_dgamma and d_dbeta may be NULL (not wanted); d_dx may be
+   the array of d_dy.  n = 0 writes zeros to dgamma and dbeta.  d_workspace:
+   huge_layer_norm_workspace_bytes(n, dim) bytes, 16-byte aligned. */
+size_t huge_layer_norm_workspace_bytes(int64_t n, int32_t dim);
+huge_status huge_layer_norm_backward(const void* d_dy, int64_t ld_dy, const void* d_x,
+                                     int64_t ld_x, int64_t n, int32_t dim, int32_t dtype,
+                                     const float* d_gamma, const float* d_mean,
+                                     const float* d_rstd, void* d_dx, int64_t ld_dx,
+                                     float* d_dgamma, float* d_dbeta, void* d_workspace,
+                                     size_t ws_bytes, void* stream);
+
+typedef struct huge_softmax_config {
+    int64_t num_classes; /* V: rows of the output table, 1 .. 2^31-1                  */
+    int64_t max_rows;    /* largest n per call, 1 .. 2^31-1                           */
+    int32_t dim;         /* D: multiple of 4, 4 .. 1024                               */
+    int32_t dtype;       /* of h, w and their gradients                               */
+    int32_t grad;        /* 1: the workspace also serves huge_softmax_grad, 0: it does not */
+} huge_softmax_config;
+
+/* Bytes of device workspace of the two calls below (256-byte aligned); 0 if
+   the config is invalid.  The table is taken in pieces whose packed copy is
+   at most 2 GiB, so that the workspace does not grow with V beyond that. */
+size_t huge_softmax_workspace_bytes(const huge_softmax_config* cfg);
+
+/* Softmax cross entropy of n rows h (n x D) against all rows of w (V x D),
+   without keeping the n x V logits:
+     x_ij = <h_i, w_j> + bias_j, lse_i = log sum_j exp x_ij,
+     loss_i = weight_i (lse_i - x_ij) with j = label_i.
+     d_bias    : V floats, or NULL (zeros).  -inf takes a class out: it counts
+                 in no sum, and nothing in its row of w, NaN included, is used
+     d_labels  : n int32 classes, -1 = no label
+     d_weight  : n floats >= 0 (co_counts), or NULL (ones)
+     d_loss    : n floats.  0 for a row without a label, with weight 0 or whose
+                 label is taken out (so also where every class is)
+     d_lse     : n floats; -inf where every class is taken out
+     d_loss_sum: device double, the sum of d_loss in a fixed order, or NULL
+   A label outside [-1, V) writes HUGE_ERR_ID_OUT_OF_RANGE to d_status, a
+   weight that is negative, NaN or infinite HUGE_ERR_BAD_COUNT; the loss of
+   such a row is NaN and it has no gradient. */
+huge_status huge_softmax_loss(const huge_softmax_config* cfg, const void* d_h, int64_t ld_h,
+                              int64_t n, const void* d_w, int64_t ld_w, const float* d_bias,
+                              const int32_t* d_labels, const float* d_weight, float* d_loss,
+                              float* d_lse, double* d_loss_sum, int32_t* d_status,
+                              void* d_workspace, size_t ws_bytes, void* stream);
+
+/* The gradient of scale * sum_i loss_i, with p_ij = exp(x_ij - lse_i) formed
+   again from the logits and g_ij = scale weight_i (p_ij - [j = label_i]) for
+   the rows that have a loss (0 for the others, whatever their h holds):
+     dh_i = sum_j g_ij w_j, dw_j = sum_i g_ij h_i, dbias_j = sum_i g_ij.
+     d_lse          : as huge_softmax_loss wrote it for the same inputs
+     d_dh           : n x D of cfg->dtype, contiguous, or NULL (not wanted)
+     d_dw           : V x D of cfg->dtype, contiguous, or NULL
+     d_dbias        : V floats, or NULL
+   All of dw and dbias is written, zeros where no row contributes. */
+huge_status huge_softmax_grad(const huge_softmax_config* cfg, const void* d_h, int64_t ld_h,
+                              int64_t n, const void* d_w, int64_t ld_w, const float* d_bias,
+                              const int32_t* d_labels, const float* d_weight, const float* d_lse,
+                              float scale, void* d_dh, void* d_dw, float* d_dbias,
+                              int32_t* d_status, void* d_workspace, size_t ws_bytes,
+                              void* stream);
+
+/* AdamW over a list of tensors in one launch per 64 of them (and per pair of
+   types).  For every element, in fp32, each product and sum rounded:
+     m' = beta1 m + (1 - beta1) g, v' = beta2 v + (1 - beta2) g g,  g = grad_scale grad
+     param = param (1 - lr weight_decay)
+             - (m' lr / (1 - beta1^step)) / (sqrt(v') / sqrt(1 - beta2^step) + eps)
+   An element whose m' or v' is not finite keeps its param, m and v, and
+   HUGE_ERR_NOT_FINITE is written to d_status.
+   States: HUGE_STATE_F32 keeps m and v as floats.  HUGE_STATE_Q8 keeps them
+   in 8 bits, in blocks of 256 consecutive elements of a tensor: m as
+   s sgn(q) (q / 127)^2 with q in -127 .. 127 and s the block's largest |m|,
+   sqrt(v) as t (u / 255)^2 with u in 0 .. 255 and t the block's largest
+   sqrt(v); both to the nearest code, u at least 1 where v > 0 (a v that
+   became 0 would let m / eps through).  The parameter moves by the m' and v'
+   before they are rounded.  A state of zero bytes is m = v = 0. */
+#define HUGE_STATE_F32 0
+#define HUGE_STATE_Q8 1
+
+typedef struct huge_adamw_tensor {
+    void* d_param;       /* n elements of param_dtype                              */
+    const void* d_grad;  /* n elements of grad_dtype                               */
+    void* d_state;       /* huge_adamw_state_bytes(n, state_kind), 16-byte aligned */
+    int64_t n;           /* 0 .. 2^40                                              */
+    int32_t param_dtype; /* HUGE_DTYPE_F32 or HUGE_DTYPE_BF16                      */
+    int32_t grad_dtype;
+} huge_adamw_tensor;
+
+typedef struct huge_adamw_config {
+    double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps > 0 */
+    int64_t step;        /* 1 for the first step                                   */
+    int32_t state_kind;  /* HUGE_STATE_F32 or HUGE_STATE_Q8                        */
+} huge_adamw_config;
+
+/* Bytes of the state of a tensor of n elements; 0 if n or the kind is out of
+   range (and for n = 0). */
+size_t huge_adamw_state_bytes(int64_t n, int32_t state_kind);
+
+/* One step over h_tensors[0 .. count) (a host array, read before the call
+   returns). */
+huge_status huge_adamw_step(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
+                            int32_t count, int32_t* d_status, void* stream);
+
+/* The moments that the states hold, as floats: h_m[k] and h_v[k] (host arrays
+   of device pointers) receive n floats each of tensor k.  Only d_state and n
+   of the tensors are read.  huge_adamw_set_state writes states from moments
+   (a checkpoint, or another kind of state); v >= 0, both finite. */
+huge_status huge_adamw_get_state(const huge_adamw_tensor* h_tensors, int32_t count,
+                                 int32_t state_kind, float* const* h_m, float* const* h_v,
+                                 void* stream);
+huge_status huge_adamw_set_state(const huge_adamw_tensor* h_tensors, int32_t count,
+                                 int32_t state_kind, const float* const* h_m,
+                                 const float* const* h_v, void* stream);
 
 void huge_destroy(huge_handle* h);
 const char* huge_status_string(huge_status s);

@@ -2,9 +2,12 @@
 over (source_id, destination_id, co_counts) batches, in hand-written HIP
 kernels behind the C ABI of ``include/huge.h``, the random-walk sampler
 that produces those batches on the GPU, and the unsupervised evaluation of
-the trained embeddings (edge SNR, distance percentiles, sampled recall).
+the trained embeddings (edge SNR, distance percentiles, sampled recall), and
+the training step of a softmax head on the embeddings (layer norm, the exact
+softmax loss over all classes, AdamW).
 
-``binding`` is the ctypes layer; ``build`` compiles ``libhuge.so`` in-tree.
+``binding`` is the ctypes layer, ``head`` that of the softmax head's operators;
+``build`` compiles ``libhuge.so`` in-tree.
 """
 from .binding import (  # noqa: F401
     EXPORTED,
@@ -25,4 +28,11 @@ from .binding import (  # noqa: F401
     status_string,
     walk_config,
     workspace_bytes,
+)
+from .head import (  # noqa: F401
+    AdamW,
+    SoftmaxHead,
+    SoftmaxLoss,
+    layer_norm,
+    layer_norm_backward,
 )

@@ -21,6 +21,7 @@ HUGE_ERR_ID_OUT_OF_RANGE = -2
 HUGE_ERR_BAD_COUNT = -3
 HUGE_ERR_WORKSPACE = -4
 HUGE_ERR_HIP = -5
+HUGE_ERR_NOT_FINITE = -6
 
 HUGE_NEG_UNIFORM = 0
 HUGE_NEG_ALIAS = 1
@@ -28,6 +29,8 @@ HUGE_SCATTER_SORTED = 0
 HUGE_SCATTER_ATOMIC = 1
 HUGE_DTYPE_F32 = 0
 HUGE_DTYPE_BF16 = 1
+HUGE_STATE_F32 = 0
+HUGE_STATE_Q8 = 1
 
 EXPORTED = [
     "huge_workspace_bytes", "huge_build_alias", "huge_init_tables", "huge_attach_tables",
@@ -38,6 +41,9 @@ EXPORTED = [
     "huge_eval_summary_static",
     "huge_eval_knn", "huge_eval_knn_lists", "huge_eval_recall", "huge_train_step_weighted", "huge_prepare_step_weighted",
     "huge_eval_loss_weighted", "huge_cocount_weights",
+    "huge_layer_norm", "huge_layer_norm_workspace_bytes", "huge_layer_norm_backward",
+    "huge_softmax_workspace_bytes", "huge_softmax_loss", "huge_softmax_grad",
+    "huge_adamw_state_bytes", "huge_adamw_step", "huge_adamw_get_state", "huge_adamw_set_state",
 ]
 HUGE_PHASES = 6
 
@@ -64,6 +70,40 @@ class HugeWalkConfig(ctypes.Structure):
         ("window", ctypes.c_int32),
         ("seed_pairs_only", ctypes.c_int32),
         ("seed", ctypes.c_uint64),
+    ]
+
+
+class HugeSoftmaxConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_classes", ctypes.c_int64),
+        ("max_rows", ctypes.c_int64),
+        ("dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("grad", ctypes.c_int32),
+    ]
+
+
+class HugeAdamwTensor(ctypes.Structure):
+    _fields_ = [
+        ("d_param", ctypes.c_void_p),
+        ("d_grad", ctypes.c_void_p),
+        ("d_state", ctypes.c_void_p),
+        ("n", ctypes.c_int64),
+        ("param_dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+    ]
+
+
+class HugeAdamwConfig(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("weight_decay", ctypes.c_double),
+        ("grad_scale", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("state_kind", ctypes.c_int32),
     ]
 
 
@@ -136,6 +176,29 @@ def load() -> ctypes.CDLL:
     L.huge_cocount_weights.argtypes = [_vp, i64, i32, ctypes.POINTER(ctypes.c_float), _vp, _vp]
     for name in ("huge_train_step_weighted", "huge_prepare_step_weighted",
                  "huge_eval_loss_weighted", "huge_cocount_weights"):
+        getattr(L, name).restype = ctypes.c_int32
+    f32 = ctypes.c_float
+    L.huge_layer_norm.argtypes = [_vp, i64, i64, i32, i32, _vp, _vp, f32, _vp, i64, _vp, _vp, _vp]
+    L.huge_layer_norm_workspace_bytes.argtypes = [i64, i32]
+    L.huge_layer_norm_workspace_bytes.restype = szt
+    L.huge_layer_norm_backward.argtypes = [_vp, i64, _vp, i64, i64, i32, i32, _vp, _vp, _vp, _vp,
+                                           i64, _vp, _vp, _vp, szt, _vp]
+    scfgp = ctypes.POINTER(HugeSoftmaxConfig)
+    L.huge_softmax_workspace_bytes.argtypes = [scfgp]
+    L.huge_softmax_workspace_bytes.restype = szt
+    L.huge_softmax_loss.argtypes = [scfgp, _vp, i64, i64, _vp, i64, _vp, _vp, _vp, _vp, _vp, _vp,
+                                    _vp, _vp, szt, _vp]
+    L.huge_softmax_grad.argtypes = [scfgp, _vp, i64, i64, _vp, i64, _vp, _vp, _vp, _vp, f32, _vp,
+                                    _vp, _vp, _vp, _vp, szt, _vp]
+    tensorsp, ptrsp = ctypes.POINTER(HugeAdamwTensor), ctypes.POINTER(_vp)
+    L.huge_adamw_state_bytes.argtypes = [i64, i32]
+    L.huge_adamw_state_bytes.restype = szt
+    L.huge_adamw_step.argtypes = [ctypes.POINTER(HugeAdamwConfig), tensorsp, i32, _vp, _vp]
+    L.huge_adamw_get_state.argtypes = [tensorsp, i32, i32, ptrsp, ptrsp, _vp]
+    L.huge_adamw_set_state.argtypes = [tensorsp, i32, i32, ptrsp, ptrsp, _vp]
+    for name in ("huge_layer_norm", "huge_layer_norm_backward", "huge_softmax_loss",
+                 "huge_softmax_grad", "huge_adamw_step", "huge_adamw_get_state",
+                 "huge_adamw_set_state"):
         getattr(L, name).restype = ctypes.c_int32
     L.huge_destroy.argtypes = [_vp]
     L.huge_destroy.restype = None

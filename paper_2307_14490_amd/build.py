@@ -18,7 +18,8 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libhuge.so")
 BUILD = os.path.join(ROOT, "_build")
 
-SOURCES = ["api.hip", "k_tables.hip", "k_sort.hip", "k_step.hip", "k_atomic.hip", "k_walk.hip", "k_eval.hip",
+SOURCES = ["api.hip", "api_head.hip", "k_tables.hip", "k_sort.hip", "k_step.hip", "k_atomic.hip", "k_walk.hip",
+           "k_eval.hip", "k_norm.hip", "k_softmax.hip", "k_adamw.hip",
            "alias.cpp"]
 ARCH = "gfx950"
 

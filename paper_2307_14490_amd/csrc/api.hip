@@ -1247,6 +1247,7 @@ const char* huge_status_string(huge_status st) {
         case HUGE_ERR_BAD_COUNT: return "negative co_count";
         case HUGE_ERR_WORKSPACE: return "workspace too small";
         case HUGE_ERR_HIP: return "HIP runtime error";
+        case HUGE_ERR_NOT_FINITE: return "state not finite";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,378 @@
+"""The softmax head's operators on torch tensors: layer norm, the exact softmax
+loss with its gradient, AdamW, and a head that trains with them.
+
+Argument marshalling for the calls of ``include/huge.h``, as in ``binding``.
+Rows may be any two-dimensional GPU tensors whose columns are adjacent (a slice
+of a wider buffer among them).  Work runs on ``stream`` (default: torch's
+current stream); outputs and workspaces are allocated for that stream, and
+arguments that live on another one are kept until the call's work is done.
+Errors that only the device can see are kept in a status word until ``check``.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+from .binding import (HUGE_DTYPE_BF16, HUGE_DTYPE_F32, HUGE_ERR_INVALID_ARG, HUGE_STATE_F32,
+                      HUGE_STATE_Q8, HugeAdamwConfig, HugeAdamwTensor, HugeError,
+                      HugeSoftmaxConfig, _arg, _dptr, _ok, load)
+
+_DTYPES = {"f32": HUGE_DTYPE_F32, "bf16": HUGE_DTYPE_BF16}
+
+
+def _dtype_code(t, what):
+    import torch
+    if t.dtype == torch.float32:
+        return HUGE_DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return HUGE_DTYPE_BF16
+    raise TypeError(f"{what}: expected float32 or bfloat16, got {t.dtype}")
+
+
+def _rows(t, what, dim=None, like=None):
+    """(pointer, row stride) of a GPU tensor of rows whose columns are adjacent."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        got = f"shape {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) \
+            else type(t).__name__
+        raise TypeError(f"{what}: expected a two-dimensional GPU tensor, got {got}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise TypeError(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if dim is not None and t.shape[1] != dim:
+        raise ValueError(f"{what}: rows of {t.shape[1]}, expected {dim}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the columns of a row must be adjacent, stride {t.stride(1)}")
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if ld < t.shape[1]:
+        raise ValueError(f"{what}: rows overlap (stride {ld} of {t.shape[1]})")
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, dtype, what, device):
+    """Pointer of a contiguous GPU vector of n elements (None stays None)."""
+    if t is None:
+        return None
+    p = _arg(t, (dtype,), what)
+    if t.numel() != n:
+        raise ValueError(f"{what}: {t.numel()} elements, expected {n}")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, expected {device}")
+    return p
+
+
+@contextlib.contextmanager
+def _on(device, stream, *tensors):
+    """The device made current, and the stream to launch on as a pointer.  With a
+    stream of the caller's, what is allocated inside belongs to it, and `tensors`
+    are not given to others before its work on them is done."""
+    import torch
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream().cuda_stream
+        else:
+            with torch.cuda.stream(stream):
+                yield stream.cuda_stream
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+
+
+class _Status:
+    """The sticky status word of an operator, and its workspace's last stream: a
+    call on another stream first waits for the work on that one."""
+
+    def __init__(self, device):
+        import torch
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._last = torch.cuda.current_stream(self.device)
+
+    def _ordered(self, stream):
+        import torch
+        now = torch.cuda.current_stream(self.device) if stream is None else stream
+        if now != self._last:
+            now.wait_stream(self._last)
+            self._last = now
+
+    def check(self):
+        """Raise HugeError if a call since the last check met a device-side error
+        (synchronises); the status is cleared."""
+        self._last.synchronize()
+        st = int(self.status.item())
+        if st != 0:
+            self.status.zero_()
+            raise HugeError(st, type(self).__name__ + " (device)")
+
+
+# --------------------------------------------------------------------------- #
+# Layer norm
+# --------------------------------------------------------------------------- #
+def layer_norm(x, gamma, beta, eps=1e-5, stream=None):
+    """(y, mean, rstd) of the rows x, by huge_layer_norm.  gamma, beta: float32."""
+    import torch
+    px, ld = _rows(x, "layer_norm x")
+    code = _dtype_code(x, "layer_norm x")
+    n, dim = x.shape
+    pg = _vector(gamma, dim, "float32", "layer_norm gamma", x.device)
+    pb = _vector(beta, dim, "float32", "layer_norm beta", x.device)
+    if pg is None or pb is None:
+        raise TypeError("layer_norm: gamma and beta are required")
+    with _on(x.device, stream, x, gamma, beta) as st:
+        y = torch.empty((n, dim), dtype=x.dtype, device=x.device)
+        stat = torch.empty((2, n), dtype=torch.float32, device=x.device)
+        mean, rstd = stat[0], stat[1]
+        _ok(load().huge_layer_norm(px, ld, n, dim, code, pg, pb, float(eps), y.data_ptr(), dim,
+                                   mean.data_ptr(), rstd.data_ptr(), st), "huge_layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, gamma, mean, rstd, want_dx=True, want_weights=True, stream=None):
+    """(dx, dgamma, dbeta) by huge_layer_norm_backward; None where not wanted."""
+    import torch
+    px, ldx = _rows(x, "layer_norm_backward x")
+    code = _dtype_code(x, "layer_norm_backward x")
+    n, dim = x.shape
+    pdy, ldy = _rows(dy, "layer_norm_backward dy", dim, x)
+    if dy.shape[0] != n:
+        raise ValueError(f"layer_norm_backward: {dy.shape[0]} rows of dy, {n} of x")
+    pg = _vector(gamma, dim, "float32", "layer_norm_backward gamma", x.device)
+    pm = _vector(mean, n, "float32", "layer_norm_backward mean", x.device)
+    pr = _vector(rstd, n, "float32", "layer_norm_backward rstd", x.device)
+    if pg is None or pm is None or pr is None:
+        raise TypeError("layer_norm_backward: gamma, mean and rstd are required")
+    L = load()
+    with _on(x.device, stream, dy, x, gamma, mean, rstd) as st:
+        dx = torch.empty((n, dim), dtype=x.dtype, device=x.device) if want_dx else None
+        dw = ws = None
+        bytes_ = 0
+        if want_weights:
+            bytes_ = L.huge_layer_norm_workspace_bytes(n, dim)
+            ws = torch.empty(bytes_, dtype=torch.uint8, device=x.device)
+            dw = torch.empty((2, dim), dtype=torch.float32, device=x.device)
+        _ok(L.huge_layer_norm_backward(pdy, ldy, px, ldx, n, dim, code, pg, pm, pr, _dptr(dx), dim,
+                                       _dptr(dw), None if dw is None else dw[1].data_ptr(),
+                                       _dptr(ws), bytes_, st), "huge_layer_norm_backward")
+    return dx, (dw[0] if want_weights else None), (dw[1] if want_weights else None)
+
+
+# --------------------------------------------------------------------------- #
+# Exact softmax loss
+# --------------------------------------------------------------------------- #
+class SoftmaxLoss(_Status):
+    """Workspace of huge_softmax_loss and huge_softmax_grad for tables of
+    num_classes x dim and up to max_rows rows a call.  grad=False: the loss only,
+    in a smaller workspace."""
+
+    def __init__(self, max_rows, num_classes, dim, dtype="f32", grad=True, device="cuda"):
+        import torch
+        L = load()
+        self.cfg = HugeSoftmaxConfig(int(num_classes), int(max_rows), int(dim), _DTYPES[dtype],
+                                     int(bool(grad)))
+        self.ws_bytes = L.huge_softmax_workspace_bytes(ctypes.byref(self.cfg))
+        if self.ws_bytes == 0:
+            raise HugeError(HUGE_ERR_INVALID_ARG, "huge_softmax_workspace_bytes")
+        super().__init__(device)
+        self._ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
+        self._ws_ptr = self._ws.data_ptr() + ((-self._ws.data_ptr()) % 256)
+
+    def _inputs(self, what, h, w, labels, bias, weights):
+        """Pointers in the order of the C calls, checked."""
+        c = self.cfg
+        ph, ldh = _rows(h, what + " h", c.dim)
+        if _dtype_code(h, what + " h") != c.dtype:
+            raise TypeError(f"{what}: h is {h.dtype}, not the type of this SoftmaxLoss")
+        if h.device != self.device:
+            raise ValueError(f"{what}: h on {h.device}, expected {self.device}")
+        pw, ldw = _rows(w, what + " w", c.dim, h)
+        if w.shape[0] != c.num_classes:
+            raise ValueError(f"{what}: {w.shape[0]} rows of w, expected {c.num_classes}")
+        n = h.shape[0]
+        return (ctypes.byref(c), ph, ldh, n, pw, ldw,
+                _vector(bias, c.num_classes, "float32", what + " bias", h.device),
+                _vector(labels, n, "int32", what + " labels", h.device),
+                _vector(weights, n, "float32", what + " weights", h.device))
+
+    def loss(self, h, w, labels, bias=None, weights=None, total=None, stream=None):
+        """(loss, lse), float32 per row of h.  total: a float64 tensor of one element
+        that receives the sum of the losses."""
+        import torch
+        a = self._inputs("SoftmaxLoss.loss", h, w, labels, bias, weights)
+        pt = _vector(total, 1, "float64", "SoftmaxLoss.loss total", h.device)
+        self._ordered(stream)
+        with _on(self.device, stream, h, w, labels, bias, weights, total) as st:
+            out = torch.empty((2, a[3]), dtype=torch.float32, device=self.device)
+            loss, lse = out[0], out[1]
+            _ok(load().huge_softmax_loss(*a, loss.data_ptr(), lse.data_ptr(), pt,
+                                         self.status.data_ptr(), self._ws_ptr, self.ws_bytes, st),
+                "huge_softmax_loss")
+        return loss, lse
+
+    def grad(self, h, w, labels, lse, bias=None, weights=None, scale=1.0, want_h=True,
+             want_w=True, want_bias=True, stream=None):
+        """(dh, dw, dbias) of scale times the sum of the losses, dh and dw in the
+        type of h; None where not wanted."""
+        import torch
+        a = self._inputs("SoftmaxLoss.grad", h, w, labels, bias, weights)
+        pl = _vector(lse, a[3], "float32", "SoftmaxLoss.grad lse", h.device)
+        if pl is None:
+            raise TypeError("SoftmaxLoss.grad: lse is required")
+        c = self.cfg
+        self._ordered(stream)
+        with _on(self.device, stream, h, w, labels, lse, bias, weights) as st:
+            new = lambda *shape, t=h.dtype: torch.empty(shape, dtype=t, device=self.device)  # noqa: E731
+            dh = new(a[3], c.dim) if want_h else None
+            dw = new(c.num_classes, c.dim) if want_w else None
+            db = new(c.num_classes, t=torch.float32) if want_bias else None
+            _ok(load().huge_softmax_grad(*a, pl, float(scale), _dptr(dh), _dptr(dw), _dptr(db),
+                                         self.status.data_ptr(), self._ws_ptr, self.ws_bytes, st),
+                "huge_softmax_grad")
+        return dh, dw, db
+
+
+# --------------------------------------------------------------------------- #
+# AdamW
+# --------------------------------------------------------------------------- #
+class AdamW(_Status):
+    """AdamW over a list of contiguous float32 or bfloat16 GPU tensors of one
+    device, updated in place by huge_adamw_step.  states: "f32", or "q8" for
+    moments in 8 bits.  The parameters' storage must stay where it is."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+                 states="f32"):
+        import torch
+        L = load()
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("AdamW: no parameters")
+        self.kind = {"f32": HUGE_STATE_F32, "q8": HUGE_STATE_Q8}[states]
+        for k, p in enumerate(self.params):
+            _arg(p, ("float32", "bfloat16"), f"AdamW params[{k}]")
+            if p.device != self.params[0].device:
+                raise ValueError(f"AdamW params[{k}]: on {p.device}, expected "
+                                 f"{self.params[0].device}")
+        super().__init__(self.params[0].device)
+        self.steps = 0
+        self.lr = float(lr)
+        self.cfg = HugeAdamwConfig(self.lr, float(betas[0]), float(betas[1]), float(eps),
+                                   float(weight_decay), 1.0, 1, self.kind)
+        count = len(self.params)
+        self._tensors = (HugeAdamwTensor * count)()
+        # one buffer for all states, each 256-byte aligned in it
+        at, self._state_at = 0, []
+        for p in self.params:
+            self._state_at.append(at)
+            at += -(-L.huge_adamw_state_bytes(p.numel(), self.kind) // 256) * 256
+        self.states = torch.zeros(at + 256, dtype=torch.uint8, device=self.device)
+        self._skip = (-self.states.data_ptr()) % 256
+        for k, p in enumerate(self.params):
+            t = self._tensors[k]
+            t.d_param, t.n = p.data_ptr(), p.numel()
+            t.d_state = self.states.data_ptr() + self._skip + self._state_at[k]
+            t.param_dtype = _dtype_code(p, f"AdamW params[{k}]")
+
+    def _list(self, ts, dtypes, what):
+        ts = list(ts)
+        if len(ts) != len(self.params):
+            raise ValueError(f"{what}: {len(ts)} tensors, expected {len(self.params)}")
+        for k, (t, p) in enumerate(zip(ts, self.params)):
+            _arg(t, dtypes, f"{what}[{k}]")
+            if t.numel() != p.numel() or t.device != p.device:
+                raise ValueError(f"{what}[{k}]: {t.numel()} elements on {t.device}, expected "
+                                 f"{p.numel()} on {p.device}")
+        return ts
+
+    def step(self, grads, lr=None, grad_scale=1.0, stream=None):
+        """One step with these gradients (float32 or bfloat16, one per parameter)."""
+        grads = self._list(grads, ("float32", "bfloat16"), "AdamW.step grads")
+        c = self.cfg
+        c.lr = self.lr if lr is None else float(lr)
+        c.grad_scale = float(grad_scale)
+        c.step = self.steps + 1
+        for t, g in zip(self._tensors, grads):
+            t.d_grad = g.data_ptr()
+            t.grad_dtype = _dtype_code(g, "AdamW.step grads")
+        self._ordered(stream)
+        with _on(self.device, stream, self.states, *self.params, *grads) as st:
+            _ok(load().huge_adamw_step(ctypes.byref(c), self._tensors, len(grads),
+                                       self.status.data_ptr(), st), "huge_adamw_step")
+        self.steps += 1
+
+    def _pointers(self, ts):
+        return (ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
+
+    def values(self, stream=None):
+        """(m, v): lists of float32 tensors shaped like the parameters, copies of
+        the moments."""
+        import torch
+        self._ordered(stream)
+        with _on(self.device, stream, self.states) as st:
+            m, v = ([torch.empty(p.shape, dtype=torch.float32, device=self.device)
+                     for p in self.params] for _ in range(2))
+            _ok(load().huge_adamw_get_state(self._tensors, len(m), self.kind, self._pointers(m),
+                                            self._pointers(v), st), "huge_adamw_get_state")
+        return m, v
+
+    def load(self, m, v, steps, stream=None):
+        """Set the moments (float32, v >= 0) and the steps that they have seen."""
+        m = self._list(m, ("float32",), "AdamW.load m")
+        v = self._list(v, ("float32",), "AdamW.load v")
+        if int(steps) < 0:
+            raise ValueError(f"AdamW.load: {steps} steps")
+        self._ordered(stream)
+        with _on(self.device, stream, self.states, *m, *v) as st:
+            _ok(load().huge_adamw_set_state(self._tensors, len(m), self.kind, self._pointers(m),
+                                            self._pointers(v), st), "huge_adamw_set_state")
+        self.steps = int(steps)
+
+
+# --------------------------------------------------------------------------- #
+# A head that trains
+# --------------------------------------------------------------------------- #
+class SoftmaxHead:
+    """Layer norm, a linear layer and the softmax loss over num_classes classes on
+    rows of embeddings, trained by AdamW: the downstream classifier of Sec. 4.2,
+    or the exact softmax over all nodes that negative sampling stands in for.
+
+    step(x, labels) trains the head on rows x (n x dim) and returns the mean loss
+    (device) and the gradient of x, for a caller that trains the rows too."""
+
+    def __init__(self, num_classes, dim, max_rows, dtype="f32", lr=1e-3, weight_decay=0.01,
+                 states="f32", eps=1e-5, seed=0, device="cuda"):
+        import torch
+        self.op = SoftmaxLoss(max_rows, num_classes, dim, dtype=dtype, device=device)
+        dev = self.op.device
+        g = torch.Generator(device=dev).manual_seed(int(seed))
+        self.eps = float(eps)
+        self.gamma = torch.ones(dim, device=dev)
+        self.beta = torch.zeros(dim, device=dev)
+        w = torch.randn((num_classes, dim), device=dev, generator=g) * dim ** -0.5
+        self.w = w.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+        self.bias = torch.zeros(num_classes, device=dev)
+        self.opt = AdamW([self.gamma, self.beta, self.w, self.bias], lr=lr,
+                         weight_decay=weight_decay, states=states)
+        self.total = torch.zeros(1, dtype=torch.float64, device=dev)
+
+    def loss(self, x, labels, weights=None, stream=None):
+        """Loss per row, forward only."""
+        y, _, _ = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
+        return self.op.loss(y, self.w, labels, self.bias, weights, stream=stream)[0]
+
+    def step(self, x, labels, weights=None, lr=None, want_dx=True, stream=None):
+        """One training step on the mean over the rows of their losses."""
+        scale = 1.0 / max(1, x.shape[0])
+        y, mean, rstd = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
+        _, lse = self.op.loss(y, self.w, labels, self.bias, weights, total=self.total,
+                              stream=stream)
+        dy, dw, db = self.op.grad(y, self.w, labels, lse, self.bias, weights, scale=scale,
+                                  stream=stream)
+        dx, dgamma, dbeta = layer_norm_backward(dy, x, self.gamma, mean, rstd, want_dx=want_dx,
+                                                stream=stream)
+        self.opt.step([dgamma, dbeta, dw, db], lr=lr, stream=stream)
+        return self.total * scale, dx
+
+    def check(self):
+        """Raise the first device-side error since the last check."""
+        self.op.check()
+        self.opt.check()
