@@ -65,20 +65,18 @@ hipError_t launch_adamw_state(const AdamArgs& a, int64_t chunks, int32_t state_k
 // ---------------------------------------------------------------------------
 // Exact softmax loss (k_softmax.hip)
 // ---------------------------------------------------------------------------
-// Rows are packed in tiles of kSmTile, as the operands of 32x32x16 matrix
+// Rows are packed in records of kSmTile, as the operands of 32x32x16 matrix
 // products in the order in which a wave's lanes take them.
 constexpr int kSmTile = 32;
-constexpr int kSmWaves = 4;                             // waves of a workgroup
-constexpr int64_t kSmPieceBytes = (int64_t)2 << 30;     // packed table rows, at most
-constexpr int64_t kSmPartRows = 131072;                 // rows of partial sums, about
+constexpr int64_t kSmPieceBytes = (int64_t)2 << 30;  // packed table rows, at most
+constexpr int64_t kSmPartRows = 131072;              // rows of partial sums of a pass
 
 // How a call of n rows is laid out, from its sizes alone.
 struct SoftmaxPlan {
     int32_t dim, parts, nd, chunks, dp, kd;  // nd 32-wide blocks of dp in each of `chunks`
-    int64_t tile_elems;                      // bf16 elements of a packed tile, one form
     int64_t piece;                           // classes packed together (multiple of kSmTile)
     int64_t rows_pad;                        // n in whole tiles
-    size_t hr, ht, wr, wt, yterm, xrow, xlab, xcw, part, total;  // workspace offsets
+    size_t h, w, part, row_part, total;      // workspace offsets
 };
 SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype, bool grad);
 

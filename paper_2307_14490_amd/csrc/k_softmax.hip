@@ -7,27 +7,35 @@
 // registers and drops it: the loss keeps a running maximum and sum per row, the
 // two gradients multiply the tile at once.  S is formed three times in all, which
 // at the widths of embeddings costs less than a round trip of its elements
-// through memory: at 4 + 4 bytes an element that would be about 0.6 clocks of a
-// CU, and 2 D flops are 0.06 at D = 128.
+// through memory: 2 D flops are 0.06 clocks of a CU at D = 128, the 2 + 2 bytes of
+// an element kept in half width 0.4 at the rate of a copy.
 //
-// Both gradients are one kernel: X are the rows whose gradient is formed (one
-// tile or two per wave, in registers), Y the rows that are summed over.  A tile
-// is computed with Y as the rows and X as the columns of the product, so that a
-// lane holds 16 elements of one X row: sums, maxima and scales per X row need no
-// exchange between lanes, and the tile in its place is the second operand of the
+// Both gradients are one kernel: X are the rows whose gradient is formed (XB tiles
+// of 32 per wave, held in registers), Y the rows that are summed over.  A tile is
+// computed with Y as the rows and X as the columns of the product, so that a lane
+// holds 16 elements of one X row: sums, maxima and scales per X row need no
+// exchange between lanes, and the tile as it lies is the second operand of the
 // product with Y' (whose operand holds Y's rows in the order in which the first
-// product leaves them).  The terms per Y row (a class's bias; a row's
-// log weight - lse) are the initial value of the tile.
+// product leaves them).
 //
-// Operands are packed before: R form (rows as they enter S) and T form (rows as
-// they enter the second product), tiles of 32 rows, each 1 KB block being one
-// operand of a 32x32x16 product in lane order.  fp32 rows are three bf16 parts,
-// whose sum is the fp32 value exactly, and the six products of parts that are
-// not below 2^-24 of the whole are formed; so are those of the tile in the
-// second product.  bf16 rows are one part, and the tile is rounded to bf16
-// (after the label is subtracted, so that a probability near one keeps its small
-// complement): an error of 2^-8 of each term at most, as in the rounding of the result.
+// Operands are packed before, in records of 32 rows: a header with the rows'
+// terms, the R form (rows as they enter S) and the T form (rows as they enter the
+// second product), each 1 KB block one operand of a 32x32x16 product in lane order.
+// A workgroup streams Y's records through two LDS buffers (copied by the loads
+// that write LDS, while the other buffer is used); reads of an operand are 1 KB in
+// a row and meet no bank conflict.
+//
+// Precision.  bf16 rows enter as they are, and the tile is rounded to bf16 after
+// the label is subtracted, so that a probability near one keeps its small
+// complement: an error of 2^-8 of each term at most, as in the rounding of the
+// result.  fp32 rows are scaled by a power of two per row and split into two fp16
+// parts, hi + lo (22 bits of an element within 2^-17 of the row's largest, and
+// 2^-40 of that for smaller ones), and the products hi hi + hi lo + lo hi are
+// summed in fp32; the tile is split the same way under a scale per X row that
+// follows the largest element so far.  Maxima, sums and gradients are fp32.
 #include <math.h>
+
+#include <type_traits>
 
 #include "device.hpp"
 #include "head.hpp"
@@ -37,56 +45,104 @@ namespace huge {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+// Element types: how rows are split, and the product of two operands.
+template <typename E>
+struct Kind;
+
+template <>
+struct Kind<bf16_t> {
+    using Vec = bf16x8;
+    static constexpr int kParts = 1;
+    static constexpr bool kScaled = false;
+    static __device__ __forceinline__ f32x16 mfma(Vec a, Vec b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <>
+struct Kind<float> {
+    using Vec = f16x8;
+    static constexpr int kParts = 2;
+    static constexpr bool kScaled = true;
+    static __device__ __forceinline__ f32x16 mfma(Vec a, Vec b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <typename E>
+struct Operand {
+    typename Kind<E>::Vec p[Kind<E>::kParts];
+};
+
+// The parts of eight values: each the nearest to what the ones before leave.
+template <typename E>
+__device__ __forceinline__ Operand<E> split(f32x8 v) {
+    Operand<E> r;
+    r.p[0] = __builtin_convertvector(v, typename Kind<E>::Vec);
+    if constexpr (Kind<E>::kParts == 2)
+        r.p[1] = __builtin_convertvector(v - __builtin_convertvector(r.p[0], f32x8),
+                                         typename Kind<E>::Vec);
+    return r;
+}
+
+// c + a b.
+template <typename E>
+__device__ __forceinline__ f32x16 product(const Operand<E>& a, const Operand<E>& b, f32x16 c) {
+    if constexpr (Kind<E>::kParts == 2) {
+        c = Kind<E>::mfma(a.p[1], b.p[0], c);
+        c = Kind<E>::mfma(a.p[0], b.p[1], c);
+    }
+    return Kind<E>::mfma(a.p[0], b.p[0], c);
 }
 
 // Row of a product's register i in lane half h (the column is lane % 32).
 __device__ __forceinline__ int tile_row(int i, int h) { return 8 * (i / 4) + 4 * h + i % 4; }
 
-template <int PARTS>
-struct Parts {
-    bf16x8 p[PARTS];
+// A record's header: 32 of each.
+constexpr int kHeader = 1024;
+enum Field : int {
+    kTerm = 0,    // classes: bias, -inf where the class is out
+    kTerm2 = 1,   // the same times log2(e); rows: (log weight - lse) log2(e), -inf without a loss
+    kMul = 2,     // fp32: what the packed row is to be multiplied by
+    kLabel = 3,   // rows: label (int32), -1 without a loss
+    kWeight = 4,  // rows: weight
 };
+__device__ __forceinline__ const float* field(const uint8_t* rec, Field f) {
+    return reinterpret_cast<const float*>(rec) + 32 * f;
+}
 
-// The parts of eight values: each the nearest bf16 to what the ones before leave.
-template <int PARTS>
-__device__ __forceinline__ Parts<PARTS> split(f32x8 v) {
-    Parts<PARTS> r;
+// Bytes of a record: `forms` forms of nfrag operands and kParts parts.
+__host__ __device__ constexpr int record_bytes(int nfrag, int parts, int forms) {
+    return kHeader + forms * parts * nfrag * 1024;
+}
+
+// Operand f of the form that starts at `form`, whose parts are nfrag operands apart.
+template <typename E>
+__device__ __forceinline__ Operand<E> load_operand(const uint8_t* form, int f, int nfrag,
+                                                   int lane) {
+    using Vec = typename Kind<E>::Vec;
+    Operand<E> r;
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
-        r.p[k] = __builtin_convertvector(v, bf16x8);
-        if (k + 1 < PARTS) v -= __builtin_convertvector(r.p[k], f32x8);
-    }
+    for (int k = 0; k < Kind<E>::kParts; ++k)
+        r.p[k] = reinterpret_cast<const Vec*>(form)[(k * nfrag + f) * 64 + lane];
     return r;
 }
 
-// c + a b, over the products of parts that reach 2^-24 of the whole.
-template <int PARTS>
-__device__ __forceinline__ f32x16 mfma_parts(const Parts<PARTS>& a, const Parts<PARTS>& b,
-                                             f32x16 c) {
-    if constexpr (PARTS == 3) {
-        c = mfma(a.p[2], b.p[0], c);
-        c = mfma(a.p[0], b.p[2], c);
-        c = mfma(a.p[1], b.p[1], c);
-        c = mfma(a.p[1], b.p[0], c);
-        c = mfma(a.p[0], b.p[1], c);
-    }
-    return mfma(a.p[0], b.p[0], c);
-}
-
-// Operand `f` of a packed tile: parts lie `stride` operands apart.
-template <int PARTS>
-__device__ __forceinline__ Parts<PARTS> load_frag(const bf16x8* __restrict__ tile, int f,
-                                                  int stride, int lane) {
-    Parts<PARTS> r;
+// The 16 values that go with a lane's elements of a tile, from a header field.
+__device__ __forceinline__ f32x16 row_values(const uint8_t* rec, Field f, int half) {
+    const float4* v = reinterpret_cast<const float4*>(field(rec, f)) + half;
+    f32x16 r;
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) r.p[k] = tile[(k * stride + f) * 64 + lane];
+    for (int g = 0; g < 4; ++g) {
+        const float4 q = v[2 * g];
+        r[4 * g] = q.x, r[4 * g + 1] = q.y, r[4 * g + 2] = q.z, r[4 * g + 3] = q.w;
+    }
     return r;
 }
 
@@ -99,147 +155,345 @@ __device__ __forceinline__ void set_status(int32_t* status, int32_t code) {
 // ---------------------------------------------------------------------------
 struct PackArgs {
     const void* m;
-    int64_t ld, first, rows;  // rows first .. first + rows of the matrix
-    int dim, nfrag;           // operands of a tile and part, one form
-    const float* bias;        // classes: the tile's terms are these (or 0), -inf past the end
-    float* term;              // or null
-    const float* live;        // rows: those at -inf are packed as zeros
-    bf16x8* r;
-    bf16x8* t;                // or null
+    int64_t ld, first, count;  // rows first .. first + count of the matrix
+    int64_t tiles;
+    uint8_t* out;
+    bool classes;              // or rows
+    bool vec;                  // four elements at a time
 };
 
-// A workgroup packs 32 rows x 128 columns.
-template <typename E, int PARTS>
-__global__ __launch_bounds__(kBlock) void k_sm_pack(PackArgs a) {
-    __shared__ float s[32][132];
+constexpr int kPackCols = 256;
+
+// Four elements of a row at a column, 0 past its end.
+template <typename E>
+__device__ __forceinline__ float4 load_cols(const E* row, int col, int dim, bool vec) {
+    if (col >= dim) return zero4();
+    if (vec) return load_chunk(row + col, 0);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(E) == 4) v[e] = row[col + e];
+        else v[e] = __uint_as_float((uint32_t)row[col + e] << 16);
+    }
+    return make_float4(v[0], v[1], v[2], v[3]);
+}
+
+__device__ __forceinline__ float max4(float m, float4 v) {
+    return fmaxf(fmaxf(fmaxf(m, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
+}
+
+// A workgroup packs a record, 256 columns at a time through LDS; eight threads
+// read a row.
+template <typename E>
+__global__ __launch_bounds__(kBlock) void k_sm_pack(SoftmaxArgs a, PackArgs w, PackArgs h,
+                                                    int nfrag, int forms) {
+    constexpr int kParts = Kind<E>::kParts;
+    using Vec = typename Kind<E>::Vec;
+    __shared__ float s[32][kPackCols + 4];
     __shared__ bool s_out[32];
-    const int64_t tile = blockIdx.x;
-    const int col0 = blockIdx.y * 128;
+    __shared__ float s_mul[32];
+    const bool second = blockIdx.x >= w.tiles;
+    const PackArgs& k = second ? h : w;
+    const int64_t tile = second ? blockIdx.x - w.tiles : blockIdx.x;
+    uint8_t* rec = k.out + tile * record_bytes(nfrag, kParts, forms);
+    float* head = reinterpret_cast<float*>(rec);
     if (threadIdx.x < 32) {
-        const int64_t r = tile * 32 + threadIdx.x;
-        bool out = r >= a.rows;
-        if (a.term != nullptr) {
-            const float b = out ? -INFINITY : a.bias == nullptr ? 0.f : a.bias[a.first + r];
-            out = b == -INFINITY;
-            if (blockIdx.y == 0) a.term[r] = b;
+        const int r = threadIdx.x;
+        const int64_t i = tile * 32 + r;
+        bool out = i >= k.count;
+        float term = -INFINITY, term2 = -INFINITY, weight = 0.f;
+        int32_t label = -1;
+        if (k.classes) {
+            if (!out) term = a.bias == nullptr ? 0.f : a.bias[k.first + i];
+            out = term == -INFINITY;
+            term2 = term * kLog2e;
+        } else if (!out && forms == 2) {
+            label = a.labels[i];
+            weight = a.weight == nullptr ? 1.f : a.weight[i];
+            const bool bad_y = label < -1 || label >= a.classes;
+            const bool bad_c = !(weight >= 0.f && weight < INFINITY);
+            if (bad_y) set_status(a.status, -2);
+            else if (bad_c) set_status(a.status, -3);
+            if (bad_y || bad_c || label < 0 || weight == 0.f ||
+                (a.bias != nullptr && a.bias[label] == -INFINITY)) {
+                label = -1;
+                weight = 0.f;
+                out = true;
+            } else {
+                // rounded once: it reaches the exponent of every element of the row
+                term2 = (float)(((double)logf(weight) - (double)a.lse[i]) * 1.4426950408889634);
+            }
         }
-        if (a.live != nullptr && !out) out = a.live[r] == -INFINITY;
-        s_out[threadIdx.x] = out;
+        s_out[r] = out;
+        head[32 * kTerm + r] = term;
+        head[32 * kTerm2 + r] = term2;
+        reinterpret_cast<int32_t*>(head)[32 * kLabel + r] = label;
+        head[32 * kWeight + r] = weight;
     }
     __syncthreads();
-    const E* m = static_cast<const E*>(a.m);
-    for (int j = threadIdx.x; j < 32 * 128; j += kBlock) {
-        const int row = j >> 7, col = j & 127;
-        float v = 0.f;
-        if (!s_out[row] && col0 + col < a.dim) {
-            const E e = m[(a.first + tile * 32 + row) * a.ld + col0 + col];
-            if constexpr (sizeof(E) == 4) v = e;
-            else v = __uint_as_float((uint32_t)e << 16);
+    const int row = threadIdx.x >> 3, j0 = (threadIdx.x & 7) * 4;
+    const E* m = static_cast<const E*>(k.m) + (k.first + tile * 32 + row) * k.ld;
+    const bool out = s_out[row];
+    if constexpr (Kind<E>::kScaled) {
+        float big = 0.f;
+        if (!out)
+            for (int col = j0; col < a.dim; col += 32) big = max4(big, load_cols(m, col, a.dim, k.vec));
+        big = fmaxf(big, __shfl_xor(big, 1));
+        big = fmaxf(big, __shfl_xor(big, 2));
+        big = fmaxf(big, __shfl_xor(big, 4));
+        if ((threadIdx.x & 7) == 0) {
+            // big < 2^e: scaled by 2^(15 - e) the row is below 2^15
+            int e = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
+            e = e < -100 ? -100 : e;
+            s_mul[row] = ldexpf(1.f, 15 - e);
+            head[32 * kMul + row] = ldexpf(1.f, e - 15);
         }
-        s[row][col] = v;
+        __syncthreads();
     }
-    __syncthreads();
+    const float mul = Kind<E>::kScaled ? s_mul[row] : 1.f;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const int nd = a.nfrag / 2;
-    for (int k = wave; k < 8; k += 4) {
-        const int f = blockIdx.y * 8 + k;
-        if (f < a.nfrag) {
-            f32x8 v;
+    const int nd = nfrag / 2;
+    Vec* form = reinterpret_cast<Vec*>(rec + kHeader);
+    for (int c0 = 0; c0 < 16 * nfrag; c0 += kPackCols) {
+        for (int col = j0; col < kPackCols; col += 32)
+            *reinterpret_cast<float4*>(&s[row][col]) =
+                out ? zero4() : scale4(mul, load_cols(m, c0 + col, a.dim, k.vec));
+        __syncthreads();
+        for (int q = wave; q < kPackCols / 16; q += 4) {
+            const int f = c0 / 16 + q;
+            if (f < nfrag) {
+                f32x8 v;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = s[lane & 31][16 * k + 8 * half + j];
-            const Parts<PARTS> p = split<PARTS>(v);
+                for (int j = 0; j < 8; ++j) v[j] = s[lane & 31][16 * q + 8 * half + j];
+                const Operand<E> p = split<E>(v);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q)
-                a.r[((tile * PARTS + q) * a.nfrag + f) * 64 + lane] = p.p[q];
+                for (int part = 0; part < kParts; ++part)
+                    form[(part * nfrag + f) * 64 + lane] = p.p[part];
+            }
+            const int db = c0 / 32 + (q >> 1), t = q & 1;
+            if (forms == 2 && db < nd) {
+                f32x8 v;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    v[j] = s[16 * t + tile_row(j, half)][32 * (q >> 1) + (lane & 31)];
+                const Operand<E> p = split<E>(v);
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+                    form[((kParts + part) * nfrag + t * nd + db) * 64 + lane] = p.p[part];
+            }
         }
-        const int db = blockIdx.y * 4 + (k & 3), t = k >> 2;
-        if (a.t != nullptr && db < nd) {
-            f32x8 v;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                v[j] = s[16 * t + tile_row(j, half)][32 * (k & 3) + (lane & 31)];
-            const Parts<PARTS> p = split<PARTS>(v);
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q)
-                a.t[((tile * PARTS + q) * a.nfrag + t * nd + db) * 64 + lane] = p.p[q];
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// What the two kernels share: X in registers, Y's records through LDS
+// ---------------------------------------------------------------------------
+struct PassArgs {
+    const uint8_t* x;      // records of X and of Y
+    const uint8_t* y;
+    int64_t x_tiles, y_tiles;
+    int64_t per;           // Y tiles of a split
+    int32_t x_blocks, splits;
+    int32_t x_groups;      // waves of a workgroup side by side along X; the others share Y
+    int32_t stage;         // Y tiles of an LDS buffer
+    int32_t nfrag, kd;
+    int32_t forms;
+    bool first;            // the first piece of the classes: partial results are written
+    // loss
+    float2* lse_part;      // [split and wave along Y][32 x_tiles]: maximum and sum
+    // gradient
+    float* part;           // [split and wave along Y][32 x_tiles][dp], or null: to `out`
+    float* bias_part;      // the same without [dp] (X: classes), or null
+    void* out;             // x_rows x dim
+    float* bias_out;
+    int64_t class0;        // first class of the piece
+    int64_t x_rows;
+    int32_t dp, dim;
+    float scale;
+    bool want_bias;
+};
+
+// The workgroup's place.  Workgroups go to the eight XCDs in turn, and those that
+// read the same Y records should share an XCD's L2: with at least eight splits, a
+// split's workgroups are eight apart.
+struct Place {
+    int32_t x_block, split;
+};
+__device__ __forceinline__ Place place(const PassArgs& a) {
+    const int32_t b = blockIdx.x;
+    if (a.splits < 8) return {b % a.x_blocks, b / a.x_blocks};
+    const int32_t k = b >> 3;
+    return {k % a.x_blocks, (k / a.x_blocks) * 8 + (b & 7)};
+}
+inline int64_t place_grid(int64_t x_blocks, int64_t splits) {
+    return x_blocks * (splits < 8 ? splits : (splits + 7) / 8 * 8);
+}
+
+// Copies n KB to LDS, a wave 1 KB at a time; arrived after the next barrier.
+template <int WAVES>
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to, int n, int wave,
+                                            int lane) {
+    for (int k = wave; k < n; k += WAVES)
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(from + (int64_t)k * 1024 + lane * 16),
+            (__attribute__((address_space(3))) void*)(to + k * 1024), 16, 0, 0);
+}
+
+// Calls body(record) for this wave's Y tiles of the split: tiles yg, yg + yw, ... of
+// each stage.
+template <int WAVES, bool STAGED, typename Body>
+__device__ __forceinline__ void stream_records(const PassArgs& a, int split, int yg, int yw,
+                                               int wave, int lane, int rec_bytes, uint8_t* lds,
+                                               Body body) {
+    const int64_t y0 = (int64_t)split * a.per;
+    const int64_t y1 = y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
+    if constexpr (!STAGED) {
+        for (int64_t yt = y0 + yg; yt < y1; yt += yw) body(a.y + yt * rec_bytes, yt);
+    } else {
+        const int kb = rec_bytes / 1024;
+        auto tiles = [&](int64_t at) { return (int)(y1 - at < a.stage ? y1 - at : a.stage); };
+        uint8_t* buf = lds;
+        uint8_t* next = lds + a.stage * rec_bytes;
+        if (y0 < y1) copy_to_lds<WAVES>(a.y + y0 * rec_bytes, buf, tiles(y0) * kb, wave, lane);
+        __syncthreads();
+        for (int64_t at = y0; at < y1; at += a.stage) {
+            const int64_t after = at + a.stage;
+            if (after < y1)
+                copy_to_lds<WAVES>(a.y + after * rec_bytes, next, tiles(after) * kb, wave, lane);
+            const int n = tiles(at);
+            for (int t = yg; t < n; t += yw) body(buf + t * rec_bytes, at + t);
+            __syncthreads();
+            uint8_t* b = buf;
+            buf = next;
+            next = b;
         }
     }
+}
+
+// The logits of a tile against XB tiles of X, before the scales of fp32 rows.
+template <typename E, int ND, int XB, bool STAGED>
+__device__ __forceinline__ void tile_products(const uint8_t* rec, const Operand<E> (*x)[2 * ND],
+                                              const uint8_t* const* xrec, int nfrag, int kd,
+                                              int lane, f32x16* c) {
+    const uint8_t* form = rec + kHeader;
+    if constexpr (STAGED) {
+#pragma unroll
+        for (int k = 0; k < 2 * ND; ++k) {
+            const Operand<E> y = load_operand<E>(form, k, 2 * ND, lane);
+#pragma unroll
+            for (int b = 0; b < XB; ++b) c[b] = product<E>(y, x[b][k], c[b]);
+        }
+    } else {
+        for (int k = 0; k < kd; ++k) {
+            const Operand<E> y = load_operand<E>(form, k, nfrag, lane);
+#pragma unroll
+            for (int b = 0; b < XB; ++b)
+                c[b] = product<E>(y, load_operand<E>(xrec[b] + kHeader, k, nfrag, lane), c[b]);
+        }
+    }
+}
+
+// X's tiles of a wave.
+template <int XB>
+struct XTiles {
+    int64_t t[XB];
+    bool in[XB];  // tiles past the end repeat the last one, and are not stored
+    const uint8_t* rec[XB];
+};
+template <int XB>
+__device__ __forceinline__ XTiles<XB> x_tiles_of(const PassArgs& a, int x_block, int xg,
+                                                 int rec_bytes) {
+    XTiles<XB> r;
+#pragma unroll
+    for (int b = 0; b < XB; ++b) {
+        int64_t t = ((int64_t)x_block * a.x_groups + xg) * XB + b;
+        r.in[b] = t < a.x_tiles;
+        if (!r.in[b]) t = a.x_tiles - 1;
+        r.t[b] = t;
+        r.rec[b] = a.x + t * rec_bytes;
+    }
+    return r;
 }
 
 // ---------------------------------------------------------------------------
 // Loss: running maximum and sum
 // ---------------------------------------------------------------------------
-struct LseArgs {
-    const bf16x8* x;     // rows, R form
-    const bf16x8* y;     // classes, R form
-    const float* term;   // a class's bias, -inf for those that are out
-    int64_t x_tiles, y_tiles, per;  // y tiles of a split
-    int nfrag, kd;
-    bool first;          // the first piece of the classes
-    float2* part;        // [split][32 x_tiles]: maximum and sum
-};
-
 // exp(a - b) for a <= b, 0 where a is -inf (also if b is).
 __device__ __forceinline__ float exp_below(float a, float b) {
     return a == -INFINITY ? 0.f : exp2f((a - b) * kLog2e);
 }
 
-template <int ND, int PARTS, bool XREG>
-__global__ __launch_bounds__(kSmWaves * 64) void k_sm_lse(LseArgs a) {
+template <typename E, int ND, int XB, int WAVES, bool STAGED>
+__global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_lse(PassArgs a) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    const Place at = place(a);
+    if (at.split >= a.splits) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int64_t xt = (int64_t)blockIdx.x * kSmWaves + (threadIdx.x >> 6);
-    if (xt >= a.x_tiles) return;
-    const bf16x8* xp = a.x + xt * PARTS * a.nfrag * 64;
-    constexpr int KD = 2 * ND;
-    Parts<PARTS> x[XREG ? KD : 1];
-    if constexpr (XREG) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int xg = wave % a.x_groups, yg = wave / a.x_groups, yw = WAVES / a.x_groups;
+    const int nfrag = STAGED ? 2 * ND : a.nfrag;
+    const int rec_bytes = record_bytes(nfrag, Kind<E>::kParts, a.forms);
+    const XTiles<XB> xt = x_tiles_of<XB>(a, at.x_block, xg, rec_bytes);
+    Operand<E> x[XB][2 * ND];
+    float xmul[XB], top[XB], sum[XB];
 #pragma unroll
-        for (int k = 0; k < KD; ++k) x[k] = load_frag<PARTS>(xp, k, a.nfrag, lane);
+    for (int b = 0; b < XB; ++b) {
+        if constexpr (STAGED) {
+#pragma unroll
+            for (int k = 0; k < 2 * ND; ++k)
+                x[b][k] = load_operand<E>(xt.rec[b] + kHeader, k, 2 * ND, lane);
+        }
+        xmul[b] = Kind<E>::kScaled ? field(xt.rec[b], kMul)[lane & 31] : 1.f;
+        top[b] = -INFINITY;
+        sum[b] = 0.f;
     }
-    const int64_t y0 = (int64_t)blockIdx.y * a.per;
-    const int64_t y1 = y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
-    float2* out = a.part + (int64_t)blockIdx.y * a.x_tiles * 32 + xt * 32 + (lane & 31);
-    float top = -INFINITY, sum = 0.f;
-    for (int64_t yt = y0; yt < y1; ++yt) {
-        const bf16x8* yp = a.y + yt * PARTS * a.nfrag * 64;
-        const float4* term = reinterpret_cast<const float4*>(a.term + yt * 32) + half;
-        f32x16 c;
+    stream_records<WAVES, STAGED>(
+        a, at.split, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t) {
+            f32x16 c[XB];
+            const f32x16 term = row_values(rec, kTerm, half);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float4 b = term[2 * g];
-            c[4 * g] = b.x, c[4 * g + 1] = b.y, c[4 * g + 2] = b.z, c[4 * g + 3] = b.w;
+            for (int b = 0; b < XB; ++b) c[b] = Kind<E>::kScaled ? f32x16{} : term;
+            tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
+            if constexpr (Kind<E>::kScaled) {
+                const f32x16 ymul = row_values(rec, kMul, half);
+#pragma unroll
+                for (int b = 0; b < XB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        c[b][i] = fmaf(c[b][i] * ymul[i], xmul[b], term[i]);
+            }
+#pragma unroll
+            for (int b = 0; b < XB; ++b) {
+                float m = top[b];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m = fmaxf(m, c[b][i]);
+                const float ref = m == -INFINITY ? 0.f : m;
+                sum[b] *= exp_below(top[b], ref);
+                top[b] = m;
+                const float sub = -ref * kLog2e;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    sum[b] += __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, sub));
+            }
+        });
+#pragma unroll
+    for (int b = 0; b < XB; ++b) {
+        // the halves hold different classes of the same row
+        const float top2 = __shfl_xor(top[b], 32), sum2 = __shfl_xor(sum[b], 32);
+        float m = fmaxf(top[b], top2);
+        float v = sum[b] * exp_below(top[b], m) + sum2 * exp_below(top2, m);
+        if (half == 0 && xt.in[b]) {
+            float2* out = a.lse_part + ((int64_t)at.split * yw + yg) * a.x_tiles * 32 +
+                          xt.t[b] * 32 + lane;
+            if (!a.first) {
+                const float2 p = *out;
+                const float mm = fmaxf(m, p.x);
+                v = v * exp_below(m, mm) + p.y * exp_below(p.x, mm);
+                m = mm;
+            }
+            *out = make_float2(m, v);
         }
-        if constexpr (XREG) {
-#pragma unroll
-            for (int k = 0; k < KD; ++k)
-                c = mfma_parts<PARTS>(load_frag<PARTS>(yp, k, a.nfrag, lane), x[k], c);
-        } else {
-            for (int k = 0; k < a.kd; ++k)
-                c = mfma_parts<PARTS>(load_frag<PARTS>(yp, k, a.nfrag, lane),
-                                      load_frag<PARTS>(xp, k, a.nfrag, lane), c);
-        }
-        float m = top;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) m = fmaxf(m, c[i]);
-        const float ref = m == -INFINITY ? 0.f : m;
-        sum *= exp_below(top, ref);
-        top = m;
-        const float sub = -ref * kLog2e;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(c[i], kLog2e, sub));
-    }
-    // the halves hold different classes of the same row
-    const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
-    float m = fmaxf(top, top2);
-    sum = sum * exp_below(top, m) + sum2 * exp_below(top2, m);
-    if (half == 0) {
-        if (!a.first) {
-            const float2 p = *out;
-            const float mm = fmaxf(m, p.x);
-            sum = sum * exp_below(m, mm) + p.y * exp_below(p.x, mm);
-            m = mm;
-        }
-        *out = make_float2(m, sum);
     }
 }
 
@@ -316,53 +570,6 @@ __global__ __launch_bounds__(1024) void k_sm_sum(const float* __restrict__ loss,
 // ---------------------------------------------------------------------------
 // Gradients
 // ---------------------------------------------------------------------------
-// Per row: log weight - lse (-inf without a loss), the label (-1 then) and the
-// weight, in whole tiles.
-__global__ __launch_bounds__(kBlock) void k_sm_rows(SoftmaxArgs a, int64_t pad,
-                                                    float* __restrict__ term,
-                                                    int32_t* __restrict__ label,
-                                                    float* __restrict__ cw) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= pad) return;
-    float t = -INFINITY, c = 0.f;
-    int32_t y = -1;
-    if (i < a.n) {
-        y = a.labels[i];
-        c = a.weight == nullptr ? 1.f : a.weight[i];
-        const bool bad_y = y < -1 || y >= a.classes, bad_c = !(c >= 0.f && c < INFINITY);
-        if (bad_y) set_status(a.status, -2);
-        else if (bad_c) set_status(a.status, -3);
-        if (bad_y || bad_c || y < 0 || c == 0.f || (a.bias != nullptr && a.bias[y] == -INFINITY)) {
-            y = -1;
-            c = 0.f;
-        } else {
-            t = logf(c) - a.lse[i];
-        }
-    }
-    term[i] = t;
-    label[i] = y;
-    cw[i] = c;
-}
-
-struct GradArgs {
-    const bf16x8* xr;      // X, R form
-    const bf16x8* yr;      // Y, R form and T form
-    const bf16x8* yt;
-    const float* xterm;    // what is added to the tile per X row and per Y row
-    const float* yterm;
-    const int32_t* label;  // of the rows (X or Y)
-    const float* cw;
-    int64_t class0;        // first class of the piece
-    int64_t x_rows, x_tiles, y_tiles, per;
-    int nfrag, kd, dp, dim;
-    bool first;            // partial sums: written, else added to
-    float* part;           // [split][32 x_tiles][dp], or null: to `out`
-    float* bias_part;      // [split][32 x_tiles] (X: classes), or null
-    void* out;             // x_rows x dim
-    float* bias_out;
-    float scale;
-};
-
 template <typename E>
 __device__ __forceinline__ void store_out(E* p, float4 v, float scale) {
     // alignment of the element type is all that the caller owes
@@ -375,131 +582,212 @@ __device__ __forceinline__ void store_out(E* p, float4 v, float scale) {
 }
 
 // ROWS: X are the rows and Y the classes (dh), else X are the classes (dw).
-template <typename E, int ND, int PARTS, bool ROWS, bool XREG>
-__global__ __launch_bounds__(kSmWaves * 64) void k_sm_grad(GradArgs a) {
+template <typename E, int ND, int XB, int WAVES, bool STAGED, bool ROWS>
+__global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    constexpr bool kScaled = Kind<E>::kScaled;
+    const Place at = place(a);
+    if (at.split >= a.splits) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int64_t xt = (int64_t)blockIdx.x * kSmWaves + (threadIdx.x >> 6);
-    if (xt >= a.x_tiles) return;
-    const int db0 = blockIdx.z * ND, nd = a.nfrag / 2;
-    const bf16x8* xp = a.xr + xt * PARTS * a.nfrag * 64;
-    constexpr int KD = 2 * ND;
-    Parts<PARTS> x[XREG ? KD : 1];
-    if constexpr (XREG) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int xg = wave % a.x_groups, yg = wave / a.x_groups, yw = WAVES / a.x_groups;
+    const int nfrag = STAGED ? 2 * ND : a.nfrag;
+    const int rec_bytes = record_bytes(nfrag, Kind<E>::kParts, 2);
+    const int db0 = blockIdx.y * ND, nd = nfrag / 2;
+    const XTiles<XB> xt = x_tiles_of<XB>(a, at.x_block, xg, rec_bytes);
+    Operand<E> x[XB][2 * ND];
+    // per X row: the factor and the term of its exponents (a class's bias is the
+    // initial value of its column where that is not scaled), the label (for
+    // classes: the class itself) and the weight
+    float xmul[XB], xterm[XB], xw[XB], bias[XB], pscale[XB];
+    int64_t xl[XB];
+    f32x16 acc[XB][ND];
 #pragma unroll
-        for (int k = 0; k < KD; ++k) x[k] = load_frag<PARTS>(xp, k, a.nfrag, lane);
+    for (int b = 0; b < XB; ++b) {
+        if constexpr (STAGED) {
+#pragma unroll
+            for (int k = 0; k < 2 * ND; ++k)
+                x[b][k] = load_operand<E>(xt.rec[b] + kHeader, k, 2 * ND, lane);
+        }
+        const int r = lane & 31;
+        xmul[b] = kScaled ? field(xt.rec[b], kMul)[r] * kLog2e : kLog2e;
+        xterm[b] = field(xt.rec[b], ROWS || kScaled ? kTerm2 : kTerm)[r];
+        xw[b] = ROWS ? field(xt.rec[b], kWeight)[r] : 0.f;
+        const int32_t label = reinterpret_cast<const int32_t*>(field(xt.rec[b], kLabel))[r];
+        xl[b] = ROWS ? (label < 0 ? -1 : label - a.class0) : a.class0 + xt.t[b] * 32 + r;
+        bias[b] = 0.f;
+        pscale[b] = 0x1p100f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[b][d] = f32x16{};
     }
-    const int64_t xi = xt * 32 + (lane & 31);
-    const float xterm = a.xterm[xi];
-    // the label that this lane's elements are compared with: a class of this piece,
-    // or (X: classes) the lane's class against each row's label
-    const int64_t xl = ROWS ? (int64_t)a.label[xi] - a.class0 : a.class0 + xi;
-    const float xc = ROWS ? a.cw[xi] : 0.f;
-    f32x16 acc[ND];
+    stream_records<WAVES, STAGED>(
+        a, at.split, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t yt) {
+            f32x16 c[XB];
 #pragma unroll
-    for (int d = 0; d < ND; ++d) acc[d] = f32x16{};
-    float bias = 0.f;
-    const int64_t y0 = (int64_t)blockIdx.y * a.per;
-    const int64_t y1 = y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
-    for (int64_t yt = y0; yt < y1; ++yt) {
-        const bf16x8* yp = a.yr + yt * PARTS * a.nfrag * 64;
-        const bf16x8* tp = a.yt + yt * PARTS * a.nfrag * 64;
-        const float4* term = reinterpret_cast<const float4*>(a.yterm + yt * 32) + half;
-        f32x16 c;
+            for (int b = 0; b < XB; ++b) {
+                if constexpr (kScaled) {
+                    c[b] = f32x16{};
+                } else if constexpr (ROWS) {
+                    c[b] = row_values(rec, kTerm, half);
+                } else {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float4 b = term[2 * g];
-            c[4 * g] = b.x, c[4 * g + 1] = b.y, c[4 * g + 2] = b.z, c[4 * g + 3] = b.w;
-        }
-        if constexpr (XREG) {
-#pragma unroll
-            for (int k = 0; k < KD; ++k)
-                c = mfma_parts<PARTS>(load_frag<PARTS>(yp, k, a.nfrag, lane), x[k], c);
-        } else {
-            for (int k = 0; k < a.kd; ++k)
-                c = mfma_parts<PARTS>(load_frag<PARTS>(yp, k, a.nfrag, lane),
-                                      load_frag<PARTS>(xp, k, a.nfrag, lane), c);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) c[i] = __builtin_amdgcn_exp2f((c[i] + xterm) * kLog2e);
-        // the label's element, in the few tiles that hold one
-        if constexpr (ROWS) {
-            const int64_t at = xl - yt * 32;
-            if (__ballot(at >= 0 && at < 32 && a.label[xi] >= 0) != 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (at == tile_row(i, half)) c[i] -= xc;
+                    for (int i = 0; i < 16; ++i) c[b][i] = xterm[b];
+                }
             }
-        } else {
-            const int32_t* lab = a.label + yt * 32;
-            const int64_t at = (int64_t)lab[lane & 31] - (a.class0 + xt * 32);
-            if (__ballot(at >= 0 && at < 32) != 0) {
+            tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
+            // probabilities times the weight
+            if constexpr (kScaled) {
+                const f32x16 ymul = row_values(rec, kMul, half);
+                const f32x16 yterm = row_values(rec, kTerm2, half);
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (lab[tile_row(i, half)] == xl) c[i] -= a.cw[yt * 32 + tile_row(i, half)];
+                for (int b = 0; b < XB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        c[b][i] = __builtin_amdgcn_exp2f(
+                            fmaf(c[b][i] * ymul[i], xmul[b], yterm[i]) + xterm[b]);
+            } else if constexpr (ROWS) {
+#pragma unroll
+                for (int b = 0; b < XB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, xterm[b]));
+            } else {
+                const f32x16 yterm = row_values(rec, kTerm2, half);
+#pragma unroll
+                for (int b = 0; b < XB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, yterm[i]));
             }
-            if (a.bias_part != nullptr || a.bias_out != nullptr) {
+            // the labels' elements, in the tiles that hold one
 #pragma unroll
-                for (int i = 0; i < 16; ++i) bias += c[i];
+            for (int b = 0; b < XB; ++b) {
+                if constexpr (ROWS) {
+                    const int64_t d = xl[b] - yt * 32;
+                    if (__ballot(d >= 0 && d < 32) != 0) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (d == tile_row(i, half)) c[b][i] -= xw[b];
+                    }
+                } else {
+                    const int32_t* lab = reinterpret_cast<const int32_t*>(field(rec, kLabel));
+                    const int64_t d = lab[lane & 31] - (a.class0 + xt.t[b] * 32);
+                    if (__ballot(d >= 0 && d < 32) != 0) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = tile_row(i, half);
+                            if (lab[r] == xl[b]) c[b][i] -= field(rec, kWeight)[r];
+                        }
+                    }
+                    if (a.want_bias) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) bias[b] += c[b][i];
+                    }
+                }
             }
-        }
+            if constexpr (kScaled) {
+                const f32x16 ymul = row_values(rec, kMul, half);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x8 v;
+                for (int b = 0; b < XB; ++b) {
+                    float big = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = c[8 * t + j];
-            const Parts<PARTS> p = split<PARTS>(v);
+                    for (int i = 0; i < 16; ++i) {
+                        c[b][i] *= ymul[i];
+                        big = fmaxf(big, fabsf(c[b][i]));
+                    }
+                    // the halves share the sums of a row: they share its scale
+                    big = fmaxf(big, __shfl_xor(big, 32));
+                    if (__ballot(big * pscale[b] > 0x1p15f) != 0) {
+                        float s = pscale[b];
+                        if (big * s > 0x1p15f)
+                            s = fminf(s, ldexpf(1.f, 15 - __builtin_amdgcn_frexp_expf(big)));
+                        const float ratio = s / pscale[b];
+                        pscale[b] = s;
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
-                acc[d] = mfma_parts<PARTS>(
-                    load_frag<PARTS>(tp, t * nd + db0 + d, a.nfrag, lane), p, acc[d]);
-        }
-    }
-    const int64_t row = (int64_t)blockIdx.y * a.x_tiles * 32 + xi;
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * (db0 + d) + 8 * g + 4 * half;
-            float4 v = make_float4(acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2],
-                                   acc[d][4 * g + 3]);
-            if (a.part != nullptr) {
-                float4* p = reinterpret_cast<float4*>(a.part + row * a.dp + col);
-                *p = a.first ? v : add4(*p, v);
-            } else if (a.out != nullptr && xi < a.x_rows && col < a.dim) {
-                store_out(static_cast<E*>(a.out) + xi * a.dim + col, v, a.scale);
+                        for (int d = 0; d < ND; ++d) acc[b][d] *= ratio;
+                    }
+                    c[b] *= pscale[b];
+                }
             }
-        }
-    }
-    if (!ROWS && blockIdx.z == 0) {
-        bias += __shfl_xor(bias, 32);
-        if (half == 0) {
-            if (a.bias_part != nullptr) a.bias_part[row] = bias;
-            else if (a.bias_out != nullptr && xi < a.x_rows) a.bias_out[xi] = bias * a.scale;
+            Operand<E> p[XB][2];
+#pragma unroll
+            for (int b = 0; b < XB; ++b)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    f32x8 v;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = c[b][8 * t + j];
+                    p[b][t] = split<E>(v);
+                }
+            const uint8_t* form = rec + kHeader + Kind<E>::kParts * nfrag * 1024;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const Operand<E> y = load_operand<E>(form, t * nd + db0 + d, nfrag, lane);
+#pragma unroll
+                    for (int b = 0; b < XB; ++b) acc[b][d] = product<E>(y, p[b][t], acc[b][d]);
+                }
+        });
+#pragma unroll
+    for (int b = 0; b < XB; ++b) {
+        if (!xt.in[b]) continue;
+        const int64_t xi = xt.t[b] * 32 + (lane & 31);
+        const int64_t row = ((int64_t)at.split * yw + yg) * a.x_tiles * 32 + xi;
+        const float back = kScaled ? 1.f / pscale[b] : 1.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * (db0 + d) + 8 * g + 4 * half;
+                float4 v = make_float4(acc[b][d][4 * g], acc[b][d][4 * g + 1],
+                                       acc[b][d][4 * g + 2], acc[b][d][4 * g + 3]);
+                if constexpr (kScaled) v = scale4(back, v);
+                if (a.part != nullptr) {
+                    float4* p = reinterpret_cast<float4*>(a.part + row * a.dp + col);
+                    *p = a.first ? v : add4(*p, v);
+                } else if (a.out != nullptr && xi < a.x_rows && col < a.dim) {
+                    store_out(static_cast<E*>(a.out) + xi * a.dim + col, v, a.scale);
+                }
+            }
+        if (!ROWS && blockIdx.y == 0 && a.want_bias) {
+            const float v = bias[b] + __shfl_xor(bias[b], 32);
+            if (half == 0) {
+                if (a.bias_part != nullptr) a.bias_part[row] = v;
+                else if (xi < a.x_rows) a.bias_out[xi] = v * a.scale;
+            }
         }
     }
 }
 
-// The splits' partial sums, in order.
-template <typename E>
+// The splits' partial sums, in an order that the sizes fix: LANES threads take
+// every LANES-th split of four columns, then add up.
+template <typename E, int LANES>
 __global__ __launch_bounds__(kBlock) void k_sm_join(const float* __restrict__ part, int splits,
                                                     int64_t rows_pad, int dp, int64_t rows,
                                                     int dim, float scale, E* __restrict__ out,
                                                     const float* __restrict__ bias_part,
                                                     float* __restrict__ bias_out) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / LANES;
+    const int lane = threadIdx.x % LANES;
     const int q = dim / 4;
     if (out != nullptr && i < rows * q) {
         const int64_t row = i / q;
         const int col = (int)(i % q) * 4;
         float4 v = zero4();
-        for (int s = 0; s < splits; ++s)
+#pragma unroll 4
+        for (int s = lane; s < splits; s += LANES)
             v = add4(v, *reinterpret_cast<const float4*>(part + (s * rows_pad + row) * dp + col));
-        store_out(out + row * dim + col, v, scale);
+        v = make_float4(group_sum<LANES>(v.x), group_sum<LANES>(v.y), group_sum<LANES>(v.z),
+                        group_sum<LANES>(v.w));
+        if (lane == 0) store_out(out + row * dim + col, v, scale);
     }
     if (bias_out != nullptr && i < rows) {
         float v = 0.f;
-        for (int s = 0; s < splits; ++s) v += bias_part[s * rows_pad + i];
-        bias_out[i] = v * scale;
+#pragma unroll 4
+        for (int s = lane; s < splits; s += LANES) v += bias_part[s * rows_pad + i];
+        v = group_sum<LANES>(v);
+        if (lane == 0) bias_out[i] = v * scale;
     }
 }
 
@@ -508,21 +796,51 @@ __global__ __launch_bounds__(kBlock) void k_sm_join(const float* __restrict__ pa
 // ---------------------------------------------------------------------------
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-struct Splits {
-    int64_t count, per;
+// Tiles of X per wave and waves of a workgroup: what keeps X, the sums and a tile
+// within the registers of two waves per SIMD (256), or of one where that cannot be.
+template <typename E, int ND, bool GRAD>
+struct Shape {
+    static constexpr int kXB = sizeof(E) == 4 ? (ND <= (GRAD ? 1 : 2) ? 2 : 1) : (ND <= 2 || !GRAD ? 2 : 1);
+    static constexpr int kWaves = sizeof(E) == 4 && ND == 8 ? 4 : 8;
 };
 
-// Enough workgroups to fill the card, from splits of the summed rows; not more
-// rows of partial sums than kSmPartRows (or one split's).
-Splits split_tiles(int64_t x_tiles, int64_t y_tiles) {
-    const int64_t blocks = div_up(x_tiles, kSmWaves);
-    int64_t want = div_up(1024, blocks);
-    const int64_t room = kSmPartRows / (x_tiles * 32);
+constexpr int kSmLds = 152 * 1024;
+
+struct Layout {
+    int32_t x_groups, stage;
+    int64_t x_blocks, splits, per, slots;  // slots: partial results per row
+};
+
+// Workgroups along X and splits of Y: enough to fill the card twice, unless a split
+// had fewer than four tiles a wave; not more partial rows than kSmPartRows (or one
+// slot's).
+Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int rec_bytes, bool staged) {
+    Layout l{};
+    const int64_t groups = div_up(x_tiles, xb);
+    int64_t stage = staged ? kSmLds / 2 / rec_bytes : waves;
+    if (stage > waves) stage = waves;
+    if (stage < 1) stage = 1;
+    int g = waves;
+    while (g > 1 && g / 2 >= groups && waves / (g / 2) <= stage) g /= 2;
+    l.x_groups = g;
+    const int yw = waves / g;
+    l.x_blocks = div_up(groups, g);
+    int64_t want = div_up(512, l.x_blocks);
+    const int64_t room = kSmPartRows / (x_tiles * 32 * yw);
+    const int64_t most = y_tiles / (4 * yw);
+    if (want > most) want = most;
     if (want > room) want = room;
-    if (want > y_tiles) want = y_tiles;
     if (want < 1) want = 1;
-    const int64_t per = div_up(y_tiles, want);
-    return {div_up(y_tiles, per), per};
+    l.per = div_up(y_tiles, want);
+    l.splits = div_up(y_tiles, l.per);
+    l.slots = l.splits * yw;
+    // a stage of about 32 KB, whole rounds of the waves along Y
+    int64_t st = 32 * 1024 / rec_bytes;
+    if (st < yw) st = yw;
+    st = st / yw * yw;
+    if (st > stage) st = stage / yw * yw;
+    l.stage = (int32_t)(st < 1 ? 1 : st);
+    return l;
 }
 
 #define HUGE_SM_ND(ND_, ...)                            \
@@ -536,72 +854,80 @@ Splits split_tiles(int64_t x_tiles, int64_t y_tiles) {
         default: return hipErrorInvalidValue;           \
     }
 
-template <typename E>
-constexpr int kPartsOf = sizeof(E) == 4 ? 3 : 1;
-
-template <typename E>
-hipError_t pack(const SoftmaxPlan& p, PackArgs a, int64_t tiles, hipStream_t s) {
-    a.dim = p.dim;
-    a.nfrag = p.dp / 16;
-    const dim3 grid((uint32_t)tiles, (uint32_t)div_up(p.dp, 128));
-    k_sm_pack<E, kPartsOf<E>><<<grid, kBlock, 0, s>>>(a);
-    return hipGetLastError();
-}
-
-template <typename E>
-hipError_t lse_pass(const SoftmaxPlan& p, const LseArgs& a, int64_t splits, hipStream_t s) {
-    const dim3 grid((uint32_t)div_up(a.x_tiles, kSmWaves), (uint32_t)splits);
-    HUGE_SM_ND(p.nd, if (p.chunks == 1) {
-        k_sm_lse<ND, kPartsOf<E>, true><<<grid, kSmWaves * 64, 0, s>>>(a);
-    } else {
-        k_sm_lse<ND, kPartsOf<E>, false><<<grid, kSmWaves * 64, 0, s>>>(a);
-    })
-    return hipGetLastError();
-}
-
-template <typename E, bool ROWS>
-hipError_t grad_pass(const SoftmaxPlan& p, const GradArgs& a, int64_t splits, hipStream_t s) {
-    const dim3 grid((uint32_t)div_up(a.x_tiles, kSmWaves), (uint32_t)splits, (uint32_t)p.chunks);
-    HUGE_SM_ND(p.nd, if (p.chunks == 1) {
-        k_sm_grad<E, ND, kPartsOf<E>, ROWS, true><<<grid, kSmWaves * 64, 0, s>>>(a);
-    } else {
-        k_sm_grad<E, ND, kPartsOf<E>, ROWS, false><<<grid, kSmWaves * 64, 0, s>>>(a);
-    })
-    return hipGetLastError();
-}
-
 #define SM_TRY(expr)                        \
     do {                                    \
         const hipError_t e_ = (expr);       \
         if (e_ != hipSuccess) return e_;    \
     } while (0)
 
+template <auto* KERNEL>
+hipError_t launch_pass(const PassArgs& a, int waves, int chunks, int lds, hipStream_t s) {
+    if (lds > 64 * 1024) SM_TRY(allow_lds<KERNEL>(kSmLds));
+    const dim3 grid((uint32_t)place_grid(a.x_blocks, a.splits), (uint32_t)chunks);
+    KERNEL<<<grid, waves * 64, lds, s>>>(a);
+    return hipGetLastError();
+}
+
+// Fills in the layout and launches the pass; `fit` sets the outputs from it.
+template <typename E, int ND, bool GRAD, bool STAGED, bool ROWS, typename Fit>
+hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
+    constexpr int kXB = STAGED ? Shape<E, ND, GRAD>::kXB : 1;
+    constexpr int kWaves = Shape<E, ND, GRAD>::kWaves;
+    const int rec = record_bytes(p.dp / 16, p.parts, a.forms);
+    // all pieces are laid out as the first, whose partial results they add to
+    const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves, rec,
+                             STAGED);
+    a.x_groups = l.x_groups, a.stage = l.stage, a.x_blocks = (int32_t)l.x_blocks;
+    a.splits = (int32_t)l.splits, a.per = l.per;
+    a.nfrag = p.dp / 16, a.kd = p.kd, a.dp = p.dp, a.dim = p.dim;
+    fit(a, l);
+    const int lds = STAGED ? 2 * l.stage * rec : 0;
+    if constexpr (GRAD)
+        return launch_pass<&k_sm_grad<E, ND, kXB, kWaves, STAGED, ROWS>>(a, kWaves, p.chunks, lds,
+                                                                        s);
+    else
+        return launch_pass<&k_sm_lse<E, ND, kXB, kWaves, STAGED>>(a, kWaves, 1, lds, s);
+}
+
+template <typename E, bool GRAD, bool ROWS, typename Fit>
+hipError_t pass(const SoftmaxPlan& p, const PassArgs& a, Fit fit, hipStream_t s) {
+    HUGE_SM_ND(p.nd, return p.chunks == 1 ? run_pass<E, ND, GRAD, true, ROWS>(p, a, fit, s)
+                                          : run_pass<E, ND, GRAD, false, ROWS>(p, a, fit, s))
+    return hipErrorInvalidValue;
+}
+
+bool fours(const void* m, int64_t ld, size_t elem) {
+    return (reinterpret_cast<uintptr_t>(m) & (4 * elem - 1)) == 0 && ld % 4 == 0;
+}
+
+// Packs a piece of the classes, and before the first the rows.
+template <typename E>
+hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t count, int forms,
+                hipStream_t s) {
+    PackArgs w{}, h{};
+    w.m = a.w, w.ld = a.ld_w, w.first = c0, w.count = count, w.tiles = div_up(count, kSmTile);
+    w.out = a.ws + p.w, w.classes = true, w.vec = fours(a.w, a.ld_w, sizeof(E));
+    h.m = a.h, h.ld = a.ld_h, h.count = a.n, h.tiles = c0 == 0 ? p.rows_pad / kSmTile : 0;
+    h.out = a.ws + p.h, h.vec = fours(a.h, a.ld_h, sizeof(E));
+    k_sm_pack<E><<<dim3((uint32_t)(w.tiles + h.tiles)), kBlock, 0, s>>>(a, w, h, p.dp / 16, forms);
+    return hipGetLastError();
+}
+
 template <typename E>
 hipError_t softmax_loss(const SoftmaxArgs& a, hipStream_t s) {
     const SoftmaxPlan p = softmax_plan(a.classes, a.n, a.dim, a.dtype, false);
-    auto at = [&](size_t off) { return a.ws + off; };
-    const int64_t x_tiles = p.rows_pad / kSmTile;
-    float2* part = reinterpret_cast<float2*>(at(p.part));
-    PackArgs h{};
-    h.m = a.h, h.ld = a.ld_h, h.rows = a.n;
-    h.r = reinterpret_cast<bf16x8*>(at(p.hr));
-    SM_TRY(pack<E>(p, h, x_tiles, s));
-    const Splits sp = split_tiles(x_tiles, p.piece / kSmTile);
+    float2* part = reinterpret_cast<float2*>(a.ws + p.part);
+    int64_t slots = 0;
     for (int64_t c0 = 0; c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
-        PackArgs w{};
-        w.m = a.w, w.ld = a.ld_w, w.first = c0, w.rows = count, w.bias = a.bias;
-        w.term = reinterpret_cast<float*>(at(p.yterm));
-        w.r = reinterpret_cast<bf16x8*>(at(p.wr));
-        SM_TRY(pack<E>(p, w, div_up(count, kSmTile), s));
-        LseArgs l{};
-        l.x = h.r, l.y = w.r, l.term = w.term;
-        l.x_tiles = x_tiles, l.y_tiles = div_up(count, kSmTile), l.per = sp.per;
-        l.nfrag = p.dp / 16, l.kd = p.kd, l.first = c0 == 0, l.part = part;
-        SM_TRY(lse_pass<E>(p, l, sp.count, s));
+        SM_TRY(pack<E>(p, a, c0, count, 1, s));
+        PassArgs l{};
+        l.x = a.ws + p.h, l.y = a.ws + p.w, l.forms = 1;
+        l.x_tiles = p.rows_pad / kSmTile, l.y_tiles = div_up(count, kSmTile);
+        l.first = c0 == 0, l.lse_part = part;
+        SM_TRY((pass<E, false, true>(p, l, [&](PassArgs&, const Layout& o) { slots = o.slots; }, s)));
     }
-    k_sm_loss<E><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)sp.count,
-                                                                  p.rows_pad);
+    k_sm_loss<E><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, p.rows_pad);
     SM_TRY(hipGetLastError());
     if (a.loss_sum != nullptr) {
         k_sm_sum<<<1, 1024, 0, s>>>(a.loss, a.n, a.loss_sum);
@@ -611,77 +937,68 @@ hipError_t softmax_loss(const SoftmaxArgs& a, hipStream_t s) {
 }
 
 template <typename E>
-hipError_t join(const SoftmaxPlan& p, const float* part, int64_t splits, int64_t rows_pad,
+hipError_t join(const SoftmaxPlan& p, const float* part, int64_t slots, int64_t rows_pad,
                 int64_t rows, float scale, void* out, const float* bias_part, float* bias_out,
                 hipStream_t s) {
     const int64_t work = out != nullptr ? rows * (p.dim / 4) : rows;
-    k_sm_join<E><<<dim3((uint32_t)div_up(work, kBlock)), kBlock, 0, s>>>(
-        part, (int)splits, rows_pad, p.dp, rows, p.dim, scale, static_cast<E*>(out), bias_part,
-        bias_out);
+    E* o = static_cast<E*>(out);
+    // few outputs of many splits: 16 threads each
+    if (work < (1 << 18) && slots >= 16)
+        k_sm_join<E, 16><<<dim3((uint32_t)div_up(work * 16, kBlock)), kBlock, 0, s>>>(
+            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, bias_part, bias_out);
+    else
+        k_sm_join<E, 1><<<dim3((uint32_t)div_up(work, kBlock)), kBlock, 0, s>>>(
+            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, bias_part, bias_out);
     return hipGetLastError();
 }
 
 template <typename E>
 hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
     const SoftmaxPlan p = softmax_plan(a.classes, a.n, a.dim, a.dtype, true);
-    auto at = [&](size_t off) { return a.ws + off; };
     const int64_t x_tiles = p.rows_pad / kSmTile;
-    float* row_term = reinterpret_cast<float*>(at(p.xrow));
-    int32_t* label = reinterpret_cast<int32_t*>(at(p.xlab));
-    float* cw = reinterpret_cast<float*>(at(p.xcw));
-    float* part = reinterpret_cast<float*>(at(p.part));
-    k_sm_rows<<<dim3((uint32_t)div_up(p.rows_pad, kBlock)), kBlock, 0, s>>>(a, p.rows_pad, row_term,
-                                                                           label, cw);
-    SM_TRY(hipGetLastError());
-    PackArgs h{};
-    h.m = a.h, h.ld = a.ld_h, h.rows = a.n, h.live = row_term;
-    h.r = reinterpret_cast<bf16x8*>(at(p.hr));
-    h.t = reinterpret_cast<bf16x8*>(at(p.ht));
-    SM_TRY(pack<E>(p, h, x_tiles, s));
-    const Splits sp = split_tiles(x_tiles, p.piece / kSmTile);
-    const bool direct = sp.count == 1 && p.piece >= a.classes;
+    float* class_part = reinterpret_cast<float*>(a.ws + p.part);
+    float* row_part = reinterpret_cast<float*>(a.ws + p.row_part);
+    int64_t row_slots = 0;
     for (int64_t c0 = 0; c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
         const int64_t w_tiles = div_up(count, kSmTile);
-        PackArgs w{};
-        w.m = a.w, w.ld = a.ld_w, w.first = c0, w.rows = count, w.bias = a.bias;
-        w.term = reinterpret_cast<float*>(at(p.yterm));
-        w.r = reinterpret_cast<bf16x8*>(at(p.wr));
-        w.t = reinterpret_cast<bf16x8*>(at(p.wt));
-        SM_TRY(pack<E>(p, w, w_tiles, s));
-        GradArgs g{};
-        g.label = label, g.cw = cw, g.class0 = c0, g.scale = a.scale;
-        g.nfrag = p.dp / 16, g.kd = p.kd, g.dp = p.dp, g.dim = p.dim;
+        SM_TRY(pack<E>(p, a, c0, count, 2, s));
+        PassArgs g{};
+        g.class0 = c0, g.scale = a.scale, g.forms = 2;
         if (a.dw != nullptr || a.dbias != nullptr) {
-            const Splits sw = split_tiles(w_tiles, x_tiles);
-            g.xr = w.r, g.yr = h.r, g.yt = h.t, g.xterm = w.term, g.yterm = row_term;
-            g.x_rows = count, g.x_tiles = w_tiles, g.y_tiles = x_tiles, g.per = sw.per;
-            g.first = true;
+            // the second product is formed also where only the bias is wanted
             E* out = a.dw == nullptr ? nullptr : static_cast<E*>(a.dw) + c0 * p.dim;
             float* bias_out = a.dbias == nullptr ? nullptr : a.dbias + c0;
-            // the second product is formed also where only the bias is wanted
-            g.part = sw.count > 1 ? part : nullptr;
-            g.bias_part = sw.count > 1 ? part + sw.count * w_tiles * 32 * p.dp : nullptr;
-            g.out = out, g.bias_out = bias_out;
-            SM_TRY((grad_pass<E, false>(p, g, sw.count, s)));
-            if (sw.count > 1)
-                SM_TRY(join<E>(p, part, sw.count, w_tiles * 32, count, a.scale, out, g.bias_part,
+            g.x = a.ws + p.w, g.y = a.ws + p.h, g.x_tiles = w_tiles, g.y_tiles = x_tiles;
+            g.x_rows = count, g.first = true, g.out = out, g.bias_out = bias_out;
+            g.want_bias = bias_out != nullptr;
+            int64_t slots = 0;
+            float* bias_part = nullptr;
+            SM_TRY((pass<E, true, false>(p, g, [&](PassArgs& q, const Layout& o) {
+                slots = o.slots;
+                if (slots == 1) return;
+                q.part = class_part;
+                bias_part = class_part + slots * w_tiles * 32 * p.dp;
+                q.bias_part = bias_part;
+            }, s)));
+            if (slots > 1)
+                SM_TRY(join<E>(p, class_part, slots, w_tiles * 32, count, a.scale, out, bias_part,
                                bias_out, s));
         }
         if (a.dh != nullptr) {
-            // the partial sums of the rows lie behind those of the classes: they
-            // stay from piece to piece
-            g.xr = h.r, g.yr = w.r, g.yt = w.t, g.xterm = row_term, g.yterm = w.term;
-            g.x_rows = a.n, g.x_tiles = x_tiles, g.y_tiles = w_tiles, g.per = sp.per;
-            g.first = c0 == 0;
-            g.part = direct ? nullptr : part + (kSmPartRows + 32) * (p.dp + 1);
-            g.bias_part = nullptr, g.bias_out = nullptr, g.out = a.dh;
-            SM_TRY((grad_pass<E, true>(p, g, sp.count, s)));
+            g.x = a.ws + p.h, g.y = a.ws + p.w, g.x_tiles = x_tiles, g.y_tiles = w_tiles;
+            g.x_rows = a.n, g.first = c0 == 0, g.out = a.dh, g.bias_out = nullptr;
+            g.want_bias = false;
+            SM_TRY((pass<E, true, true>(p, g, [&](PassArgs& q, const Layout& o) {
+                row_slots = o.slots;
+                // sums that stay from piece to piece
+                if (row_slots > 1 || p.piece < a.classes) q.part = row_part;
+                else row_slots = 0;
+            }, s)));
         }
     }
-    if (a.dh != nullptr && !direct)
-        SM_TRY(join<E>(p, part + (kSmPartRows + 32) * (p.dp + 1), sp.count, p.rows_pad, a.n,
-                       a.scale, a.dh, nullptr, nullptr, s));
+    if (a.dh != nullptr && row_slots > 0)
+        SM_TRY(join<E>(p, row_part, row_slots, p.rows_pad, a.n, a.scale, a.dh, nullptr, nullptr, s));
     return hipSuccess;
 }
 
@@ -690,18 +1007,16 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
 SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype, bool grad) {
     SoftmaxPlan p{};
     p.dim = dim;
-    p.parts = dtype == kDtypeBf16 ? 1 : 3;
+    p.parts = dtype == kDtypeBf16 ? Kind<bf16_t>::kParts : Kind<float>::kParts;
     const int nd = (int)div_up(dim, 32);
     p.chunks = (int)div_up(nd, 8);
     p.nd = (int)div_up(nd, p.chunks);
     if (p.nd == 5 || p.nd == 7) ++p.nd;
     p.dp = 32 * p.nd * p.chunks;
     p.kd = (int)div_up(dim, 16);
-    p.tile_elems = (int64_t)kSmTile * p.dp * p.parts;
-    const int64_t forms = grad ? 2 : 1;
-    const int64_t row_bytes = 2 * (int64_t)p.dp * p.parts * forms;
+    const int64_t rec = record_bytes(p.dp / 16, p.parts, grad ? 2 : 1);
     p.piece = div_up(classes, kSmTile) * kSmTile;
-    const int64_t most = kSmPieceBytes / row_bytes / kSmTile * kSmTile;
+    const int64_t most = kSmPieceBytes / rec * kSmTile;
     if (p.piece > most) p.piece = most;
     p.rows_pad = n > 0 ? div_up(n, kSmTile) * kSmTile : kSmTile;
     size_t off = 0;
@@ -710,19 +1025,11 @@ SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype,
         off += ((size_t)bytes + 255) & ~(size_t)255;
         return o;
     };
-    const int64_t h_bytes = 2 * (int64_t)p.dp * p.parts * p.rows_pad;
-    const int64_t w_bytes = 2 * (int64_t)p.dp * p.parts * p.piece;
-    p.hr = take(h_bytes);
-    p.ht = take(grad ? h_bytes : 0);
-    p.wr = take(w_bytes);
-    p.wt = take(grad ? w_bytes : 0);
-    p.yterm = take(4 * p.piece);
-    p.xrow = take(grad ? 4 * p.rows_pad : 0);
-    p.xlab = take(grad ? 4 * p.rows_pad : 0);
-    p.xcw = take(grad ? 4 * p.rows_pad : 0);
+    p.h = take(p.rows_pad / kSmTile * rec);
+    p.w = take(p.piece / kSmTile * rec);
     const int64_t rows = p.rows_pad > kSmPartRows ? p.rows_pad : kSmPartRows;
-    p.part = take(grad ? 4 * ((kSmPartRows + 32) * (int64_t)(p.dp + 1) + rows * (int64_t)p.dp)
-                       : 8 * rows);
+    p.part = take(grad ? 4 * kSmPartRows * (int64_t)(p.dp + 1) : 8 * rows);
+    p.row_part = take(grad ? 4 * rows * (int64_t)p.dp : 0);
     p.total = off;
     return p;
 }
