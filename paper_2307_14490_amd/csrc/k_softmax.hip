@@ -46,6 +46,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -134,16 +135,27 @@ __device__ __forceinline__ Operand<E> load_operand(const uint8_t* form, int f, i
     return r;
 }
 
-// The 16 values that go with a lane's elements of a tile, from a header field.
+// The 16 values that go with a lane's elements of a tile, from a header field.  LDS
+// is read here, as everywhere in the loops below, as vector types: a read of
+// another type is taken to alias the copy in flight, and waits for it.
+__device__ __forceinline__ f32x4 row_four(const uint8_t* rec, Field f, int half, int g) {
+    return reinterpret_cast<const f32x4*>(field(rec, f))[2 * g + half];
+}
 __device__ __forceinline__ f32x16 row_values(const uint8_t* rec, Field f, int half) {
-    const float4* v = reinterpret_cast<const float4*>(field(rec, f)) + half;
     f32x16 r;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        const float4 q = v[2 * g];
+        const f32x4 q = row_four(rec, f, half, g);
         r[4 * g] = q.x, r[4 * g + 1] = q.y, r[4 * g + 2] = q.z, r[4 * g + 3] = q.w;
     }
     return r;
+}
+
+// A lane's value of a header field (its row is the lane's column).
+__device__ __forceinline__ int32_t lane_label(const uint8_t* rec, int lane) {
+    typedef int32_t one __attribute__((ext_vector_type(2)));
+    const one v = reinterpret_cast<const one*>(field(rec, kLabel))[(lane & 31) >> 1];
+    return lane & 1 ? v.y : v.x;
 }
 
 __device__ __forceinline__ void set_status(int32_t* status, int32_t code) {
@@ -314,20 +326,20 @@ struct PassArgs {
     bool want_bias;
 };
 
-// The workgroup's place.  Workgroups go to the eight XCDs in turn, and those that
-// read the same Y records should share an XCD's L2: with at least eight splits, a
-// split's workgroups are eight apart.
+// The workgroup's place.  Workgroups go to the eight XCDs in turn; each XCD takes a
+// run of the places in the order of the splits, so that workgroups which read the
+// same Y records share an L2.
 struct Place {
     int32_t x_block, split;
 };
 __device__ __forceinline__ Place place(const PassArgs& a) {
-    const int32_t b = blockIdx.x;
-    if (a.splits < 8) return {b % a.x_blocks, b / a.x_blocks};
-    const int32_t k = b >> 3;
-    return {k % a.x_blocks, (k / a.x_blocks) * 8 + (b & 7)};
+    const int32_t total = a.x_blocks * a.splits, run = (total + 7) / 8;
+    const int32_t k = (int32_t)(blockIdx.x & 7) * run + (int32_t)(blockIdx.x >> 3);
+    const bool none = k >= total || (int32_t)(blockIdx.x >> 3) >= run;
+    return {k % a.x_blocks, none ? a.splits : k / a.x_blocks};
 }
 inline int64_t place_grid(int64_t x_blocks, int64_t splits) {
-    return x_blocks * (splits < 8 ? splits : (splits + 7) / 8 * 8);
+    return (x_blocks * splits + 7) / 8 * 8;
 }
 
 // Copies n KB to LDS, a wave 1 KB at a time; arrived after the next barrier.
@@ -371,6 +383,41 @@ __device__ __forceinline__ void stream_records(const PassArgs& a, int split, int
     }
 }
 
+// Operands of a form that a wave reads ahead of the products that use them.  An LDS
+// read takes as long as two to four products; left alone the compiler reads one or
+// two ahead.
+template <typename E, int N>
+struct Ahead {
+    static constexpr int kMost = 4 / Kind<E>::kParts;
+    static constexpr int kCount = N < kMost ? N : kMost;
+    Operand<E> q[kCount];
+
+    template <typename Load>
+    __device__ __forceinline__ void start(Load load) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) q[i] = load(i);
+    }
+    // use(i, operand i) for all of them, each read kCount uses before.
+    template <int PRODUCTS, typename Load, typename Use>
+    __device__ __forceinline__ void run(Load load, Use use) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            use(i, q[i % kCount]);
+            if (i + kCount < N) q[i % kCount] = load(i + kCount);
+        }
+        constexpr int kMfma = 0x8, kDsRead = 0x100;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, PRODUCTS, 0);
+            if (i + kCount < N)
+                __builtin_amdgcn_sched_group_barrier(kDsRead, Kind<E>::kParts, 0);
+        }
+    }
+};
+
+template <typename E>
+constexpr int kProducts = Kind<E>::kParts == 2 ? 3 : 1;  // matrix products of two operands
+
 // The logits of a tile against XB tiles of X, before the scales of fp32 rows.
 template <typename E, int ND, int XB, bool STAGED>
 __device__ __forceinline__ void tile_products(const uint8_t* rec, const Operand<E> (*x)[2 * ND],
@@ -378,12 +425,14 @@ __device__ __forceinline__ void tile_products(const uint8_t* rec, const Operand<
                                               int lane, f32x16* c) {
     const uint8_t* form = rec + kHeader;
     if constexpr (STAGED) {
+        auto load = [&](int k) { return load_operand<E>(form, k, 2 * ND, lane); };
+        Ahead<E, 2 * ND> y;
+        y.start(load);
+        __builtin_amdgcn_sched_barrier(0);
+        y.template run<kProducts<E> * XB>(load, [&](int k, const Operand<E>& q) {
 #pragma unroll
-        for (int k = 0; k < 2 * ND; ++k) {
-            const Operand<E> y = load_operand<E>(form, k, 2 * ND, lane);
-#pragma unroll
-            for (int b = 0; b < XB; ++b) c[b] = product<E>(y, x[b][k], c[b]);
-        }
+            for (int b = 0; b < XB; ++b) c[b] = product<E>(q, x[b][k], c[b]);
+        });
     } else {
         for (int k = 0; k < kd; ++k) {
             const Operand<E> y = load_operand<E>(form, k, nfrag, lane);
@@ -424,8 +473,9 @@ __device__ __forceinline__ float exp_below(float a, float b) {
     return a == -INFINITY ? 0.f : exp2f((a - b) * kLog2e);
 }
 
-template <typename E, int ND, int XB, int WAVES, bool STAGED>
-__global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_lse(PassArgs a) {
+template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED>
+__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+void k_sm_lse(PassArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
     const Place at = place(a);
     if (at.split >= a.splits) return;
@@ -582,8 +632,9 @@ __device__ __forceinline__ void store_out(E* p, float4 v, float scale) {
 }
 
 // ROWS: X are the rows and Y the classes (dh), else X are the classes (dw).
-template <typename E, int ND, int XB, int WAVES, bool STAGED, bool ROWS>
-__global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
+template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED, bool ROWS>
+__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+void k_sm_grad(PassArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
     constexpr bool kScaled = Kind<E>::kScaled;
     const Place at = place(a);
@@ -600,7 +651,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
     // initial value of its column where that is not scaled), the label (for
     // classes: the class itself) and the weight
     float xmul[XB], xterm[XB], xw[XB], bias[XB], pscale[XB];
-    int64_t xl[XB];
+    int32_t xl[XB];
     f32x16 acc[XB][ND];
 #pragma unroll
     for (int b = 0; b < XB; ++b) {
@@ -613,8 +664,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
         xmul[b] = kScaled ? field(xt.rec[b], kMul)[r] * kLog2e : kLog2e;
         xterm[b] = field(xt.rec[b], ROWS || kScaled ? kTerm2 : kTerm)[r];
         xw[b] = ROWS ? field(xt.rec[b], kWeight)[r] : 0.f;
-        const int32_t label = reinterpret_cast<const int32_t*>(field(xt.rec[b], kLabel))[r];
-        xl[b] = ROWS ? (label < 0 ? -1 : label - a.class0) : a.class0 + xt.t[b] * 32 + r;
+        const int32_t label = lane_label(xt.rec[b], lane);
+        // classes fit 31 bits; a label of an earlier piece is below 0 here
+        xl[b] = (int32_t)(ROWS ? (label < 0 ? -1 : label - a.class0)
+                               : a.class0 + xt.t[b] * 32 + r);
         bias[b] = 0.f;
         pscale[b] = 0x1p100f;
 #pragma unroll
@@ -635,6 +688,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
                 }
             }
             tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
+            // the first operands of the second product are read behind the exponentials
+            const uint8_t* form = rec + kHeader + Kind<E>::kParts * nfrag * 1024;
+            auto load = [&](int f) {
+                return load_operand<E>(form, (f / ND) * nd + db0 + f % ND, nfrag, lane);
+            };
+            Ahead<E, 2 * ND> y;
+            y.start(load);
+            __builtin_amdgcn_sched_barrier(0);
             // probabilities times the weight
             if constexpr (kScaled) {
                 const f32x16 ymul = row_values(rec, kMul, half);
@@ -652,31 +713,37 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
                     for (int i = 0; i < 16; ++i)
                         c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, xterm[b]));
             } else {
-                const f32x16 yterm = row_values(rec, kTerm2, half);
 #pragma unroll
-                for (int b = 0; b < XB; ++b)
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 yterm = row_four(rec, kTerm2, half, g);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, yterm[i]));
+                    for (int b = 0; b < XB; ++b)
+#pragma unroll
+                        for (int i = 4 * g; i < 4 * g + 4; ++i)
+                            c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, yterm[i - 4 * g]));
+                }
             }
             // the labels' elements, in the tiles that hold one
 #pragma unroll
             for (int b = 0; b < XB; ++b) {
                 if constexpr (ROWS) {
-                    const int64_t d = xl[b] - yt * 32;
-                    if (__ballot(d >= 0 && d < 32) != 0) {
+                    const int32_t d = xl[b] - (int32_t)yt * 32;
+                    if (__ballot((uint32_t)d < 32u) != 0) {
+                        const int32_t e = d - 4 * half;
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            if (d == tile_row(i, half)) c[b][i] -= xw[b];
+                            if (e == tile_row(i, 0)) c[b][i] -= xw[b];
                     }
                 } else {
-                    const int32_t* lab = reinterpret_cast<const int32_t*>(field(rec, kLabel));
-                    const int64_t d = lab[lane & 31] - (a.class0 + xt.t[b] * 32);
-                    if (__ballot(d >= 0 && d < 32) != 0) {
+                    const int32_t d = lane_label(rec, lane) - (int32_t)(a.class0 + xt.t[b] * 32);
+                    if (__ballot((uint32_t)d < 32u) != 0) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int r = tile_row(i, half);
-                            if (lab[r] == xl[b]) c[b][i] -= field(rec, kWeight)[r];
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x4 label = row_four(rec, kLabel, half, g);
+                            const f32x4 weight = row_four(rec, kWeight, half, g);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (__float_as_int(label[i]) == xl[b]) c[b][4 * g + i] -= weight[i];
                         }
                     }
                     if (a.want_bias) {
@@ -719,15 +786,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_sm_grad(PassArgs a) {
                     for (int j = 0; j < 8; ++j) v[j] = c[b][8 * t + j];
                     p[b][t] = split<E>(v);
                 }
-            const uint8_t* form = rec + kHeader + Kind<E>::kParts * nfrag * 1024;
+            y.template run<kProducts<E> * XB>(load, [&](int f, const Operand<E>& q) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const Operand<E> y = load_operand<E>(form, t * nd + db0 + d, nfrag, lane);
-#pragma unroll
-                    for (int b = 0; b < XB; ++b) acc[b][d] = product<E>(y, p[b][t], acc[b][d]);
-                }
+                for (int b = 0; b < XB; ++b)
+                    acc[b][f % ND] = product<E>(q, p[b][f / ND], acc[b][f % ND]);
+            });
         });
 #pragma unroll
     for (int b = 0; b < XB; ++b) {
@@ -796,12 +859,16 @@ __global__ __launch_bounds__(kBlock) void k_sm_join(const float* __restrict__ pa
 // ---------------------------------------------------------------------------
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Tiles of X per wave and waves of a workgroup: what keeps X, the sums and a tile
-// within the registers of two waves per SIMD (256), or of one where that cannot be.
+// Waves per SIMD, waves of a workgroup and tiles of X per wave, as the registers of
+// X, the sums and a tile allow.
 template <typename E, int ND, bool GRAD>
 struct Shape {
-    static constexpr int kXB = sizeof(E) == 4 ? (ND <= (GRAD ? 1 : 2) ? 2 : 1) : (ND <= 2 || !GRAD ? 2 : 1);
-    static constexpr int kWaves = sizeof(E) == 4 && ND == 8 ? 4 : 8;
+    static constexpr bool kWide = sizeof(E) == 4;  // fp32: two parts
+    static constexpr int kXB = !GRAD && !kWide && ND <= 4 ? 2 : 1;
+    static constexpr int kOcc = !GRAD ? (kWide ? (ND <= 4 ? 4 : 2) : 4)
+                              : kWide ? (ND <= 1 ? 4 : ND <= 2 ? 3 : ND <= 4 ? 2 : 1)
+                                      : (ND <= 2 ? 4 : ND <= 4 ? 3 : 2);
+    static constexpr int kWaves = kOcc == 4 ? 8 : 4 * kOcc;
 };
 
 constexpr int kSmLds = 152 * 1024;
@@ -811,13 +878,16 @@ struct Layout {
     int64_t x_blocks, splits, per, slots;  // slots: partial results per row
 };
 
-// Workgroups along X and splits of Y: enough to fill the card twice, unless a split
-// had fewer than four tiles a wave; not more partial rows than kSmPartRows (or one
-// slot's).
-Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int rec_bytes, bool staged) {
+constexpr int64_t kCus = 256;
+
+// Workgroups along X and splits of Y: whole rounds of the card's places (`resident`
+// workgroups of a CU), unless a split had fewer than four tiles a wave; not more
+// partial rows than kSmPartRows (or one slot's).
+Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident, int rec_bytes,
+               bool staged) {
     Layout l{};
     const int64_t groups = div_up(x_tiles, xb);
-    int64_t stage = staged ? kSmLds / 2 / rec_bytes : waves;
+    int64_t stage = staged ? kSmLds / 2 / resident / rec_bytes : waves;
     if (stage > waves) stage = waves;
     if (stage < 1) stage = 1;
     int g = waves;
@@ -825,12 +895,22 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int rec_byte
     l.x_groups = g;
     const int yw = waves / g;
     l.x_blocks = div_up(groups, g);
-    int64_t want = div_up(512, l.x_blocks);
+    int64_t most = y_tiles / (4 * yw);
     const int64_t room = kSmPartRows / (x_tiles * 32 * yw);
-    const int64_t most = y_tiles / (4 * yw);
-    if (want > most) want = most;
-    if (want > room) want = room;
-    if (want < 1) want = 1;
+    if (most > room) most = room;
+    int64_t want = 1;
+    double best = 0.0;
+    for (int64_t rounds = 1; rounds <= 4 && best < 0.95; ++rounds) {
+        const int64_t places = kCus * resident * rounds;
+        int64_t n = places / l.x_blocks;
+        if (n > most) n = most;
+        if (n < 1) break;
+        const double fill = (double)(n * l.x_blocks) / (double)places;
+        if (fill > best + 0.02) {
+            best = fill;
+            want = n;
+        }
+    }
     l.per = div_up(y_tiles, want);
     l.splits = div_up(y_tiles, l.per);
     l.slots = l.splits * yw;
@@ -872,27 +952,31 @@ hipError_t launch_pass(const PassArgs& a, int waves, int chunks, int lds, hipStr
 template <typename E, int ND, bool GRAD, bool STAGED, bool ROWS, typename Fit>
 hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
     constexpr int kXB = STAGED ? Shape<E, ND, GRAD>::kXB : 1;
-    constexpr int kWaves = Shape<E, ND, GRAD>::kWaves;
+    constexpr int kWaves = STAGED ? Shape<E, ND, GRAD>::kWaves : 8;
+    constexpr int kOcc = STAGED ? Shape<E, ND, GRAD>::kOcc : 2;
     const int rec = record_bytes(p.dp / 16, p.parts, a.forms);
     // all pieces are laid out as the first, whose partial results they add to
-    const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves, rec,
-                             STAGED);
+    const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves,
+                             kOcc * 4 / kWaves, rec, STAGED);
     a.x_groups = l.x_groups, a.stage = l.stage, a.x_blocks = (int32_t)l.x_blocks;
     a.splits = (int32_t)l.splits, a.per = l.per;
     a.nfrag = p.dp / 16, a.kd = p.kd, a.dp = p.dp, a.dim = p.dim;
     fit(a, l);
     const int lds = STAGED ? 2 * l.stage * rec : 0;
     if constexpr (GRAD)
-        return launch_pass<&k_sm_grad<E, ND, kXB, kWaves, STAGED, ROWS>>(a, kWaves, p.chunks, lds,
+        return launch_pass<&k_sm_grad<E, ND, kXB, kWaves, kOcc, STAGED, ROWS>>(a, kWaves, p.chunks, lds,
                                                                         s);
     else
-        return launch_pass<&k_sm_lse<E, ND, kXB, kWaves, STAGED>>(a, kWaves, 1, lds, s);
+        return launch_pass<&k_sm_lse<E, ND, kXB, kWaves, kOcc, STAGED>>(a, kWaves, 1, lds, s);
 }
 
 template <typename E, bool GRAD, bool ROWS, typename Fit>
 hipError_t pass(const SoftmaxPlan& p, const PassArgs& a, Fit fit, hipStream_t s) {
-    HUGE_SM_ND(p.nd, return p.chunks == 1 ? run_pass<E, ND, GRAD, true, ROWS>(p, a, fit, s)
-                                          : run_pass<E, ND, GRAD, false, ROWS>(p, a, fit, s))
+    HUGE_SM_ND(p.nd, {
+        if (p.chunks == 1) return run_pass<E, ND, GRAD, true, ROWS>(p, a, fit, s);
+        // rows above 256 columns: at least five blocks in each of two chunks or more
+        if constexpr (ND >= 6) return run_pass<E, ND, GRAD, false, ROWS>(p, a, fit, s);
+    })
     return hipErrorInvalidValue;
 }
 
