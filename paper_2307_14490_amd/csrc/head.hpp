@@ -97,6 +97,7 @@ struct SoftmaxArgs {
     float* dbias;
     int32_t* status;
     uint8_t* ws;
+    bool vec, vec16;      // h and w can be read four elements, 16 bytes at a time
 };
 hipError_t launch_softmax_loss(const SoftmaxArgs& a, hipStream_t s);
 hipError_t launch_softmax_grad(const SoftmaxArgs& a, hipStream_t s);

@@ -547,34 +547,198 @@ void k_sm_lse(PassArgs a) {
     }
 }
 
-// lse and loss of a row, a wave each: the splits are joined in order, and the
-// label's logit is formed from the rows themselves.
+// ---------------------------------------------------------------------------
+// Loss of few rows
+// ---------------------------------------------------------------------------
+// With few rows the table is read once and that is all: no packing.  A wave takes
+// 16 classes at a time, each lane 16 bytes of one class's row, which are an operand
+// of a 16x16 product as they lie (fp32: exact fp32 products); the rows h are the
+// other operand, from LDS.  A lane then holds four classes' logits of one row.
+// Loads run one group of kFewGroup operands ahead.  Bound by memory: 1e6 x 128
+// fp32, one row, see the measurement at launch_few.
+constexpr int kFewGroup = 8;
+constexpr int kFewWaves = 4;
+constexpr int kFewLds = 60 * 1024;
+
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+
 template <typename E>
+struct Few;
+template <>
+struct Few<bf16_t> {
+    static constexpr int kCols = 32;   // columns of a 16x16 product
+    using Vec = bf16x8;
+    static __device__ __forceinline__ f32x4v mfma(Vec a, Vec b, f32x4v c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <>
+struct Few<float> {
+    static constexpr int kCols = 16;   // of four 16x16x4 products
+    using Vec = f32x4;
+    static __device__ __forceinline__ f32x4v mfma(Vec a, Vec b, f32x4v c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// 16 bytes of a row at a column, 0 past its end.
+template <typename E, bool VEC>
+__device__ __forceinline__ typename Few<E>::Vec load_few_cols(const E* row, int col, int dim) {
+    using Vec = typename Few<E>::Vec;
+    constexpr int kN = 16 / sizeof(E);
+    union {
+        Vec v;
+        E e[kN];
+    } u;
+    if constexpr (VEC) {
+        u.v = col < dim ? *reinterpret_cast<const Vec*>(row + col) : Vec{};
+    } else {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) u.e[j] = col + j < dim ? row[col + j] : (E)0;
+    }
+    return u.v;
+}
+
+// NB blocks of 16 rows.
+template <typename E, int NB, bool VEC>
+__global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
+                                                           float2* __restrict__ part, int64_t pad) {
+    using F = Few<E>;
+    using Vec = typename F::Vec;
+    constexpr int kN = 16 / sizeof(E);
+    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ float2 s_part[kFewWaves][NB * 16];
+    Vec* sh = reinterpret_cast<Vec*>(lds);  // [operand][block of rows][lane]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
+    const int ops = (a.dim + F::kCols - 1) / F::kCols;
+    for (int j = threadIdx.x; j < ops * NB * 64; j += kFewWaves * 64) {
+        const int l = j & 63, b = (j >> 6) % NB, k = (j >> 6) / NB;
+        const int64_t row = 16 * b + (l & 15);
+        sh[j] = row < a.n ? load_few_cols<E, VEC>(static_cast<const E*>(a.h) + row * a.ld_h,
+                                                  F::kCols * k + kN * (l >> 4), a.dim)
+                          : Vec{};
+    }
+    __syncthreads();
+    const int groups = (ops + kFewGroup - 1) / kFewGroup;
+    const int64_t step = (int64_t)gridDim.x * kFewWaves;
+    int64_t tile = (int64_t)blockIdx.x * kFewWaves + wave;
+    const E* w = static_cast<const E*>(a.w);
+    auto fetch = [&](int64_t t, int g, Vec* v) {
+        int64_t row = t * 16 + (lane & 15);
+        row = row < a.classes ? row : a.classes - 1;
+#pragma unroll
+        for (int i = 0; i < kFewGroup; ++i)
+            if (g * kFewGroup + i < ops)
+                v[i] = load_few_cols<E, VEC>(w + row * a.ld_w,
+                                             F::kCols * (g * kFewGroup + i) + kN * quad, a.dim);
+    };
+    float top[NB], sum[NB];
+    f32x4v c[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        top[b] = -INFINITY;
+        sum[b] = 0.f;
+        c[b] = f32x4v{};
+    }
+    Vec now[kFewGroup], next[kFewGroup];
+    if (tile < tiles) fetch(tile, 0, now);
+    int g = 0;
+    while (tile < tiles) {
+        const bool last = g + 1 == groups;
+        const int64_t next_tile = last ? tile + step : tile;
+        if (next_tile < tiles) fetch(next_tile, last ? 0 : g + 1, next);
+        float term[4];
+        if (last) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t k = tile * 16 + 4 * quad + i;
+                term[i] = k >= a.classes ? -INFINITY : a.bias == nullptr ? 0.f : a.bias[k];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kFewGroup; ++i)
+            if (g * kFewGroup + i < ops) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    c[b] = F::mfma(now[i], sh[((g * kFewGroup + i) * NB + b) * 64 + lane], c[b]);
+            }
+        if (last) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float x[4], m = top[b];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // a class that is out counts for nothing, whatever its row holds
+                    x[i] = term[i] == -INFINITY ? -INFINITY : c[b][i] + term[i];
+                    m = fmaxf(m, x[i]);
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                sum[b] *= exp_below(top[b], ref);
+                top[b] = m;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sum[b] += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -ref * kLog2e));
+                c[b] = f32x4v{};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kFewGroup; ++i) now[i] = next[i];
+        tile = next_tile;
+        g = last ? 0 : g + 1;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int off = 16; off < 64; off <<= 1) {
+            const float t2 = __shfl_xor(top[b], off), s2 = __shfl_xor(sum[b], off);
+            const float m = fmaxf(top[b], t2);
+            sum[b] = sum[b] * exp_below(top[b], m) + s2 * exp_below(t2, m);
+            top[b] = m;
+        }
+        if (lane < 16) s_part[wave][16 * b + lane] = make_float2(top[b], sum[b]);
+    }
+    __syncthreads();
+    if (threadIdx.x < NB * 16) {
+        float2 r = s_part[0][threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < kFewWaves; ++k) {
+            const float2 q = s_part[k][threadIdx.x];
+            const float m = fmaxf(r.x, q.x);
+            r.y = r.y * exp_below(r.x, m) + q.y * exp_below(q.x, m);
+            r.x = m;
+        }
+        part[blockIdx.x * pad + threadIdx.x] = r;
+    }
+}
+
+// lse and loss of a row, LANES threads each: the splits are joined in an order that
+// the sizes fix, and the label's logit is formed from the rows themselves.
+template <typename E, int LANES>
 __global__ __launch_bounds__(kBlock) void k_sm_loss(SoftmaxArgs a, const float2* __restrict__ part,
                                                     int splits, int64_t pad) {
-    const int lane = threadIdx.x & 63;
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x % LANES;
+    const int64_t i = (int64_t)blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES;
     if (i >= a.n) return;
+    const int32_t y = a.labels[i];
+    const float c = a.weight == nullptr ? 1.f : a.weight[i];
     float m = -INFINITY, sum = 0.f;
-    bool nan = false;
-    for (int s = lane; s < splits; s += 64) {
+    for (int s = lane; s < splits; s += LANES) {
         const float2 p = part[(int64_t)s * pad + i];
         const float mm = fmaxf(m, p.x);
-        nan |= p.y != p.y;
         sum = sum * exp_below(m, mm) + p.y * exp_below(p.x, mm);
         m = mm;
     }
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
+    for (int off = 1; off < LANES; off <<= 1) {
         const float m2 = __shfl_xor(m, off), s2 = __shfl_xor(sum, off);
         const float mm = fmaxf(m, m2);
         sum = sum * exp_below(m, mm) + s2 * exp_below(m2, mm);
         m = mm;
     }
-    nan = __ballot(nan) != 0;
-    const float lse = nan ? NAN : m == -INFINITY ? -INFINITY : m + logf(sum);
-    const int32_t y = a.labels[i];
-    const float c = a.weight == nullptr ? 1.f : a.weight[i];
+    // a NaN among the logits is in the sum, though no maximum
+    const float lse = sum != sum ? sum : m == -INFINITY ? -INFINITY : m + logf(sum);
     float loss = 0.f;
     if (y < -1 || y >= a.classes) {
         loss = NAN;
@@ -588,12 +752,10 @@ __global__ __launch_bounds__(kBlock) void k_sm_loss(SoftmaxArgs a, const float2*
             const E* h = static_cast<const E*>(a.h) + i * a.ld_h;
             const E* w = static_cast<const E*>(a.w) + (int64_t)y * a.ld_w;
             float dot = 0.f;
-            for (int d = lane; d < a.dim; d += 64) {
-                if constexpr (sizeof(E) == 4) dot = fmaf(h[d], w[d], dot);
-                else dot = fmaf(__uint_as_float((uint32_t)h[d] << 16),
-                                __uint_as_float((uint32_t)w[d] << 16), dot);
-            }
-            const float below = lse - (group_sum<64>(dot) + b);
+#pragma unroll 4
+            for (int d = 4 * lane; d < a.dim; d += 4 * LANES)
+                dot += dot4(load_cols(h, d, a.dim, a.vec), load_cols(w, d, a.dim, a.vec));
+            const float below = lse - (group_sum<LANES>(dot) + b);
             loss = c * (below < 0.f ? 0.f : below);  // rounding alone takes it below 0
         }
     }
@@ -888,7 +1050,7 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
     Layout l{};
     const int64_t groups = div_up(x_tiles, xb);
     int64_t stage = staged ? kSmLds / 2 / resident / rec_bytes : waves;
-    if (stage > waves) stage = waves;
+    if (stage > 2 * waves) stage = 2 * waves;
     if (stage < 1) stage = 1;
     int g = waves;
     while (g > 1 && g / 2 >= groups && waves / (g / 2) <= stage) g /= 2;
@@ -914,12 +1076,9 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
     l.per = div_up(y_tiles, want);
     l.splits = div_up(y_tiles, l.per);
     l.slots = l.splits * yw;
-    // a stage of about 32 KB, whole rounds of the waves along Y
-    int64_t st = 32 * 1024 / rec_bytes;
-    if (st < yw) st = yw;
-    st = st / yw * yw;
-    if (st > stage) st = stage / yw * yw;
-    l.stage = (int32_t)(st < 1 ? 1 : st);
+    // as much of LDS as there is, in whole rounds of the waves along Y: a barrier
+    // brings the waves into step, and their products then wait for each other
+    l.stage = (int32_t)(stage / yw * yw);
     return l;
 }
 
@@ -997,12 +1156,47 @@ hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t 
     return hipGetLastError();
 }
 
+// The loss of few rows: up to 64 whose operands fit kFewLds.  Above that the tables'
+// packing is paid for by the faster products.
+int few_blocks(const SoftmaxArgs& a) {
+    const int64_t cols = a.dtype == kDtypeBf16 ? Few<bf16_t>::kCols : Few<float>::kCols;
+    for (int nb = 1; nb <= 4; nb <<= 1)
+        if (a.n <= 16 * nb) return div_up(a.dim, cols) * nb * 1024 <= kFewLds ? nb : 0;
+    return 0;
+}
+
+template <typename E, int NB>
+hipError_t few_pass(const SoftmaxArgs& a, float2* part, int64_t* slots, hipStream_t s) {
+    const int64_t tiles = div_up(a.classes, 16);
+    const int64_t most = 2048, blocks = div_up(tiles, kFewWaves) < most ? div_up(tiles, kFewWaves) : most;
+    const int lds = (int)div_up(a.dim, Few<E>::kCols) * NB * 1024;
+    const bool vec = a.vec16;
+    const dim3 grid((uint32_t)blocks);
+    if (vec) k_sm_few<E, NB, true><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+    else k_sm_few<E, NB, false><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+    *slots = blocks;
+    return hipGetLastError();
+}
+
 template <typename E>
-hipError_t softmax_loss(const SoftmaxArgs& a, hipStream_t s) {
+hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
     const SoftmaxPlan p = softmax_plan(a.classes, a.n, a.dim, a.dtype, false);
     float2* part = reinterpret_cast<float2*>(a.ws + p.part);
-    int64_t slots = 0;
-    for (int64_t c0 = 0; c0 < a.classes; c0 += p.piece) {
+    a.vec = fours(a.h, a.ld_h, sizeof(E)) && fours(a.w, a.ld_w, sizeof(E));
+    constexpr int kN = 16 / sizeof(E);
+    auto sixteen = [](const void* m, int64_t ld) {
+        return (reinterpret_cast<uintptr_t>(m) & 15) == 0 && ld % kN == 0;
+    };
+    a.vec16 = a.dim % kN == 0 && sixteen(a.h, a.ld_h) && sixteen(a.w, a.ld_w);
+    int64_t slots = 0, pad = p.rows_pad;
+    const int few = few_blocks(a);
+    if (few != 0) {
+        pad = 16 * few;
+        SM_TRY((few == 1   ? few_pass<E, 1>(a, part, &slots, s)
+                : few == 2 ? few_pass<E, 2>(a, part, &slots, s)
+                           : few_pass<E, 4>(a, part, &slots, s)));
+    }
+    for (int64_t c0 = 0; few == 0 && c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
         SM_TRY(pack<E>(p, a, c0, count, 1, s));
         PassArgs l{};
@@ -1011,7 +1205,10 @@ hipError_t softmax_loss(const SoftmaxArgs& a, hipStream_t s) {
         l.first = c0 == 0, l.lse_part = part;
         SM_TRY((pass<E, false, true>(p, l, [&](PassArgs&, const Layout& o) { slots = o.slots; }, s)));
     }
-    k_sm_loss<E><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, p.rows_pad);
+    if (a.n < 4096)
+        k_sm_loss<E, 64><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, pad);
+    else
+        k_sm_loss<E, 16><<<dim3((uint32_t)div_up(a.n, 16)), kBlock, 0, s>>>(a, part, (int)slots, pad);
     SM_TRY(hipGetLastError());
     if (a.loss_sum != nullptr) {
         k_sm_sum<<<1, 1024, 0, s>>>(a.loss, a.n, a.loss_sum);

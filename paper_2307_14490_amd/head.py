@@ -10,7 +10,6 @@ Errors that only the device can see are kept in a status word until ``check``.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 from .binding import (HUGE_DTYPE_BF16, HUGE_DTYPE_F32, HUGE_ERR_INVALID_ARG, HUGE_STATE_F32,
@@ -60,21 +59,41 @@ def _vector(t, n, dtype, what, device):
     return p
 
 
-@contextlib.contextmanager
-def _on(device, stream, *tensors):
-    """The device made current, and the stream to launch on as a pointer.  With a
-    stream of the caller's, what is allocated inside belongs to it, and `tensors`
-    are not given to others before its work on them is done."""
+def _current(device):
+    """torch's current stream on a device, as a pointer."""
     import torch
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream().cuda_stream
-        else:
-            with torch.cuda.stream(stream):
-                yield stream.cuda_stream
-            for t in tensors:
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+class _on:
+    """``with _on(device, stream, tensors) as pointer``: the device is current, and
+    the pointer is the stream to launch on.  With a stream of the caller's, what is
+    allocated inside belongs to it, and `tensors` are not given to others before its
+    work on them is done."""
+
+    __slots__ = ("stream", "tensors", "guards", "device")
+
+    def __init__(self, device, stream, tensors):
+        self.device, self.stream, self.tensors = device, stream, tensors
+
+    def __enter__(self):
+        import torch
+        self.guards = []
+        if torch.cuda.current_device() != self.device.index:
+            self.guards.append(torch.cuda.device(self.device))
+        if self.stream is not None:
+            self.guards.append(torch.cuda.stream(self.stream))
+        for g in self.guards:
+            g.__enter__()
+        return _current(self.device) if self.stream is None else self.stream.cuda_stream
+
+    def __exit__(self, *error):
+        for g in reversed(self.guards):
+            g.__exit__(*error)
+        if self.stream is not None:
+            for t in self.tensors:
                 if t is not None:
-                    t.record_stream(stream)
+                    t.record_stream(self.stream)
 
 
 class _Status:
@@ -87,14 +106,17 @@ class _Status:
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._status_ptr = self.status.data_ptr()
         self._last = torch.cuda.current_stream(self.device)
+        self._last_ptr = self._last.cuda_stream
 
     def _ordered(self, stream):
         import torch
-        now = torch.cuda.current_stream(self.device) if stream is None else stream
-        if now != self._last:
-            now.wait_stream(self._last)
-            self._last = now
+        now = _current(self.device) if stream is None else stream.cuda_stream
+        if now != self._last_ptr:
+            stream = torch.cuda.current_stream(self.device) if stream is None else stream
+            stream.wait_stream(self._last)
+            self._last, self._last_ptr = stream, now
 
     def check(self):
         """Raise HugeError if a call since the last check met a device-side error
@@ -119,10 +141,9 @@ def layer_norm(x, gamma, beta, eps=1e-5, stream=None):
     pb = _vector(beta, dim, "float32", "layer_norm beta", x.device)
     if pg is None or pb is None:
         raise TypeError("layer_norm: gamma and beta are required")
-    with _on(x.device, stream, x, gamma, beta) as st:
+    with _on(x.device, stream, (x, gamma, beta,)) as st:
         y = torch.empty((n, dim), dtype=x.dtype, device=x.device)
-        stat = torch.empty((2, n), dtype=torch.float32, device=x.device)
-        mean, rstd = stat[0], stat[1]
+        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind()
         _ok(load().huge_layer_norm(px, ld, n, dim, code, pg, pb, float(eps), y.data_ptr(), dim,
                                    mean.data_ptr(), rstd.data_ptr(), st), "huge_layer_norm")
     return y, mean, rstd
@@ -143,7 +164,7 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, want_dx=True, want_weights=Tru
     if pg is None or pm is None or pr is None:
         raise TypeError("layer_norm_backward: gamma, mean and rstd are required")
     L = load()
-    with _on(x.device, stream, dy, x, gamma, mean, rstd) as st:
+    with _on(x.device, stream, (dy, x, gamma, mean, rstd,)) as st:
         dx = torch.empty((n, dim), dtype=x.dtype, device=x.device) if want_dx else None
         dw = ws = None
         bytes_ = 0
@@ -201,11 +222,10 @@ class SoftmaxLoss(_Status):
         a = self._inputs("SoftmaxLoss.loss", h, w, labels, bias, weights)
         pt = _vector(total, 1, "float64", "SoftmaxLoss.loss total", h.device)
         self._ordered(stream)
-        with _on(self.device, stream, h, w, labels, bias, weights, total) as st:
-            out = torch.empty((2, a[3]), dtype=torch.float32, device=self.device)
-            loss, lse = out[0], out[1]
+        with _on(self.device, stream, (h, w, labels, bias, weights, total,)) as st:
+            loss, lse = torch.empty((2, a[3]), dtype=torch.float32, device=self.device).unbind()
             _ok(load().huge_softmax_loss(*a, loss.data_ptr(), lse.data_ptr(), pt,
-                                         self.status.data_ptr(), self._ws_ptr, self.ws_bytes, st),
+                                         self._status_ptr, self._ws_ptr, self.ws_bytes, st),
                 "huge_softmax_loss")
         return loss, lse
 
@@ -220,13 +240,13 @@ class SoftmaxLoss(_Status):
             raise TypeError("SoftmaxLoss.grad: lse is required")
         c = self.cfg
         self._ordered(stream)
-        with _on(self.device, stream, h, w, labels, lse, bias, weights) as st:
+        with _on(self.device, stream, (h, w, labels, lse, bias, weights,)) as st:
             new = lambda *shape, t=h.dtype: torch.empty(shape, dtype=t, device=self.device)  # noqa: E731
             dh = new(a[3], c.dim) if want_h else None
             dw = new(c.num_classes, c.dim) if want_w else None
             db = new(c.num_classes, t=torch.float32) if want_bias else None
             _ok(load().huge_softmax_grad(*a, pl, float(scale), _dptr(dh), _dptr(dw), _dptr(db),
-                                         self.status.data_ptr(), self._ws_ptr, self.ws_bytes, st),
+                                         self._status_ptr, self._ws_ptr, self.ws_bytes, st),
                 "huge_softmax_grad")
         return dh, dw, db
 
@@ -271,6 +291,15 @@ class AdamW(_Status):
             t.d_param, t.n = p.data_ptr(), p.numel()
             t.d_state = self.states.data_ptr() + self._skip + self._state_at[k]
             t.param_dtype = _dtype_code(p, f"AdamW params[{k}]")
+        if self.kind == HUGE_STATE_F32:  # m, then v, each in whole blocks of 256
+            half = [L.huge_adamw_state_bytes(p.numel(), self.kind) // 2 for p in self.params]
+            self._views = [[self._view(self._state_at[k] + which * half[k], p)
+                            for k, p in enumerate(self.params)] for which in (0, 1)]
+
+    def _view(self, at, p):
+        import torch
+        at += self._skip
+        return self.states[at:at + 4 * p.numel()].view(torch.float32).view(p.shape)
 
     def _list(self, ts, dtypes, what):
         ts = list(ts)
@@ -294,20 +323,22 @@ class AdamW(_Status):
             t.d_grad = g.data_ptr()
             t.grad_dtype = _dtype_code(g, "AdamW.step grads")
         self._ordered(stream)
-        with _on(self.device, stream, self.states, *self.params, *grads) as st:
+        with _on(self.device, stream, (self.states, *self.params, *grads,)) as st:
             _ok(load().huge_adamw_step(ctypes.byref(c), self._tensors, len(grads),
-                                       self.status.data_ptr(), st), "huge_adamw_step")
+                                       self._status_ptr, st), "huge_adamw_step")
         self.steps += 1
 
     def _pointers(self, ts):
         return (ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
 
     def values(self, stream=None):
-        """(m, v): lists of float32 tensors shaped like the parameters, copies of
-        the moments."""
+        """(m, v): lists of float32 tensors shaped like the parameters.  States "f32":
+        the moments themselves, as views of the states; "q8": what they stand for."""
         import torch
+        if self.kind == HUGE_STATE_F32:
+            return [list(ts) for ts in self._views]
         self._ordered(stream)
-        with _on(self.device, stream, self.states) as st:
+        with _on(self.device, stream, (self.states,)) as st:
             m, v = ([torch.empty(p.shape, dtype=torch.float32, device=self.device)
                      for p in self.params] for _ in range(2))
             _ok(load().huge_adamw_get_state(self._tensors, len(m), self.kind, self._pointers(m),
@@ -321,7 +352,7 @@ class AdamW(_Status):
         if int(steps) < 0:
             raise ValueError(f"AdamW.load: {steps} steps")
         self._ordered(stream)
-        with _on(self.device, stream, self.states, *m, *v) as st:
+        with _on(self.device, stream, (self.states, *m, *v,)) as st:
             _ok(load().huge_adamw_set_state(self._tensors, len(m), self.kind, self._pointers(m),
                                             self._pointers(v), st), "huge_adamw_set_state")
         self.steps = int(steps)
