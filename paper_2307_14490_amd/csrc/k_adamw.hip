@@ -24,43 +24,73 @@ namespace {
 constexpr float kInv127 = 1.0f / 127.0f;
 constexpr float kInv255 = 1.0f / 255.0f;
 
-template <typename E>
-__device__ __forceinline__ void load4(const E* __restrict__ p, int64_t i, int64_t n, bool vec,
-                                      float* v) {
-    if (vec && i + 4 <= n) {
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Four elements at i.  FULL: all there, at an address aligned for all four.
+template <bool FULL, typename E>
+__device__ __forceinline__ void load4(const E* __restrict__ p, int64_t i, int64_t n, float* v) {
+    if constexpr (FULL) {
         const float4 q = load_chunk(p + i, 0);
         v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[e] = 0.f;
-        if (i + e < n) {
-            if constexpr (sizeof(E) == 4) v[e] = p[i + e];
-            else v[e] = __uint_as_float((uint32_t)p[i + e] << 16);
+        for (int e = 0; e < 4; ++e) {
+            v[e] = 0.f;
+            if (i + e < n) {
+                if constexpr (sizeof(E) == 4) v[e] = p[i + e];
+                else v[e] = __uint_as_float((uint32_t)p[i + e] << 16);
+            }
         }
     }
 }
 
-template <typename E>
-__device__ __forceinline__ void store4(E* __restrict__ p, int64_t i, int64_t n, bool vec,
-                                       const float* v) {
-    if (vec && i + 4 <= n) {
+template <bool FULL, typename E>
+__device__ __forceinline__ void store4(E* __restrict__ p, int64_t i, int64_t n, const float* v) {
+    if constexpr (FULL && sizeof(E) == 4) {
         store_chunk(p + i, 0, make_float4(v[0], v[1], v[2], v[3]));
-        return;
-    }
+    } else if constexpr (FULL) {
+        *reinterpret_cast<bf16x4*>(p + i) =
+            __builtin_convertvector((f32x4{v[0], v[1], v[2], v[3]}), bf16x4);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (i + e < n) {
-            if constexpr (sizeof(E) == 4) p[i + e] = v[e];
-            else p[i + e] = (bf16_t)float_to_bf16_bits(v[e]);
-        }
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) {
+                if constexpr (sizeof(E) == 4) p[i + e] = v[e];
+                else p[i + e] = (bf16_t)float_to_bf16_bits(v[e]);
+            }
+    }
 }
 
+// Maximum over the wave of values >= 0, without LDS (as xor_add).
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF,
+                                                               0xF, false)));
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    return v;
+    v = dpp_max<0xB1>(v);
+    v = dpp_max<0x4E>(v);
+    v = dpp_max<0x141>(v);
+    v = dpp_max<0x140>(v);
+    const int a = __float_as_int(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    v = fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+    const int b = __float_as_int(v);
+    const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return fmaxf(__int_as_float(q[0]), __int_as_float(q[1]));
+}
+
+// sqrt, correctly rounded, of x in 2^-60 .. 2^60: a Goldschmidt iteration from the
+// hardware's reciprocal root, then Markstein's correction by the exact residual.
+// Half the instructions of sqrtf, which also serves subnormal numbers.
+__device__ __forceinline__ float sqrt_mid(float x) {
+    const float y = __builtin_amdgcn_rsqf(x);
+    float s = x * y, h = 0.5f * y;
+    const float e = __builtin_fmaf(-h, s, 0.5f);
+    s = __builtin_fmaf(s, e, s);
+    h = __builtin_fmaf(h, e, h);
+    return __builtin_fmaf(__builtin_fmaf(-s, s, x), h, s);
 }
 
 // The moments of four elements at i (a multiple of 4) of a tensor of n.  `b`: the
@@ -70,31 +100,31 @@ struct Moments;
 
 template <>
 struct Moments<false> {
-    static __device__ __forceinline__ void load(const uint8_t* state, int64_t n, int64_t i,
+    // the two arrays are padded to whole blocks: always four at a time
+    static __device__ __forceinline__ void load(const uint8_t* state, int64_t padded, int64_t i,
                                                 float* m, float* v) {
-        // padded to whole blocks: always four at a time
         const float* sm = reinterpret_cast<const float*>(state);
-        load4(sm, i, i + 4, true, m);
-        load4(sm + adam_padded(n), i, i + 4, true, v);
+        load4<true>(sm, i, 0, m);
+        load4<true>(sm + padded, i, 0, v);
     }
-    static __device__ __forceinline__ void store(uint8_t* state, int64_t n, int64_t i,
+    static __device__ __forceinline__ void store(uint8_t* state, int64_t padded, int64_t i,
                                                  const float* m, const float* v, const float*) {
         float* sm = reinterpret_cast<float*>(state);
-        store4(sm, i, i + 4, true, m);
-        store4(sm + adam_padded(n), i, i + 4, true, v);
+        store4<true>(sm, i, 0, m);
+        store4<true>(sm + padded, i, 0, v);
     }
 };
 
 template <>
 struct Moments<true> {
-    static __device__ __forceinline__ float2* scales(uint8_t* state, int64_t n, int64_t i) {
-        return reinterpret_cast<float2*>(state + 2 * adam_padded(n)) + i / kAdamBlock;
+    static __device__ __forceinline__ float2* scales(uint8_t* state, int64_t padded, int64_t i) {
+        return reinterpret_cast<float2*>(state + 2 * padded) + i / kAdamBlock;
     }
-    static __device__ __forceinline__ void load(const uint8_t* state, int64_t n, int64_t i,
+    static __device__ __forceinline__ void load(const uint8_t* state, int64_t padded, int64_t i,
                                                 float* m, float* v) {
         const uint32_t q = *reinterpret_cast<const uint32_t*>(state + i);
-        const uint32_t u = *reinterpret_cast<const uint32_t*>(state + adam_padded(n) + i);
-        const float2 s = *scales(const_cast<uint8_t*>(state), n, i);
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(state + padded + i);
+        const float2 s = *scales(const_cast<uint8_t*>(state), padded, i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float k = (float)(int8_t)(q >> (8 * e));
@@ -107,7 +137,7 @@ struct Moments<true> {
     }
     // r: sqrt(v), 0 past the end of the tensor (as m is).  Every lane of the wave
     // takes part: its 256 elements are one block.
-    static __device__ __forceinline__ void store(uint8_t* state, int64_t n, int64_t i,
+    static __device__ __forceinline__ void store(uint8_t* state, int64_t padded, int64_t i,
                                                  const float* m, const float*, const float* r) {
         float s = fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])));
         float t = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
@@ -119,17 +149,17 @@ struct Moments<true> {
         uint32_t q = 0, u = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float a = fminf(rintf(sqrtf(fabsf(m[e]) * is) * 127.0f), 127.0f);
-            float c = fminf(rintf(sqrtf(r[e] * it) * 255.0f), 255.0f);
-            if (r[e] > 0.f) c = fmaxf(c, 1.0f);
-            const int k = m[e] < 0.f ? -(int)a : (int)a;
-            q |= (uint32_t)(k & 0xFF) << (8 * e);
-            u |= (uint32_t)c << (8 * e);
+            // below 2^-60 a root is far below half a code
+            const float a = sqrt_mid(fmaxf(fabsf(m[e]) * is, 0x1p-60f));
+            const float c = sqrt_mid(fmaxf(r[e] * it, 0x1p-60f));
+            const float qa = copysignf(fminf(rintf(a * 127.0f), 127.0f), m[e]);
+            const float ua = fmaxf(fminf(rintf(c * 255.0f), 255.0f), r[e] > 0.f ? 1.0f : 0.0f);
+            q |= ((uint32_t)(int)qa & 0xFFu) << (8 * e);
+            u |= (uint32_t)ua << (8 * e);
         }
-        if (i >= adam_padded(n)) return;
         *reinterpret_cast<uint32_t*>(state + i) = q;
-        *reinterpret_cast<uint32_t*>(state + adam_padded(n) + i) = u;
-        if ((threadIdx.x & 63) == 0) *scales(state, n, i) = make_float2(s, t);
+        *reinterpret_cast<uint32_t*>(state + padded + i) = u;
+        if ((threadIdx.x & 63) == 0) *scales(state, padded, i) = make_float2(s, t);
     }
 };
 
@@ -142,23 +172,21 @@ __device__ __forceinline__ int find_tensor(const AdamArgs& a) {
     return k;
 }
 
-template <typename P, typename G, bool Q8>
-__global__ __launch_bounds__(kBlock) void k_adamw(AdamArgs a) {
-    const AdamTensor& T = a.t[find_tensor(a)];
+// One chunk, 1024 elements at a time.  FULL: all of it inside the tensor and aligned.
+template <typename P, typename G, bool Q8, bool FULL>
+__device__ __forceinline__ bool update_chunk(const AdamArgs& a, const AdamTensor& T, int64_t at) {
     P* p = static_cast<P*>(T.p);
     const G* g = static_cast<const G*>(T.g);
     const int64_t n = T.n, padded = adam_padded(n);
-    const bool vec = T.vec != 0;
-    const int64_t at = (int64_t)(blockIdx.x - T.first) * kAdamChunk + threadIdx.x * 4;
     bool bad = false;
 #pragma unroll
     for (int k = 0; k < kAdamChunk; k += kBlock * 4) {
         const int64_t i = at + k;
-        if (i >= padded) break;  // whole waves: 256 elements each
+        if (!FULL && i >= padded) break;  // whole waves: 256 elements each
         float x[4], d[4], m[4], v[4], r[4];
-        load4(p, i, n, vec, x);
-        load4(g, i, n, vec, d);
-        Moments<Q8>::load(T.state, n, i, m, v);
+        load4<FULL>(p, i, n, x);
+        load4<FULL>(g, i, n, d);
+        Moments<Q8>::load(T.state, padded, i, m, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float ge = d[e] * a.grad_scale;
@@ -166,47 +194,62 @@ __global__ __launch_bounds__(kBlock) void k_adamw(AdamArgs a) {
             const float vn = v[e] * a.beta2 + (ge * ge) * a.one_beta2;
             // |.| < inf is false for NaN too
             const bool ok = fabsf(mn) < INFINITY && vn < INFINITY;
-            r[e] = sqrtf(ok ? vn : v[e]);
+            v[e] = ok ? vn : v[e];
+            r[e] = sqrtf(v[e]);
             const float step = (mn * a.rate) / (r[e] * a.fix + a.eps);
-            if (ok) {
-                x[e] = x[e] * a.keep - step;
-                m[e] = mn;
-                v[e] = vn;
-            } else if (i + e < n) {
-                bad = true;
-            }
+            x[e] = ok ? x[e] * a.keep - step : x[e];
+            m[e] = ok ? mn : m[e];
+            bad |= !ok && (FULL || i + e < n);
         }
-        store4(p, i, n, vec, x);
-        Moments<Q8>::store(T.state, n, i, m, v, r);
+        store4<FULL>(p, i, n, x);
+        Moments<Q8>::store(T.state, padded, i, m, v, r);
     }
+    return bad;
+}
+
+template <typename P, typename G, bool Q8>
+__global__ __launch_bounds__(kBlock) void k_adamw(AdamArgs a) {
+    const AdamTensor& T = a.t[find_tensor(a)];
+    const int64_t first = (int64_t)(blockIdx.x - T.first) * kAdamChunk;
+    const int64_t at = first + threadIdx.x * 4;
+    const bool full = T.vec != 0 && first + kAdamChunk <= T.n;
+    const bool bad = full ? update_chunk<P, G, Q8, true>(a, T, at)
+                          : update_chunk<P, G, Q8, false>(a, T, at);
     if (bad) atomicCAS(a.status, 0, -6);
+}
+
+template <bool Q8, bool WRITE, bool FULL>
+__device__ __forceinline__ void state_chunk(const AdamTensor& T, int64_t at) {
+    float* pm = static_cast<float*>(T.p);
+    float* pv = static_cast<float*>(const_cast<void*>(T.g));
+    const int64_t n = T.n, padded = adam_padded(n);
+#pragma unroll
+    for (int k = 0; k < kAdamChunk; k += kBlock * 4) {
+        const int64_t i = at + k;
+        if (!FULL && i >= padded) break;
+        float m[4], v[4], r[4];
+        if constexpr (WRITE) {
+            load4<FULL>(pm, i, n, m);
+            load4<FULL>(pv, i, n, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = sqrtf(v[e]);
+            Moments<Q8>::store(T.state, padded, i, m, v, r);
+        } else {
+            Moments<Q8>::load(T.state, padded, i, m, v);
+            store4<FULL>(pm, i, n, m);
+            store4<FULL>(pv, i, n, v);
+        }
+    }
 }
 
 template <bool Q8, bool WRITE>
 __global__ __launch_bounds__(kBlock) void k_adamw_state(AdamArgs a) {
     const AdamTensor& T = a.t[find_tensor(a)];
-    float* pm = static_cast<float*>(T.p);
-    float* pv = static_cast<float*>(const_cast<void*>(T.g));
-    const int64_t n = T.n, padded = adam_padded(n);
-    const bool vec = T.vec != 0;
-    const int64_t at = (int64_t)(blockIdx.x - T.first) * kAdamChunk + threadIdx.x * 4;
-#pragma unroll
-    for (int k = 0; k < kAdamChunk; k += kBlock * 4) {
-        const int64_t i = at + k;
-        if (i >= padded) break;
-        float m[4], v[4], r[4];
-        if constexpr (WRITE) {
-            load4(pm, i, n, vec, m);
-            load4(pv, i, n, vec, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = sqrtf(v[e]);
-            Moments<Q8>::store(T.state, n, i, m, v, r);
-        } else {
-            Moments<Q8>::load(T.state, n, i, m, v);
-            store4(pm, i, n, vec, m);
-            store4(pv, i, n, vec, v);
-        }
-    }
+    const int64_t first = (int64_t)(blockIdx.x - T.first) * kAdamChunk;
+    if (T.vec != 0 && first + kAdamChunk <= T.n)
+        state_chunk<Q8, WRITE, true>(T, first + threadIdx.x * 4);
+    else
+        state_chunk<Q8, WRITE, false>(T, first + threadIdx.x * 4);
 }
 
 }  // namespace

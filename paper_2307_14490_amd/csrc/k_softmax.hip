@@ -323,7 +323,7 @@ struct PassArgs {
     int64_t x_rows;
     int32_t dp, dim;
     float scale;
-    bool want_bias;
+    bool want_bias, out_vec;
 };
 
 // The workgroup's place.  Workgroups go to the eight XCDs in turn; each XCD takes a
@@ -782,14 +782,29 @@ __global__ __launch_bounds__(1024) void k_sm_sum(const float* __restrict__ loss,
 // ---------------------------------------------------------------------------
 // Gradients
 // ---------------------------------------------------------------------------
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+
+// Four elements of a result; vec: the array is aligned for four (its element type is
+// all that the caller owes).
 template <typename E>
-__device__ __forceinline__ void store_out(E* p, float4 v, float scale) {
-    // alignment of the element type is all that the caller owes
-    const float q[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
+__device__ __forceinline__ void store_out(E* p, float4 v, float scale, bool vec) {
+    const f32x4 q = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
+    if constexpr (sizeof(E) == 4) {
+        if (vec) {
+            *reinterpret_cast<f32x4*>(p) = q;
+        } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(E) == 4) p[e] = q[e];
-        else p[e] = (bf16_t)float_to_bf16_bits(q[e]);
+            for (int e = 0; e < 4; ++e) p[e] = q[e];
+        }
+    } else {
+        const u16x4 u = __builtin_bit_cast(u16x4, __builtin_convertvector(q, bf16x4));
+        if (vec) {
+            *reinterpret_cast<u16x4*>(p) = u;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = u[e];
+        }
     }
 }
 
@@ -972,7 +987,7 @@ void k_sm_grad(PassArgs a) {
                     float4* p = reinterpret_cast<float4*>(a.part + row * a.dp + col);
                     *p = a.first ? v : add4(*p, v);
                 } else if (a.out != nullptr && xi < a.x_rows && col < a.dim) {
-                    store_out(static_cast<E*>(a.out) + xi * a.dim + col, v, a.scale);
+                    store_out(static_cast<E*>(a.out) + xi * a.dim + col, v, a.scale, a.out_vec);
                 }
             }
         if (!ROWS && blockIdx.y == 0 && a.want_bias) {
@@ -991,6 +1006,7 @@ template <typename E, int LANES>
 __global__ __launch_bounds__(kBlock) void k_sm_join(const float* __restrict__ part, int splits,
                                                     int64_t rows_pad, int dp, int64_t rows,
                                                     int dim, float scale, E* __restrict__ out,
+                                                    bool out_vec,
                                                     const float* __restrict__ bias_part,
                                                     float* __restrict__ bias_out) {
     const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / LANES;
@@ -1005,7 +1021,7 @@ __global__ __launch_bounds__(kBlock) void k_sm_join(const float* __restrict__ pa
             v = add4(v, *reinterpret_cast<const float4*>(part + (s * rows_pad + row) * dp + col));
         v = make_float4(group_sum<LANES>(v.x), group_sum<LANES>(v.y), group_sum<LANES>(v.z),
                         group_sum<LANES>(v.w));
-        if (lane == 0) store_out(out + row * dim + col, v, scale);
+        if (lane == 0) store_out(out + row * dim + col, v, scale, out_vec);
     }
     if (bias_out != nullptr && i < rows) {
         float v = 0.f;
@@ -1223,13 +1239,14 @@ hipError_t join(const SoftmaxPlan& p, const float* part, int64_t slots, int64_t 
                 hipStream_t s) {
     const int64_t work = out != nullptr ? rows * (p.dim / 4) : rows;
     E* o = static_cast<E*>(out);
+    const bool vec = fours(out, 0, sizeof(E));
     // few outputs of many splits: 16 threads each
     if (work < (1 << 18) && slots >= 16)
         k_sm_join<E, 16><<<dim3((uint32_t)div_up(work * 16, kBlock)), kBlock, 0, s>>>(
-            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, bias_part, bias_out);
+            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, vec, bias_part, bias_out);
     else
         k_sm_join<E, 1><<<dim3((uint32_t)div_up(work, kBlock)), kBlock, 0, s>>>(
-            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, bias_part, bias_out);
+            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, vec, bias_part, bias_out);
     return hipGetLastError();
 }
 
@@ -1252,6 +1269,7 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
             float* bias_out = a.dbias == nullptr ? nullptr : a.dbias + c0;
             g.x = a.ws + p.w, g.y = a.ws + p.h, g.x_tiles = w_tiles, g.y_tiles = x_tiles;
             g.x_rows = count, g.first = true, g.out = out, g.bias_out = bias_out;
+            g.out_vec = fours(out, 0, sizeof(E));
             g.want_bias = bias_out != nullptr;
             int64_t slots = 0;
             float* bias_part = nullptr;
@@ -1269,6 +1287,7 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
         if (a.dh != nullptr) {
             g.x = a.ws + p.h, g.y = a.ws + p.w, g.x_tiles = x_tiles, g.y_tiles = w_tiles;
             g.x_rows = a.n, g.first = c0 == 0, g.out = a.dh, g.bias_out = nullptr;
+            g.out_vec = fours(a.dh, 0, sizeof(E));
             g.want_bias = false;
             SM_TRY((pass<E, true, true>(p, g, [&](PassArgs& q, const Layout& o) {
                 row_slots = o.slots;
