@@ -566,7 +566,7 @@ typedef struct huge_adamw_tensor {
 } huge_adamw_tensor;
 
 typedef struct huge_adamw_config {
-    double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps > 0 */
+    double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps >= 1e-30 */
     int64_t step;        /* 1 for the first step                                   */
     int32_t state_kind;  /* HUGE_STATE_F32 or HUGE_STATE_Q8                        */
 } huge_adamw_config;

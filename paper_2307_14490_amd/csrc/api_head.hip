@@ -221,7 +221,7 @@ huge_status huge_adamw_step(const huge_adamw_config* cfg, const huge_adamw_tenso
         !state_ok(cfg->state_kind) || cfg->step < 1 || !rate_ok(cfg->lr) ||
         !rate_ok(cfg->weight_decay) || !isfinite(cfg->grad_scale) ||
         !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) ||
-        !((float)cfg->eps > 0.f && isfinite((float)cfg->eps)))
+        !(cfg->eps >= 1e-30 && isfinite((float)cfg->eps)))
         return HUGE_ERR_INVALID_ARG;
     for (int32_t k = 0; k < count; ++k) {
         const huge_adamw_tensor& t = h_tensors[k];

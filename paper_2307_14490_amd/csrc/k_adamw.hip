@@ -81,16 +81,25 @@ __device__ __forceinline__ float wave_max(float v) {
     return fmaxf(__int_as_float(q[0]), __int_as_float(q[1]));
 }
 
-// sqrt, correctly rounded, of x in 2^-60 .. 2^60: a Goldschmidt iteration from the
-// hardware's reciprocal root, then Markstein's correction by the exact residual.
-// Half the instructions of sqrtf, which also serves subnormal numbers.
-__device__ __forceinline__ float sqrt_mid(float x) {
-    const float y = __builtin_amdgcn_rsqf(x);
-    float s = x * y, h = 0.5f * y;
-    const float e = __builtin_fmaf(-h, s, 0.5f);
-    s = __builtin_fmaf(s, e, s);
-    h = __builtin_fmaf(h, e, h);
-    return __builtin_fmaf(__builtin_fmaf(-s, s, x), h, s);
+// Roots and quotients to the nearest float by Markstein's method: the hardware's
+// reciprocal (root), then a correction by the residual, which an fma gives without
+// error.  A third of the instructions of sqrtf and of the division, which also
+// serve subnormal numbers and infinities.
+constexpr float kTiny = 0x1p-100f;  // above it, residuals are normal numbers
+
+// sqrt(x) for x = 0 and x >= kTiny (what is between gives less than 2^-49).
+__device__ __forceinline__ float root(float x) {
+    const float y = __builtin_amdgcn_rsqf(fmaxf(x, kTiny));
+    const float s = x * y;
+    return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+}
+
+// a / b for b >= 1e-30 and a quotient below 2^127.
+__device__ __forceinline__ float quotient(float a, float b) {
+    float y = __builtin_amdgcn_rcpf(b);
+    y = __builtin_fmaf(__builtin_fmaf(-b, y, 1.0f), y, y);
+    const float q = a * y;
+    return __builtin_fmaf(__builtin_fmaf(-b, q, a), y, q);
 }
 
 // The moments of four elements at i (a multiple of 4) of a tensor of n.  `b`: the
@@ -127,9 +136,9 @@ struct Moments<true> {
         const float2 s = *scales(const_cast<uint8_t*>(state), padded, i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float k = (float)(int8_t)(q >> (8 * e));
-            const float a = fabsf(k) * kInv127;
-            m[e] = copysignf(s.x * (a * a), k);
+            // codes of m are stored as q + 128
+            const float k = ((float)((q >> (8 * e)) & 0xFFu) - 128.0f) * kInv127;
+            m[e] = s.x * (k * fabsf(k));
             const float c = (float)((u >> (8 * e)) & 0xFFu) * kInv255;
             const float r = s.y * (c * c);
             v[e] = r * r;
@@ -149,13 +158,10 @@ struct Moments<true> {
         uint32_t q = 0, u = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            // below 2^-60 a root is far below half a code
-            const float a = sqrt_mid(fmaxf(fabsf(m[e]) * is, 0x1p-60f));
-            const float c = sqrt_mid(fmaxf(r[e] * it, 0x1p-60f));
-            const float qa = copysignf(fminf(rintf(a * 127.0f), 127.0f), m[e]);
-            const float ua = fmaxf(fminf(rintf(c * 255.0f), 255.0f), r[e] > 0.f ? 1.0f : 0.0f);
-            q |= ((uint32_t)(int)qa & 0xFFu) << (8 * e);
-            u |= (uint32_t)ua << (8 * e);
+            const float a = rintf(root(fabsf(m[e]) * is) * 127.0f);
+            const float c = rintf(root(r[e] * it) * 255.0f);
+            q = __builtin_amdgcn_cvt_pk_u8_f32(copysignf(a, m[e]) + 128.0f, e, q);
+            u = __builtin_amdgcn_cvt_pk_u8_f32(fmaxf(c, r[e] > 0.f ? 1.0f : 0.0f), e, u);
         }
         *reinterpret_cast<uint32_t*>(state + i) = q;
         *reinterpret_cast<uint32_t*>(state + padded + i) = u;
@@ -187,19 +193,39 @@ __device__ __forceinline__ bool update_chunk(const AdamArgs& a, const AdamTensor
         load4<FULL>(p, i, n, x);
         load4<FULL>(g, i, n, d);
         Moments<Q8>::load(T.state, padded, i, m, v);
+        float mn[4], vn[4];
+        uint32_t top = 0, low = 0xFFFFFFFFu;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float ge = d[e] * a.grad_scale;
-            const float mn = m[e] * a.beta1 + ge * a.one_beta1;
-            const float vn = v[e] * a.beta2 + (ge * ge) * a.one_beta2;
-            // |.| < inf is false for NaN too
-            const bool ok = fabsf(mn) < INFINITY && vn < INFINITY;
-            v[e] = ok ? vn : v[e];
-            r[e] = sqrtf(v[e]);
-            const float step = (mn * a.rate) / (r[e] * a.fix + a.eps);
-            x[e] = ok ? x[e] * a.keep - step : x[e];
-            m[e] = ok ? mn : m[e];
-            bad |= !ok && (FULL || i + e < n);
+            mn[e] = m[e] * a.beta1 + ge * a.one_beta1;
+            vn[e] = v[e] * a.beta2 + (ge * ge) * a.one_beta2;
+            // as integers, infinities and NaN are above all numbers; 0 - 1 is too
+            const uint32_t mb = __float_as_uint(fabsf(mn[e])), vb = __float_as_uint(vn[e]);
+            top = max(top, max(mb, vb));
+            low = min(low, vb - 1u);
+        }
+        constexpr uint32_t kInf = 0x7F800000u, kLeast = (127u - 100u) << 23;
+        if (__ballot(top >= kInf || low < kLeast - 1u) == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[e] = mn[e];
+                v[e] = vn[e];
+                r[e] = root(v[e]);
+                x[e] = x[e] * a.keep - quotient(m[e] * a.rate, r[e] * a.fix + a.eps);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // |.| < inf is false for NaN too
+                const bool ok = fabsf(mn[e]) < INFINITY && vn[e] < INFINITY;
+                v[e] = ok ? vn[e] : v[e];
+                r[e] = sqrtf(v[e]);
+                const float step = (mn[e] * a.rate) / (r[e] * a.fix + a.eps);
+                x[e] = ok ? x[e] * a.keep - step : x[e];
+                m[e] = ok ? mn[e] : m[e];
+                bad |= !ok && (FULL || i + e < n);
+            }
         }
         store4<FULL>(p, i, n, x);
         Moments<Q8>::store(T.state, padded, i, m, v, r);

@@ -480,6 +480,38 @@ def test_adamw_steps_bit_for_bit(ptype, gtype, states):
     opt.check()
 
 
+@pytest.mark.parametrize("states", ["f32", "q8"])
+def test_adamw_magnitudes(states):
+    """Gradients of 1e-30 to 1e18, whole blocks of zeros, tiny and large moments beside
+    each other: the same bits as the float32 form."""
+    rng = np.random.default_rng(25)
+    f = np.float32
+    size = 64 * 256 + 77
+    p, _, m, v = adam_values(size, rng)
+    g = (rng.normal(size=size) * 10.0 ** rng.uniform(-30, 18, size)).astype(f)
+    scale = np.repeat(10.0 ** rng.uniform(-25, 15, 65), 256)[:size]
+    m, v = (m * scale).astype(f), (v * scale * scale).astype(f)
+    g[:512] = m[:256] = v[:256] = 0
+    g[1024:8192] = (g[1024:8192] * 1e-12).astype(f)
+    ok = np.abs(g) < 1e18
+    g[~ok] = 0
+    t = vec(p)
+    opt = P.AdamW([t], states=states)
+    opt.load([vec(m)], [vec(v)], 3)
+    s = (m, v) if states == "f32" else ref.q8_f32(m, v)
+    for step in (4, 5):
+        opt.step([vec(g)])
+        pn, mn, vn, ok = ref.adamw_f32(p, g, *s, step, 1e-3, 0.9, 0.999, 1e-8, 0.01)
+        assert ok.all()
+        s = (mn, vn) if states == "f32" else ref.q8_f32(mn, vn)
+        gm, gv = opt.values()
+        np.testing.assert_array_equal(gm[0].cpu().numpy(), s[0])
+        np.testing.assert_array_equal(gv[0].cpu().numpy(), s[1])
+        np.testing.assert_array_equal(t.cpu().numpy(), pn)
+        p = pn
+    opt.check()
+
+
 def test_adamw_against_float64():
     rng = np.random.default_rng(22)
     p, g, m, v = adam_values(5000, rng)

@@ -115,7 +115,7 @@ def test_adamw_state_sizes():
 
 @pytest.mark.parametrize("kw", [
     dict(lr=-1.0), dict(lr=math.nan), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
-    dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-60), dict(weight_decay=-1.0),
+    dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-31), dict(weight_decay=-1.0),
     dict(grad_scale=math.inf), dict(step=0), dict(state_kind=2),
 ])
 def test_adamw_refuses_bad_settings(kw):
