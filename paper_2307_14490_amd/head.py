@@ -21,9 +21,9 @@ _DTYPES = {"f32": HUGE_DTYPE_F32, "bf16": HUGE_DTYPE_BF16}
 
 def _dtype_code(t, what):
     import torch
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return HUGE_DTYPE_F32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return HUGE_DTYPE_BF16
     raise TypeError(f"{what}: expected float32 or bfloat16, got {t.dtype}")
 
@@ -35,28 +35,33 @@ def _rows(t, what, dim=None, like=None):
         got = f"shape {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) \
             else type(t).__name__
         raise TypeError(f"{what}: expected a two-dimensional GPU tensor, got {got}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+    if like is not None and (t.dtype is not like.dtype or t.device != like.device):
         raise TypeError(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    if dim is not None and t.shape[1] != dim:
-        raise ValueError(f"{what}: rows of {t.shape[1]}, expected {dim}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{what}: the columns of a row must be adjacent, stride {t.stride(1)}")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if ld < t.shape[1]:
-        raise ValueError(f"{what}: rows overlap (stride {ld} of {t.shape[1]})")
+    n, cols = t.shape
+    if dim is not None and cols != dim:
+        raise ValueError(f"{what}: rows of {cols}, expected {dim}")
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{what}: the columns of a row must be adjacent, stride {step}")
+    if n <= 1:
+        ld = cols
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap (stride {ld} of {cols})")
     return t.data_ptr(), ld
 
 
 def _vector(t, n, dtype, what, device):
     """Pointer of a contiguous GPU vector of n elements (None stays None)."""
+    import torch
     if t is None:
         return None
-    p = _arg(t, (dtype,), what)
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()):
+        _arg(t, (str(dtype).split(".")[1],), what)
     if t.numel() != n:
         raise ValueError(f"{what}: {t.numel()} elements, expected {n}")
     if t.device != device:
         raise ValueError(f"{what}: on {t.device}, expected {device}")
-    return p
+    return t.data_ptr()
 
 
 def _current(device):
@@ -137,8 +142,8 @@ def layer_norm(x, gamma, beta, eps=1e-5, stream=None):
     px, ld = _rows(x, "layer_norm x")
     code = _dtype_code(x, "layer_norm x")
     n, dim = x.shape
-    pg = _vector(gamma, dim, "float32", "layer_norm gamma", x.device)
-    pb = _vector(beta, dim, "float32", "layer_norm beta", x.device)
+    pg = _vector(gamma, dim, torch.float32, "layer_norm gamma", x.device)
+    pb = _vector(beta, dim, torch.float32, "layer_norm beta", x.device)
     if pg is None or pb is None:
         raise TypeError("layer_norm: gamma and beta are required")
     with _on(x.device, stream, (x, gamma, beta,)) as st:
@@ -158,24 +163,24 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, want_dx=True, want_weights=Tru
     pdy, ldy = _rows(dy, "layer_norm_backward dy", dim, x)
     if dy.shape[0] != n:
         raise ValueError(f"layer_norm_backward: {dy.shape[0]} rows of dy, {n} of x")
-    pg = _vector(gamma, dim, "float32", "layer_norm_backward gamma", x.device)
-    pm = _vector(mean, n, "float32", "layer_norm_backward mean", x.device)
-    pr = _vector(rstd, n, "float32", "layer_norm_backward rstd", x.device)
+    pg = _vector(gamma, dim, torch.float32, "layer_norm_backward gamma", x.device)
+    pm = _vector(mean, n, torch.float32, "layer_norm_backward mean", x.device)
+    pr = _vector(rstd, n, torch.float32, "layer_norm_backward rstd", x.device)
     if pg is None or pm is None or pr is None:
         raise TypeError("layer_norm_backward: gamma, mean and rstd are required")
     L = load()
     with _on(x.device, stream, (dy, x, gamma, mean, rstd,)) as st:
         dx = torch.empty((n, dim), dtype=x.dtype, device=x.device) if want_dx else None
-        dw = ws = None
+        dgamma = dbeta = ws = None
         bytes_ = 0
         if want_weights:
             bytes_ = L.huge_layer_norm_workspace_bytes(n, dim)
             ws = torch.empty(bytes_, dtype=torch.uint8, device=x.device)
-            dw = torch.empty((2, dim), dtype=torch.float32, device=x.device)
+            dgamma, dbeta = torch.empty((2, dim), dtype=torch.float32, device=x.device).unbind()
         _ok(L.huge_layer_norm_backward(pdy, ldy, px, ldx, n, dim, code, pg, pm, pr, _dptr(dx), dim,
-                                       _dptr(dw), None if dw is None else dw[1].data_ptr(),
-                                       _dptr(ws), bytes_, st), "huge_layer_norm_backward")
-    return dx, (dw[0] if want_weights else None), (dw[1] if want_weights else None)
+                                       _dptr(dgamma), _dptr(dbeta), _dptr(ws), bytes_, st),
+            "huge_layer_norm_backward")
+    return dx, dgamma, dbeta
 
 
 # --------------------------------------------------------------------------- #
@@ -200,6 +205,7 @@ class SoftmaxLoss(_Status):
 
     def _inputs(self, what, h, w, labels, bias, weights):
         """Pointers in the order of the C calls, checked."""
+        import torch
         c = self.cfg
         ph, ldh = _rows(h, what + " h", c.dim)
         if _dtype_code(h, what + " h") != c.dtype:
@@ -211,16 +217,16 @@ class SoftmaxLoss(_Status):
             raise ValueError(f"{what}: {w.shape[0]} rows of w, expected {c.num_classes}")
         n = h.shape[0]
         return (ctypes.byref(c), ph, ldh, n, pw, ldw,
-                _vector(bias, c.num_classes, "float32", what + " bias", h.device),
-                _vector(labels, n, "int32", what + " labels", h.device),
-                _vector(weights, n, "float32", what + " weights", h.device))
+                _vector(bias, c.num_classes, torch.float32, what + " bias", h.device),
+                _vector(labels, n, torch.int32, what + " labels", h.device),
+                _vector(weights, n, torch.float32, what + " weights", h.device))
 
     def loss(self, h, w, labels, bias=None, weights=None, total=None, stream=None):
         """(loss, lse), float32 per row of h.  total: a float64 tensor of one element
         that receives the sum of the losses."""
         import torch
         a = self._inputs("SoftmaxLoss.loss", h, w, labels, bias, weights)
-        pt = _vector(total, 1, "float64", "SoftmaxLoss.loss total", h.device)
+        pt = _vector(total, 1, torch.float64, "SoftmaxLoss.loss total", h.device)
         self._ordered(stream)
         with _on(self.device, stream, (h, w, labels, bias, weights, total,)) as st:
             loss, lse = torch.empty((2, a[3]), dtype=torch.float32, device=self.device).unbind()
@@ -235,7 +241,7 @@ class SoftmaxLoss(_Status):
         type of h; None where not wanted."""
         import torch
         a = self._inputs("SoftmaxLoss.grad", h, w, labels, bias, weights)
-        pl = _vector(lse, a[3], "float32", "SoftmaxLoss.grad lse", h.device)
+        pl = _vector(lse, a[3], torch.float32, "SoftmaxLoss.grad lse", h.device)
         if pl is None:
             raise TypeError("SoftmaxLoss.grad: lse is required")
         c = self.cfg
@@ -302,11 +308,15 @@ class AdamW(_Status):
         return self.states[at:at + 4 * p.numel()].view(torch.float32).view(p.shape)
 
     def _list(self, ts, dtypes, what):
+        import torch
         ts = list(ts)
         if len(ts) != len(self.params):
             raise ValueError(f"{what}: {len(ts)} tensors, expected {len(self.params)}")
+        types = [getattr(torch, d) for d in dtypes]
         for k, (t, p) in enumerate(zip(ts, self.params)):
-            _arg(t, dtypes, f"{what}[{k}]")
+            if not (isinstance(t, torch.Tensor) and t.dtype in types and t.is_cuda
+                    and t.is_contiguous()):
+                _arg(t, dtypes, f"{what}[{k}]")
             if t.numel() != p.numel() or t.device != p.device:
                 raise ValueError(f"{what}[{k}]: {t.numel()} elements on {t.device}, expected "
                                  f"{p.numel()} on {p.device}")
