@@ -74,6 +74,7 @@ constexpr int64_t kSmPartRows = 131072;              // rows of partial sums of 
 // How a call of n rows is laid out, from its sizes alone.
 struct SoftmaxPlan {
     int32_t dim, parts, nd, chunks, dp, kd;  // nd 32-wide blocks of dp in each of `chunks`
+    int64_t classes;
     int64_t piece;                           // classes packed together (multiple of kSmTile)
     int64_t rows_pad;                        // n in whole tiles
     size_t h, w, part, row_part, total;      // workspace offsets

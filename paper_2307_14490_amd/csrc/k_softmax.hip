@@ -306,17 +306,20 @@ struct PassArgs {
     const uint8_t* y;
     int64_t x_tiles, y_tiles;
     int64_t per;           // Y tiles of a split
-    int32_t x_blocks, splits;
+    int32_t x_blocks;      // workgroups along X: the first x_whole take all of Y, the
+    int32_t x_whole;       // others a split of it each
+    int32_t splits;
     int32_t x_groups;      // waves of a workgroup side by side along X; the others share Y
     int32_t stage;         // Y tiles of an LDS buffer
     int32_t nfrag, kd;
     int32_t forms;
     bool first;            // the first piece of the classes: partial results are written
-    // loss
-    float2* lse_part;      // [split and wave along Y][32 x_tiles]: maximum and sum
-    // gradient
-    float* part;           // [split and wave along Y][32 x_tiles][dp], or null: to `out`
-    float* bias_part;      // the same without [dp] (X: classes), or null
+    // partial results of the rows behind those of the whole workgroups, one slot per
+    // split and wave along Y: [slot][part_rows]...
+    int64_t part_first, part_rows;
+    float2* lse_part;      // loss: maximum and sum
+    float* part;           // gradient: [dp], or null: to `out`
+    float* bias_part;      // gradient of the bias (X: classes)
     void* out;             // x_rows x dim
     float* bias_out;
     int64_t class0;        // first class of the piece
@@ -331,15 +334,20 @@ struct PassArgs {
 // same Y records share an L2.
 struct Place {
     int32_t x_block, split;
+    bool whole, none;
 };
 __device__ __forceinline__ Place place(const PassArgs& a) {
-    const int32_t total = a.x_blocks * a.splits, run = (total + 7) / 8;
-    const int32_t k = (int32_t)(blockIdx.x & 7) * run + (int32_t)(blockIdx.x >> 3);
-    const bool none = k >= total || (int32_t)(blockIdx.x >> 3) >= run;
-    return {k % a.x_blocks, none ? a.splits : k / a.x_blocks};
+    int32_t b = blockIdx.x;
+    const int32_t head = (a.x_whole + 7) / 8 * 8;
+    const bool whole = b < head;
+    if (!whole) b -= head;
+    const int32_t wide = whole ? a.x_whole : a.x_blocks - a.x_whole;
+    const int32_t total = whole ? wide : wide * a.splits, run = (total + 7) / 8;
+    const int32_t k = (b & 7) * run + (b >> 3);
+    return {whole ? k : a.x_whole + k % wide, whole ? 0 : k / wide, whole, k >= total};
 }
-inline int64_t place_grid(int64_t x_blocks, int64_t splits) {
-    return (x_blocks * splits + 7) / 8 * 8;
+inline int64_t place_grid(int64_t x_blocks, int64_t x_whole, int64_t splits) {
+    return (x_whole + 7) / 8 * 8 + ((x_blocks - x_whole) * splits + 7) / 8 * 8;
 }
 
 // Copies n KB to LDS, a wave 1 KB at a time; arrived after the next barrier.
@@ -355,11 +363,11 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to, in
 // Calls body(record) for this wave's Y tiles of the split: tiles yg, yg + yw, ... of
 // each stage.
 template <int WAVES, bool STAGED, typename Body>
-__device__ __forceinline__ void stream_records(const PassArgs& a, int split, int yg, int yw,
+__device__ __forceinline__ void stream_records(const PassArgs& a, const Place& at_, int yg, int yw,
                                                int wave, int lane, int rec_bytes, uint8_t* lds,
                                                Body body) {
-    const int64_t y0 = (int64_t)split * a.per;
-    const int64_t y1 = y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
+    const int64_t y0 = (int64_t)at_.split * a.per;
+    const int64_t y1 = !at_.whole && y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
     if constexpr (!STAGED) {
         for (int64_t yt = y0 + yg; yt < y1; yt += yw) body(a.y + yt * rec_bytes, yt);
     } else {
@@ -478,7 +486,7 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC,
 void k_sm_lse(PassArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
     const Place at = place(a);
-    if (at.split >= a.splits) return;
+    if (at.none) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int xg = wave % a.x_groups, yg = wave / a.x_groups, yw = WAVES / a.x_groups;
@@ -499,7 +507,7 @@ void k_sm_lse(PassArgs a) {
         sum[b] = 0.f;
     }
     stream_records<WAVES, STAGED>(
-        a, at.split, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t) {
+        a, at, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t) {
             f32x16 c[XB];
             const f32x16 term = row_values(rec, kTerm, half);
 #pragma unroll
@@ -534,7 +542,7 @@ void k_sm_lse(PassArgs a) {
         float m = fmaxf(top[b], top2);
         float v = sum[b] * exp_below(top[b], m) + sum2 * exp_below(top2, m);
         if (half == 0 && xt.in[b]) {
-            float2* out = a.lse_part + ((int64_t)at.split * yw + yg) * a.x_tiles * 32 +
+            float2* out = a.lse_part + ((int64_t)at.split * yw + yg) * a.part_rows +
                           xt.t[b] * 32 + lane;
             if (!a.first) {
                 const float2 p = *out;
@@ -815,7 +823,7 @@ void k_sm_grad(PassArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
     constexpr bool kScaled = Kind<E>::kScaled;
     const Place at = place(a);
-    if (at.split >= a.splits) return;
+    if (at.none) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int xg = wave % a.x_groups, yg = wave / a.x_groups, yw = WAVES / a.x_groups;
@@ -851,7 +859,7 @@ void k_sm_grad(PassArgs a) {
         for (int d = 0; d < ND; ++d) acc[b][d] = f32x16{};
     }
     stream_records<WAVES, STAGED>(
-        a, at.split, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t yt) {
+        a, at, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t yt) {
             f32x16 c[XB];
 #pragma unroll
             for (int b = 0; b < XB; ++b) {
@@ -973,7 +981,8 @@ void k_sm_grad(PassArgs a) {
     for (int b = 0; b < XB; ++b) {
         if (!xt.in[b]) continue;
         const int64_t xi = xt.t[b] * 32 + (lane & 31);
-        const int64_t row = ((int64_t)at.split * yw + yg) * a.x_tiles * 32 + xi;
+        const int64_t row = ((int64_t)at.split * yw + yg) * a.part_rows + xi - a.part_first;
+        const bool direct = at.whole || a.part == nullptr;
         const float back = kScaled ? 1.f / pscale[b] : 1.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
@@ -983,7 +992,7 @@ void k_sm_grad(PassArgs a) {
                 float4 v = make_float4(acc[b][d][4 * g], acc[b][d][4 * g + 1],
                                        acc[b][d][4 * g + 2], acc[b][d][4 * g + 3]);
                 if constexpr (kScaled) v = scale4(back, v);
-                if (a.part != nullptr) {
+                if (!direct) {
                     float4* p = reinterpret_cast<float4*>(a.part + row * a.dp + col);
                     *p = a.first ? v : add4(*p, v);
                 } else if (a.out != nullptr && xi < a.x_rows && col < a.dim) {
@@ -993,7 +1002,7 @@ void k_sm_grad(PassArgs a) {
         if (!ROWS && blockIdx.y == 0 && a.want_bias) {
             const float v = bias[b] + __shfl_xor(bias[b], 32);
             if (half == 0) {
-                if (a.bias_part != nullptr) a.bias_part[row] = v;
+                if (!direct) a.bias_part[row] = v;
                 else if (xi < a.x_rows) a.bias_out[xi] = v * a.scale;
             }
         }
@@ -1053,16 +1062,20 @@ constexpr int kSmLds = 152 * 1024;
 
 struct Layout {
     int32_t x_groups, stage;
-    int64_t x_blocks, splits, per, slots;  // slots: partial results per row
+    int64_t x_blocks, x_whole, splits, per;
+    int64_t slots, part_first, part_rows;  // partial results
 };
 
 constexpr int64_t kCus = 256;
 
-// Workgroups along X and splits of Y: whole rounds of the card's places (`resident`
-// workgroups of a CU), unless a split had fewer than four tiles a wave; not more
-// partial rows than kSmPartRows (or one slot's).
+// Workgroups along X and splits of Y.  With x_blocks above the card's places
+// (`resident` workgroups of a CU), whole rounds of them take all of Y (where
+// `whole` allows it) and what is left over is split; else all are.  A split has at
+// least four tiles a wave; there are at most kSmPartRows partial rows (or one
+// slot's).  Of the numbers of splits, the fewest that come within 3% of the
+// shortest: r workgroups of 1 / s each take ceil(r s / places) / s.
 Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident, int rec_bytes,
-               bool staged) {
+               bool staged, bool whole) {
     Layout l{};
     const int64_t groups = div_up(x_tiles, xb);
     int64_t stage = staged ? kSmLds / 2 / resident / rec_bytes : waves;
@@ -1073,25 +1086,28 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
     l.x_groups = g;
     const int yw = waves / g;
     l.x_blocks = div_up(groups, g);
-    int64_t most = y_tiles / (4 * yw);
-    const int64_t room = kSmPartRows / (x_tiles * 32 * yw);
-    if (most > room) most = room;
+    const int64_t places = kCus * resident;
+    if (whole && yw == 1) l.x_whole = l.x_blocks / places * places;
+    const int64_t left = l.x_blocks - l.x_whole;
+    l.part_first = l.x_whole * g * xb * 32;
+    l.part_rows = x_tiles * 32 - l.part_first;
     int64_t want = 1;
-    double best = 0.0;
-    for (int64_t rounds = 1; rounds <= 4 && best < 0.95; ++rounds) {
-        const int64_t places = kCus * resident * rounds;
-        int64_t n = places / l.x_blocks;
-        if (n > most) n = most;
-        if (n < 1) break;
-        const double fill = (double)(n * l.x_blocks) / (double)places;
-        if (fill > best + 0.02) {
-            best = fill;
-            want = n;
+    if (left > 0) {
+        int64_t most = y_tiles / (4 * yw);
+        const int64_t room = kSmPartRows / (l.part_rows * yw);
+        if (most > room) most = room;
+        double best = 1e30;
+        for (int64_t s = 1; s <= most || s == 1; ++s) {
+            const double time = (double)div_up(left * s, places) / (double)s;
+            if (time < 0.97 * best) {
+                best = time;
+                want = s;
+            }
         }
     }
     l.per = div_up(y_tiles, want);
     l.splits = div_up(y_tiles, l.per);
-    l.slots = l.splits * yw;
+    l.slots = left > 0 ? l.splits * yw : 0;
     // as much of LDS as there is, in whole rounds of the waves along Y: a barrier
     // brings the waves into step, and their products then wait for each other
     l.stage = (int32_t)(stage / yw * yw);
@@ -1118,7 +1134,7 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
 template <auto* KERNEL>
 hipError_t launch_pass(const PassArgs& a, int waves, int chunks, int lds, hipStream_t s) {
     if (lds > 64 * 1024) SM_TRY(allow_lds<KERNEL>(kSmLds));
-    const dim3 grid((uint32_t)place_grid(a.x_blocks, a.splits), (uint32_t)chunks);
+    const dim3 grid((uint32_t)place_grid(a.x_blocks, a.x_whole, a.splits), (uint32_t)chunks);
     KERNEL<<<grid, waves * 64, lds, s>>>(a);
     return hipGetLastError();
 }
@@ -1132,9 +1148,10 @@ hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
     const int rec = record_bytes(p.dp / 16, p.parts, a.forms);
     // all pieces are laid out as the first, whose partial results they add to
     const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves,
-                             kOcc * 4 / kWaves, rec, STAGED);
+                             kOcc * 4 / kWaves, rec, STAGED, GRAD && (!ROWS || p.piece >= p.classes));
     a.x_groups = l.x_groups, a.stage = l.stage, a.x_blocks = (int32_t)l.x_blocks;
-    a.splits = (int32_t)l.splits, a.per = l.per;
+    a.x_whole = (int32_t)l.x_whole, a.splits = (int32_t)l.splits, a.per = l.per;
+    a.part_first = l.part_first, a.part_rows = l.part_rows;
     a.nfrag = p.dp / 16, a.kd = p.kd, a.dp = p.dp, a.dim = p.dim;
     fit(a, l);
     const int lds = STAGED ? 2 * l.stage * rec : 0;
@@ -1233,20 +1250,25 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
     return hipSuccess;
 }
 
+// Joins the partial results of the rows from lay.part_first on, of `rows`.
 template <typename E>
-hipError_t join(const SoftmaxPlan& p, const float* part, int64_t slots, int64_t rows_pad,
-                int64_t rows, float scale, void* out, const float* bias_part, float* bias_out,
-                hipStream_t s) {
+hipError_t join(const SoftmaxPlan& p, const float* part, const Layout& lay, int64_t rows,
+                float scale, void* out, const float* bias_part, float* bias_out, hipStream_t s) {
+    rows -= lay.part_first;
+    if (rows <= 0) return hipSuccess;
     const int64_t work = out != nullptr ? rows * (p.dim / 4) : rows;
-    E* o = static_cast<E*>(out);
-    const bool vec = fours(out, 0, sizeof(E));
+    E* o = out == nullptr ? nullptr : static_cast<E*>(out) + lay.part_first * p.dim;
+    if (bias_out != nullptr) bias_out += lay.part_first;
+    const bool vec = fours(o, 0, sizeof(E));
     // few outputs of many splits: 16 threads each
-    if (work < (1 << 18) && slots >= 16)
+    if (work < (1 << 18) && lay.slots >= 16)
         k_sm_join<E, 16><<<dim3((uint32_t)div_up(work * 16, kBlock)), kBlock, 0, s>>>(
-            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, vec, bias_part, bias_out);
+            part, (int)lay.slots, lay.part_rows, p.dp, rows, p.dim, scale, o, vec, bias_part,
+            bias_out);
     else
         k_sm_join<E, 1><<<dim3((uint32_t)div_up(work, kBlock)), kBlock, 0, s>>>(
-            part, (int)slots, rows_pad, p.dp, rows, p.dim, scale, o, vec, bias_part, bias_out);
+            part, (int)lay.slots, lay.part_rows, p.dp, rows, p.dim, scale, o, vec, bias_part,
+            bias_out);
     return hipGetLastError();
 }
 
@@ -1256,7 +1278,8 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
     const int64_t x_tiles = p.rows_pad / kSmTile;
     float* class_part = reinterpret_cast<float*>(a.ws + p.part);
     float* row_part = reinterpret_cast<float*>(a.ws + p.row_part);
-    int64_t row_slots = 0;
+    Layout row_lay{};
+    bool row_parts = false;
     for (int64_t c0 = 0; c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
         const int64_t w_tiles = div_up(count, kSmTile);
@@ -1271,18 +1294,17 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
             g.x_rows = count, g.first = true, g.out = out, g.bias_out = bias_out;
             g.out_vec = fours(out, 0, sizeof(E));
             g.want_bias = bias_out != nullptr;
-            int64_t slots = 0;
+            Layout lay{};
             float* bias_part = nullptr;
             SM_TRY((pass<E, true, false>(p, g, [&](PassArgs& q, const Layout& o) {
-                slots = o.slots;
-                if (slots == 1) return;
+                lay = o;
+                if (o.slots <= 1) return;
                 q.part = class_part;
-                bias_part = class_part + slots * w_tiles * 32 * p.dp;
+                bias_part = class_part + o.slots * o.part_rows * p.dp;
                 q.bias_part = bias_part;
             }, s)));
-            if (slots > 1)
-                SM_TRY(join<E>(p, class_part, slots, w_tiles * 32, count, a.scale, out, bias_part,
-                               bias_out, s));
+            if (lay.slots > 1)
+                SM_TRY(join<E>(p, class_part, lay, count, a.scale, out, bias_part, bias_out, s));
         }
         if (a.dh != nullptr) {
             g.x = a.ws + p.h, g.y = a.ws + p.w, g.x_tiles = x_tiles, g.y_tiles = w_tiles;
@@ -1290,15 +1312,15 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
             g.out_vec = fours(a.dh, 0, sizeof(E));
             g.want_bias = false;
             SM_TRY((pass<E, true, true>(p, g, [&](PassArgs& q, const Layout& o) {
-                row_slots = o.slots;
+                row_lay = o;
                 // sums that stay from piece to piece
-                if (row_slots > 1 || p.piece < a.classes) q.part = row_part;
-                else row_slots = 0;
+                row_parts = o.slots > 1 || p.piece < a.classes;
+                if (row_parts) q.part = row_part;
             }, s)));
         }
     }
-    if (a.dh != nullptr && row_slots > 0)
-        SM_TRY(join<E>(p, row_part, row_slots, p.rows_pad, a.n, a.scale, a.dh, nullptr, nullptr, s));
+    if (row_parts)
+        SM_TRY(join<E>(p, row_part, row_lay, a.n, a.scale, a.dh, nullptr, nullptr, s));
     return hipSuccess;
 }
 
@@ -1306,6 +1328,7 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
 
 SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype, bool grad) {
     SoftmaxPlan p{};
+    p.classes = classes;
     p.dim = dim;
     p.parts = dtype == kDtypeBf16 ? Kind<bf16_t>::kParts : Kind<float>::kParts;
     const int nd = (int)div_up(dim, 32);
