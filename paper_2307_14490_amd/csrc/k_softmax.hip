@@ -481,6 +481,8 @@ __device__ __forceinline__ float exp_below(float a, float b) {
     return a == -INFINITY ? 0.f : exp2f((a - b) * kLog2e);
 }
 
+constexpr float kRise = 8.f;
+
 template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED>
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void k_sm_lse(PassArgs a) {
@@ -521,15 +523,19 @@ void k_sm_lse(PassArgs a) {
                     for (int i = 0; i < 16; ++i)
                         c[b][i] = fmaf(c[b][i] * ymul[i], xmul[b], term[i]);
             }
+            // `top` is where the sums' exponentials start from, and is raised only when a
+            // logit is far above it: sums of a few hundred e^kRise are no trouble
 #pragma unroll
             for (int b = 0; b < XB; ++b) {
-                float m = top[b];
+                float m = c[b][0];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) m = fmaxf(m, c[b][i]);
-                const float ref = m == -INFINITY ? 0.f : m;
-                sum[b] *= exp_below(top[b], ref);
-                top[b] = m;
-                const float sub = -ref * kLog2e;
+                for (int i = 1; i < 16; ++i) m = fmaxf(m, c[b][i]);
+                if (__ballot(m > top[b] + kRise) != 0) {
+                    const float up = fmaxf(m, top[b]);
+                    sum[b] *= exp_below(top[b], up);
+                    top[b] = up;
+                }
+                const float sub = top[b] == -INFINITY ? 0.f : -top[b] * kLog2e;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     sum[b] += __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, sub));
@@ -868,8 +874,11 @@ void k_sm_grad(PassArgs a) {
                 } else if constexpr (ROWS) {
                     c[b] = row_values(rec, kTerm, half);
                 } else {
+                    // written anew for every tile: kept, it would take 16 registers
+                    float bias0 = xterm[b];
+                    asm("" : "+v"(bias0));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) c[b][i] = xterm[b];
+                    for (int i = 0; i < 16; ++i) c[b][i] = bias0;
                 }
             }
             tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
