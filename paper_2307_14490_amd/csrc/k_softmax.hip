@@ -313,6 +313,8 @@ struct PassArgs {
     int32_t stage;         // Y tiles of an LDS buffer
     int32_t nfrag, kd;
     int32_t forms;
+    const bf16_t* y_rows;  // loss: the classes unpacked, instead of y
+    int64_t ld, classes;
     bool first;            // the first piece of the classes: partial results are written
     // partial results of the rows behind those of the whole workgroups, one slot per
     // split and wave along Y: [slot][part_rows]...
@@ -360,27 +362,47 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to, in
             (__attribute__((address_space(3))) void*)(to + k * 1024), 16, 0, 0);
 }
 
+// Copies the rows of n tiles to LDS as records without a header, straight from a
+// bf16 matrix of `nfrag` operands a row: each lane of an operand fetches its own 16
+// bytes.  A wave takes four operands of a tile, 128 bytes of every row.
+template <int WAVES>
+__device__ __forceinline__ void gather_to_lds(const bf16_t* m, int64_t ld, int64_t rows,
+                                              int64_t tile, uint8_t* to, int n, int nfrag,
+                                              int wave, int lane) {
+    const int quads = nfrag / 2 > 1 ? nfrag / 4 + (nfrag % 4 != 0) : 1;
+    for (int k = wave; k < n * quads; k += WAVES) {
+        const int t = k / quads, f0 = k % quads * 4;
+        int64_t row = (tile + t) * 32 + (lane & 31);
+        row = row < rows ? row : rows - 1;
+        const bf16_t* from = m + row * ld + 16 * f0 + 8 * (lane >> 5);
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+            if (f0 + f < nfrag)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void*)(from + 16 * f),
+                    (__attribute__((address_space(3))) void*)(to + (t * nfrag + f0 + f) * 1024),
+                    16, 0, 0);
+    }
+}
+
 // Calls body(record) for this wave's Y tiles of the split: tiles yg, yg + yw, ... of
-// each stage.
-template <int WAVES, bool STAGED, typename Body>
+// each stage.  copy(tile, buffer, n) brings n of them to LDS.
+template <int WAVES, bool STAGED, typename Copy, typename Body>
 __device__ __forceinline__ void stream_records(const PassArgs& a, const Place& at_, int yg, int yw,
-                                               int wave, int lane, int rec_bytes, uint8_t* lds,
-                                               Body body) {
+                                               int rec_bytes, uint8_t* lds, Copy copy, Body body) {
     const int64_t y0 = (int64_t)at_.split * a.per;
     const int64_t y1 = !at_.whole && y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
     if constexpr (!STAGED) {
         for (int64_t yt = y0 + yg; yt < y1; yt += yw) body(a.y + yt * rec_bytes, yt);
     } else {
-        const int kb = rec_bytes / 1024;
         auto tiles = [&](int64_t at) { return (int)(y1 - at < a.stage ? y1 - at : a.stage); };
         uint8_t* buf = lds;
         uint8_t* next = lds + a.stage * rec_bytes;
-        if (y0 < y1) copy_to_lds<WAVES>(a.y + y0 * rec_bytes, buf, tiles(y0) * kb, wave, lane);
+        if (y0 < y1) copy(y0, buf, tiles(y0));
         __syncthreads();
         for (int64_t at = y0; at < y1; at += a.stage) {
             const int64_t after = at + a.stage;
-            if (after < y1)
-                copy_to_lds<WAVES>(a.y + after * rec_bytes, next, tiles(after) * kb, wave, lane);
+            if (after < y1) copy(after, next, tiles(after));
             const int n = tiles(at);
             for (int t = yg; t < n; t += yw) body(buf + t * rec_bytes, at + t);
             __syncthreads();
@@ -483,7 +505,7 @@ __device__ __forceinline__ float exp_below(float a, float b) {
 
 constexpr float kRise = 8.f;
 
-template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED>
+template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED, bool DIRECT>
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void k_sm_lse(PassArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
@@ -508,13 +530,29 @@ void k_sm_lse(PassArgs a) {
         top[b] = -INFINITY;
         sum[b] = 0.f;
     }
+    // DIRECT: no headers; there is no bias then, only the end of the classes
+    const int y_bytes = DIRECT ? 2 * ND * 1024 : rec_bytes;
     stream_records<WAVES, STAGED>(
-        a, at, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t) {
-            f32x16 c[XB];
-            const f32x16 term = row_values(rec, kTerm, half);
+        a, at, yg, yw, y_bytes, lds,
+        [&](int64_t tile, uint8_t* to, int n) {
+            if constexpr (DIRECT)
+                gather_to_lds<WAVES>(a.y_rows, a.ld, a.classes, tile, to, n, 2 * ND, wave, lane);
+            else
+                copy_to_lds<WAVES>(a.y + tile * rec_bytes, to, n * (rec_bytes / 1024), wave, lane);
+        },
+        [&](const uint8_t* rec, int64_t yt) {
+            f32x16 c[XB], term = {};
+            if constexpr (!DIRECT) {
+                term = row_values(rec, kTerm, half);
+            } else if (yt * 32 + 32 > a.classes) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (yt * 32 + tile_row(i, half) >= a.classes) term[i] = -INFINITY;
+            }
 #pragma unroll
             for (int b = 0; b < XB; ++b) c[b] = Kind<E>::kScaled ? f32x16{} : term;
-            tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
+            tile_products<E, ND, XB, STAGED>(DIRECT ? rec - kHeader : rec, x, xt.rec, nfrag, a.kd,
+                                             lane, c);
             if constexpr (Kind<E>::kScaled) {
                 const f32x16 ymul = row_values(rec, kMul, half);
 #pragma unroll
@@ -865,7 +903,11 @@ void k_sm_grad(PassArgs a) {
         for (int d = 0; d < ND; ++d) acc[b][d] = f32x16{};
     }
     stream_records<WAVES, STAGED>(
-        a, at, yg, yw, wave, lane, rec_bytes, lds, [&](const uint8_t* rec, int64_t yt) {
+        a, at, yg, yw, rec_bytes, lds,
+        [&](int64_t tile, uint8_t* to, int n) {
+            copy_to_lds<WAVES>(a.y + tile * rec_bytes, to, n * (rec_bytes / 1024), wave, lane);
+        },
+        [&](const uint8_t* rec, int64_t yt) {
             f32x16 c[XB];
 #pragma unroll
             for (int b = 0; b < XB; ++b) {
@@ -1082,7 +1124,8 @@ constexpr int64_t kCus = 256;
 // `whole` allows it) and what is left over is split; else all are.  A split has at
 // least four tiles a wave; there are at most kSmPartRows partial rows (or one
 // slot's).  Of the numbers of splits, the fewest that come within 3% of the
-// shortest: r workgroups of 1 / s each take ceil(r s / places) / s.
+// shortest: r workgroups of 1 / s each take ceil(r s / places) / s, and a start that
+// costs about as much as four tiles.
 Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident, int rec_bytes,
                bool staged, bool whole) {
     Layout l{};
@@ -1107,7 +1150,8 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
         if (most > room) most = room;
         double best = 1e30;
         for (int64_t s = 1; s <= most || s == 1; ++s) {
-            const double time = (double)div_up(left * s, places) / (double)s;
+            const double time = (double)div_up(left * s, places) *
+                                (1.0 / (double)s + 4.0 / (double)y_tiles);
             if (time < 0.97 * best) {
                 best = time;
                 want = s;
@@ -1149,12 +1193,12 @@ hipError_t launch_pass(const PassArgs& a, int waves, int chunks, int lds, hipStr
 }
 
 // Fills in the layout and launches the pass; `fit` sets the outputs from it.
-template <typename E, int ND, bool GRAD, bool STAGED, bool ROWS, typename Fit>
+template <typename E, int ND, bool GRAD, bool STAGED, bool ROWS, bool DIRECT, typename Fit>
 hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
     constexpr int kXB = STAGED ? Shape<E, ND, GRAD>::kXB : 1;
     constexpr int kWaves = STAGED ? Shape<E, ND, GRAD>::kWaves : 8;
     constexpr int kOcc = STAGED ? Shape<E, ND, GRAD>::kOcc : 2;
-    const int rec = record_bytes(p.dp / 16, p.parts, a.forms);
+    const int rec = DIRECT ? 2 * ND * 1024 : record_bytes(p.dp / 16, p.parts, a.forms);
     // all pieces are laid out as the first, whose partial results they add to
     const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves,
                              kOcc * 4 / kWaves, rec, STAGED, GRAD && (!ROWS || p.piece >= p.classes));
@@ -1168,15 +1212,19 @@ hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
         return launch_pass<&k_sm_grad<E, ND, kXB, kWaves, kOcc, STAGED, ROWS>>(a, kWaves, p.chunks, lds,
                                                                         s);
     else
-        return launch_pass<&k_sm_lse<E, ND, kXB, kWaves, kOcc, STAGED>>(a, kWaves, 1, lds, s);
+        return launch_pass<&k_sm_lse<E, ND, kXB, kWaves, kOcc, STAGED, DIRECT>>(a, kWaves, 1, lds,
+                                                                               s);
 }
 
 template <typename E, bool GRAD, bool ROWS, typename Fit>
 hipError_t pass(const SoftmaxPlan& p, const PassArgs& a, Fit fit, hipStream_t s) {
     HUGE_SM_ND(p.nd, {
-        if (p.chunks == 1) return run_pass<E, ND, GRAD, true, ROWS>(p, a, fit, s);
+        if constexpr (!GRAD && sizeof(E) == 2)
+            if (a.y_rows != nullptr)
+                return run_pass<E, ND, GRAD, true, ROWS, true>(p, a, fit, s);
+        if (p.chunks == 1) return run_pass<E, ND, GRAD, true, ROWS, false>(p, a, fit, s);
         // rows above 256 columns: at least five blocks in each of two chunks or more
-        if constexpr (ND >= 6) return run_pass<E, ND, GRAD, false, ROWS>(p, a, fit, s);
+        if constexpr (ND >= 6) return run_pass<E, ND, GRAD, false, ROWS, false>(p, a, fit, s);
     })
     return hipErrorInvalidValue;
 }
@@ -1185,7 +1233,7 @@ bool fours(const void* m, int64_t ld, size_t elem) {
     return (reinterpret_cast<uintptr_t>(m) & (4 * elem - 1)) == 0 && ld % 4 == 0;
 }
 
-// Packs a piece of the classes, and before the first the rows.
+// Packs a piece of the classes (or none), and before the first the rows.
 template <typename E>
 hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t count, int forms,
                 hipStream_t s) {
@@ -1238,7 +1286,18 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
                 : few == 2 ? few_pass<E, 2>(a, part, &slots, s)
                            : few_pass<E, 4>(a, part, &slots, s)));
     }
-    for (int64_t c0 = 0; few == 0 && c0 < a.classes; c0 += p.piece) {
+    // bf16 classes without a bias whose rows are whole operands are used as they lie
+    const bool direct = few == 0 && sizeof(E) == 2 && a.bias == nullptr && a.vec16 &&
+                        p.chunks == 1 && a.dim == p.dp;
+    if (direct) {
+        SM_TRY(pack<E>(p, a, 0, 0, 1, s));
+        PassArgs l{};
+        l.x = a.ws + p.h, l.forms = 1, l.first = true, l.lse_part = part;
+        l.y_rows = static_cast<const bf16_t*>(a.w), l.ld = a.ld_w, l.classes = a.classes;
+        l.x_tiles = p.rows_pad / kSmTile, l.y_tiles = div_up(a.classes, kSmTile);
+        SM_TRY((pass<E, false, false>(p, l, [&](PassArgs&, const Layout& o) { slots = o.slots; }, s)));
+    }
+    for (int64_t c0 = 0; few == 0 && !direct && c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
         SM_TRY(pack<E>(p, a, c0, count, 1, s));
         PassArgs l{};

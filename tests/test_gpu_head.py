@@ -229,6 +229,57 @@ def test_softmax_loss_and_gradient(n, classes, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 256, 512])
+def test_softmax_aligned_without_bias(dim, dtype):
+    """Rows of whole 16-byte pieces and no bias: the table is used as it lies."""
+    rng = np.random.default_rng(dim)
+    for n, classes, pad in ((90, 77, 0), (200, 1003, 8), (333, 64, 0)):
+        say(f"softmax {n} x {classes} x {dim} {dtype}, pad {pad}")
+        check_softmax(softmax_case(n, classes, dim, dtype, rng, pad=pad, bias=False), dtype)
+
+
+def softmax_on_device(h, w, labels, bias, c, scale):
+    """loss, lse, dh, dw, dbias in float64 on the GPU, for sizes beyond the oracle's."""
+    h, w, labels = h.double(), w.double(), labels.long()
+    x = h @ w.t() + bias.double()
+    lse = torch.logsumexp(x, 1)
+    live = labels >= 0
+    at = x.gather(1, labels.clamp(min=0)[:, None])[:, 0]
+    k = torch.where(live, c.double(), torch.zeros_like(at))
+    g = torch.exp(x - lse[:, None]) * (k * scale)[:, None]
+    g[torch.arange(len(h), device="cuda")[live], labels[live]] -= (k * scale)[live]
+    return k * (lse - at), lse, g @ w, g.t().contiguous() @ h, g.sum(0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,dim", [(140_003, 37, 32), (70, 140_003, 32), (110_001, 70, 128),
+                                           (96, 150_001, 100), (9_001, 3_001, 256)])
+def test_softmax_many_tiles(n, classes, dim, dtype):
+    """More tiles than the card takes at once: whole rounds of them and what is left
+    over, along the rows and along the classes."""
+    say(f"softmax {n} x {classes} x {dim} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(n + dim)
+    new = lambda *s: torch.randn(s, device="cuda", generator=g)  # noqa: E731
+    h = new(n, dim).to(TYPES[dtype])
+    w = (new(classes, dim) * 1.5 / math.sqrt(dim)).to(TYPES[dtype])
+    labels = torch.randint(-1, classes, (n,), device="cuda", generator=g).to(torch.int32)
+    bias, c = new(classes), torch.rand(n, device="cuda", generator=g) + 0.5
+    op = P.SoftmaxLoss(n, classes, dim, dtype=dtype)
+    loss, lse = op.loss(h, w, labels, bias, c)
+    got = (loss, lse, *op.grad(h, w, labels, lse, bias, c, scale=1.0))
+    want = softmax_on_device(h, w, labels, bias, c, 1.0)
+    # norms here: fp32 sums of many terms about 1e-6, a rounding to bf16 and one of
+    # the probabilities before it 2^-8 each at most
+    for name, x, y in zip(("loss", "lse", "dh", "dw", "db"), got, want):
+        tol = 2.0 ** -8 if dtype == "bf16" and name in ("dh", "dw") else 2e-6
+        err = ((x.double() - y).norm() / y.norm()).item()
+        far = ((x.double() - y).abs().max() / y.abs().max()).item()
+        say(f"  {name}: {err:.3g} of the norm, {far:.3g} of the largest")
+        assert err <= tol and far <= 4 * tol, name
+    op.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_softmax_many_rows_few_classes_and_few_rows_many_classes(dtype):
     rng = np.random.default_rng(11)
     check_softmax(softmax_case(20_011, 37, 32, dtype, rng), dtype)
