@@ -151,6 +151,15 @@ __device__ __forceinline__ f32x16 row_values(const uint8_t* rec, Field f, int ha
     return r;
 }
 
+// Sum of a lane's elements of a tile, in pairs: added one by one to a running sum,
+// each would be rounded at the size of that.
+__device__ __forceinline__ float sum16(f32x16 v) {
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = v[i] + v[i + 8];
+    return ((s[0] + s[4]) + (s[2] + s[6])) + ((s[1] + s[5]) + (s[3] + s[7]));
+}
+
 // A lane's value of a header field (its row is the lane's column).
 __device__ __forceinline__ int32_t lane_label(const uint8_t* rec, int lane) {
     typedef int32_t one __attribute__((ext_vector_type(2)));
@@ -576,7 +585,8 @@ void k_sm_lse(PassArgs a) {
                 const float sub = top[b] == -INFINITY ? 0.f : -top[b] * kLog2e;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    sum[b] += __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, sub));
+                    c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, sub));
+                sum[b] += sum16(c[b]);
             }
         });
 #pragma unroll
@@ -983,8 +993,7 @@ void k_sm_grad(PassArgs a) {
                         }
                     }
                     if (a.want_bias) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) bias[b] += c[b][i];
+                        bias[b] += sum16(c[b]);
                     }
                 }
             }
