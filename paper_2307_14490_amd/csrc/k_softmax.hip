@@ -645,8 +645,8 @@ struct Few<float> {
     }
 };
 
-// 16 bytes of a row at a column, 0 past its end.
-template <typename E, bool VEC>
+// 16 bytes of a row at a column, 0 past its end, read BYTES at a time.
+template <typename E, int BYTES>
 __device__ __forceinline__ typename Few<E>::Vec load_few_cols(const E* row, int col, int dim) {
     using Vec = typename Few<E>::Vec;
     constexpr int kN = 16 / sizeof(E);
@@ -654,8 +654,14 @@ __device__ __forceinline__ typename Few<E>::Vec load_few_cols(const E* row, int 
         Vec v;
         E e[kN];
     } u;
-    if constexpr (VEC) {
+    if constexpr (BYTES == 16) {
         u.v = col < dim ? *reinterpret_cast<const Vec*>(row + col) : Vec{};
+    } else if constexpr (BYTES == 8) {  // bf16 rows of an odd number of fours
+        typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+        const u16x4 a = col < dim ? *reinterpret_cast<const u16x4*>(row + col) : u16x4{};
+        const u16x4 b = col + 4 < dim ? *reinterpret_cast<const u16x4*>(row + col + 4) : u16x4{};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u.e[j] = a[j], u.e[4 + j] = b[j];
     } else {
 #pragma unroll
         for (int j = 0; j < kN; ++j) u.e[j] = col + j < dim ? row[col + j] : (E)0;
@@ -664,7 +670,7 @@ __device__ __forceinline__ typename Few<E>::Vec load_few_cols(const E* row, int 
 }
 
 // NB blocks of 16 rows.
-template <typename E, int NB, bool VEC>
+template <typename E, int NB, int BYTES>
 __global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
                                                            float2* __restrict__ part, int64_t pad) {
     using F = Few<E>;
@@ -678,7 +684,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_
     for (int j = threadIdx.x; j < ops * NB * 64; j += kFewWaves * 64) {
         const int l = j & 63, b = (j >> 6) % NB, k = (j >> 6) / NB;
         const int64_t row = 16 * b + (l & 15);
-        sh[j] = row < a.n ? load_few_cols<E, VEC>(static_cast<const E*>(a.h) + row * a.ld_h,
+        sh[j] = row < a.n ? load_few_cols<E, BYTES>(static_cast<const E*>(a.h) + row * a.ld_h,
                                                   F::kCols * k + kN * (l >> 4), a.dim)
                           : Vec{};
     }
@@ -693,7 +699,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_
 #pragma unroll
         for (int i = 0; i < kFewGroup; ++i)
             if (g * kFewGroup + i < ops)
-                v[i] = load_few_cols<E, VEC>(w + row * a.ld_w,
+                v[i] = load_few_cols<E, BYTES>(w + row * a.ld_w,
                                              F::kCols * (g * kFewGroup + i) + kN * quad, a.dim);
     };
     float top[NB], sum[NB];
@@ -1110,13 +1116,30 @@ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // X, the sums and a tile allow.
 template <typename E, int ND, bool GRAD>
 struct Shape {
-    static constexpr bool kWide = sizeof(E) == 4;  // fp32: two parts
-    static constexpr int kXB = !GRAD && !kWide && ND <= 4 ? 2 : 1;
-    static constexpr int kOcc = !GRAD ? (kWide ? (ND <= 4 ? 4 : 2) : 4)
-                              : kWide ? (ND <= 1 ? 4 : ND <= 2 ? 3 : ND <= 4 ? 2 : 1)
-                                      : (ND <= 2 ? 4 : ND <= 4 ? 3 : 2);
+    static constexpr bool kTwo = sizeof(E) == 4;  // fp32: two parts
+    static constexpr int kXB = !GRAD && !kTwo && ND <= 4 ? 2 : 1;
+    static constexpr int loss_occ() {
+        if (kTwo) return ND <= 4 ? 4 : ND <= 8 ? 2 : 1;
+        return ND <= 8 ? 4 : ND <= 12 ? 3 : 2;
+    }
+    static constexpr int grad_occ() {
+        if (kTwo) return ND <= 1 ? 4 : ND <= 2 ? 3 : ND <= 4 ? 2 : 1;
+        return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 8 ? 2 : 1;
+    }
+    static constexpr int kOcc = GRAD ? grad_occ() : loss_occ();
     static constexpr int kWaves = kOcc == 4 ? 8 : 4 * kOcc;
+    // Rows of up to this many blocks go through LDS whole: two records, and X, the sums
+    // and a tile within a wave's 512 registers.
+    static constexpr int kMostStaged = !GRAD ? 16 : kTwo ? 8 : 12;
+    static constexpr bool kStaged = ND <= kMostStaged;
 };
+
+// Blocks of 32 columns that the kernels are made for.
+inline int made_for(int nd) {
+    for (int k : {1, 2, 3, 4, 6, 8, 10, 12, 16})
+        if (nd <= k) return k;
+    return 0;
+}
 
 constexpr int kSmLds = 152 * 1024;
 
@@ -1184,6 +1207,9 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
         case 4: { constexpr int ND = 4; __VA_ARGS__; } break; \
         case 6: { constexpr int ND = 6; __VA_ARGS__; } break; \
         case 8: { constexpr int ND = 8; __VA_ARGS__; } break; \
+        case 10: { constexpr int ND = 10; __VA_ARGS__; } break; \
+        case 12: { constexpr int ND = 12; __VA_ARGS__; } break; \
+        case 16: { constexpr int ND = 16; __VA_ARGS__; } break; \
         default: return hipErrorInvalidValue;           \
     }
 
@@ -1205,8 +1231,8 @@ hipError_t launch_pass(const PassArgs& a, int waves, int chunks, int lds, hipStr
 template <typename E, int ND, bool GRAD, bool STAGED, bool ROWS, bool DIRECT, typename Fit>
 hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
     constexpr int kXB = STAGED ? Shape<E, ND, GRAD>::kXB : 1;
-    constexpr int kWaves = STAGED ? Shape<E, ND, GRAD>::kWaves : 8;
-    constexpr int kOcc = STAGED ? Shape<E, ND, GRAD>::kOcc : 2;
+    constexpr int kOcc = STAGED ? Shape<E, ND, GRAD>::kOcc : ND > 8 ? 1 : 2;
+    constexpr int kWaves = STAGED ? Shape<E, ND, GRAD>::kWaves : 4 * kOcc;
     const int rec = DIRECT ? 2 * ND * 1024 : record_bytes(p.dp / 16, p.parts, a.forms);
     // all pieces are laid out as the first, whose partial results they add to
     const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves,
@@ -1231,9 +1257,11 @@ hipError_t pass(const SoftmaxPlan& p, const PassArgs& a, Fit fit, hipStream_t s)
         if constexpr (!GRAD && sizeof(E) == 2)
             if (a.y_rows != nullptr)
                 return run_pass<E, ND, GRAD, true, ROWS, true>(p, a, fit, s);
-        if (p.chunks == 1) return run_pass<E, ND, GRAD, true, ROWS, false>(p, a, fit, s);
-        // rows above 256 columns: at least five blocks in each of two chunks or more
-        if constexpr (ND >= 6) return run_pass<E, ND, GRAD, false, ROWS, false>(p, a, fit, s);
+        if constexpr (Shape<E, ND, GRAD>::kStaged)
+            if (p.chunks == 1) return run_pass<E, ND, GRAD, true, ROWS, false>(p, a, fit, s);
+        // wider rows: at least half of the largest ND in each of two chunks or more
+        if constexpr (GRAD ? ND >= 6 && Shape<E, ND, GRAD>::kStaged : ND == 8)
+            return run_pass<E, ND, GRAD, false, ROWS, false>(p, a, fit, s);
     })
     return hipErrorInvalidValue;
 }
@@ -1269,10 +1297,18 @@ hipError_t few_pass(const SoftmaxArgs& a, float2* part, int64_t* slots, hipStrea
     const int64_t tiles = div_up(a.classes, 16);
     const int64_t most = 2048, blocks = div_up(tiles, kFewWaves) < most ? div_up(tiles, kFewWaves) : most;
     const int lds = (int)div_up(a.dim, Few<E>::kCols) * NB * 1024;
-    const bool vec = a.vec16;
     const dim3 grid((uint32_t)blocks);
-    if (vec) k_sm_few<E, NB, true><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
-    else k_sm_few<E, NB, false><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+    if (a.vec16) {
+        k_sm_few<E, NB, 16><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+    } else {
+        if constexpr (sizeof(E) == 2)
+            if (a.vec) {
+                k_sm_few<E, NB, 8><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+                *slots = blocks;
+                return hipGetLastError();
+            }
+        k_sm_few<E, NB, sizeof(E)><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+    }
     *slots = blocks;
     return hipGetLastError();
 }
@@ -1409,15 +1445,15 @@ SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype,
     p.dim = dim;
     p.parts = dtype == kDtypeBf16 ? Kind<bf16_t>::kParts : Kind<float>::kParts;
     const int nd = (int)div_up(dim, 32);
-    p.chunks = (int)div_up(nd, 8);
-    p.nd = (int)div_up(nd, p.chunks);
-    if (p.nd == 5 || p.nd == 7) ++p.nd;
+    const int most = !grad ? 16 : p.parts == 2 ? 8 : 12;
+    p.chunks = (int)div_up(nd, nd > most && !grad ? 8 : most);
+    p.nd = nd > most && !grad ? 8 : made_for((int)div_up(nd, p.chunks));
     p.dp = 32 * p.nd * p.chunks;
     p.kd = (int)div_up(dim, 16);
     const int64_t rec = record_bytes(p.dp / 16, p.parts, grad ? 2 : 1);
     p.piece = div_up(classes, kSmTile) * kSmTile;
-    const int64_t most = kSmPieceBytes / rec * kSmTile;
-    if (p.piece > most) p.piece = most;
+    const int64_t fits = kSmPieceBytes / rec * kSmTile;
+    if (p.piece > fits) p.piece = fits;
     p.rows_pad = n > 0 ? div_up(n, kSmTile) * kSmTile : kSmTile;
     size_t off = 0;
     auto take = [&](int64_t bytes) {

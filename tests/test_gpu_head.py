@@ -214,7 +214,8 @@ def check_softmax(k, dtype, scale=0.5, grad=True):
 
 SOFT = [(1, 1, 4), (1, 2, 8), (2, 33, 4), (5, 31, 36), (33, 32, 32), (32, 65, 64), (100, 257, 100),
         (129, 1000, 128), (300, 10, 128), (64, 511, 160), (70, 300, 224), (31, 999, 256),
-        (40, 333, 260), (65, 130, 384), (17, 70, 516), (40, 64, 1024), (1000, 5, 32),
+        (40, 333, 260), (65, 130, 384), (17, 70, 516), (90, 200, 300), (100, 99, 420),
+        (70, 150, 772), (66, 90, 900), (67, 301, 188), (40, 64, 1024), (1000, 5, 32),
         (1, 5000, 64), (7, 3001, 24), (513, 700, 68)]
 
 
@@ -229,7 +230,7 @@ def test_softmax_loss_and_gradient(n, classes, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 256, 512])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 256, 320, 384, 512, 640])
 def test_softmax_aligned_without_bias(dim, dtype):
     """Rows of whole 16-byte pieces and no bias: the table is used as it lies."""
     rng = np.random.default_rng(dim)
