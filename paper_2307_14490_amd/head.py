@@ -297,6 +297,14 @@ class AdamW(_Status):
             t.d_param, t.n = p.data_ptr(), p.numel()
             t.d_state = self.states.data_ptr() + self._skip + self._state_at[k]
             t.param_dtype = _dtype_code(p, f"AdamW params[{k}]")
+        # where values() puts the moments: one array, each 16-byte aligned in it
+        self._flat_at, self._flat_split, self._flat = [], [], 0
+        for p in 2 * self.params:
+            pad = -p.numel() % 4
+            self._flat_at.append(self._flat)
+            self._flat_split += [p.numel(), pad]
+            self._flat += p.numel() + pad
+        self._values = (ctypes.c_void_p * (2 * count))()
         if self.kind == HUGE_STATE_F32:  # m, then v, each in whole blocks of 256
             half = [L.huge_adamw_state_bytes(p.numel(), self.kind) // 2 for p in self.params]
             self._views = [[self._view(self._state_at[k] + which * half[k], p)
@@ -349,11 +357,18 @@ class AdamW(_Status):
             return [list(ts) for ts in self._views]
         self._ordered(stream)
         with _on(self.device, stream, (self.states,)) as st:
-            m, v = ([torch.empty(p.shape, dtype=torch.float32, device=self.device)
-                     for p in self.params] for _ in range(2))
-            _ok(load().huge_adamw_get_state(self._tensors, len(m), self.kind, self._pointers(m),
-                                            self._pointers(v), st), "huge_adamw_get_state")
-        return m, v
+            flat = torch.empty(self._flat, dtype=torch.float32, device=self.device)
+            base, count = flat.data_ptr(), len(self.params)
+            for k, at in enumerate(self._flat_at):
+                self._values[k] = base + 4 * at
+            m, v = (ctypes.byref(self._values, 8 * count * which) for which in (0, 1))
+            _ok(load().huge_adamw_get_state(self._tensors, count, self.kind,
+                                            ctypes.cast(m, ctypes.POINTER(ctypes.c_void_p)),
+                                            ctypes.cast(v, ctypes.POINTER(ctypes.c_void_p)), st),
+                "huge_adamw_get_state")
+        parts = flat.split(self._flat_split)[::2]
+        out = [t if p.dim() == 1 else t.view(p.shape) for t, p in zip(parts, 2 * self.params)]
+        return out[:count], out[count:]
 
     def load(self, m, v, steps, stream=None):
         """Set the moments (float32, v >= 0) and the steps that they have seen."""
