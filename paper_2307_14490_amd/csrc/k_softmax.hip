@@ -338,6 +338,9 @@ struct PassArgs {
     int32_t dp, dim;
     float scale;
     bool want_bias, out_vec;
+    // host: workgroups and bytes of LDS
+    int64_t grid;
+    int32_t lds;
 };
 
 // The workgroup's place.  Workgroups go to the eight XCDs in turn; each XCD takes a
@@ -347,8 +350,7 @@ struct Place {
     int32_t x_block, split;
     bool whole, none;
 };
-__device__ __forceinline__ Place place(const PassArgs& a) {
-    int32_t b = blockIdx.x;
+__device__ __forceinline__ Place place(const PassArgs& a, int32_t b) {
     const int32_t head = (a.x_whole + 7) / 8 * 8;
     const bool whole = b < head;
     if (!whole) b -= head;
@@ -518,7 +520,7 @@ template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED, bool DIRE
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void k_sm_lse(PassArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
-    const Place at = place(a);
+    const Place at = place(a, blockIdx.x);
     if (at.none) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -877,12 +879,10 @@ __device__ __forceinline__ void store_out(E* p, float4 v, float scale, bool vec)
 }
 
 // ROWS: X are the rows and Y the classes (dh), else X are the classes (dw).
-template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED, bool ROWS>
-__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
-void k_sm_grad(PassArgs a) {
-    extern __shared__ __align__(16) uint8_t lds[];
+template <typename E, int ND, int XB, int WAVES, bool STAGED, bool ROWS>
+__device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uint8_t* lds) {
     constexpr bool kScaled = Kind<E>::kScaled;
-    const Place at = place(a);
+    const Place at = place(a, block);
     if (at.none) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1075,36 +1075,67 @@ void k_sm_grad(PassArgs a) {
     }
 }
 
-// The splits' partial sums, in an order that the sizes fix: LANES threads take
-// every LANES-th split of four columns, then add up.
+// Both gradients in one launch, the classes' workgroups first: one's last workgroups
+// share the card with the other's first.
+template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED>
+__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+void k_sm_grad(PassArgs classes, PassArgs rows, int32_t class_blocks) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int32_t b = blockIdx.x;
+    if (b < class_blocks) grad_block<E, ND, XB, WAVES, STAGED, false>(classes, b, lds);
+    else grad_block<E, ND, XB, WAVES, STAGED, true>(rows, b - class_blocks, lds);
+}
+
+// Partial results to be joined: `rows` rows from a slot each, part_rows apart.
+struct JoinArgs {
+    const float* part;
+    const float* bias_part;
+    void* out;
+    float* bias_out;
+    int64_t part_rows, rows;
+    int32_t slots, lanes;  // threads that share an output
+    int64_t blocks;        // workgroups
+    bool vec;
+};
+
+// The slots of four columns (or a bias), in an order that the sizes fix: LANES
+// threads take every LANES-th, then add up.
 template <typename E, int LANES>
-__global__ __launch_bounds__(kBlock) void k_sm_join(const float* __restrict__ part, int splits,
-                                                    int64_t rows_pad, int dp, int64_t rows,
-                                                    int dim, float scale, E* __restrict__ out,
-                                                    bool out_vec,
-                                                    const float* __restrict__ bias_part,
-                                                    float* __restrict__ bias_out) {
-    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / LANES;
+__device__ __forceinline__ void join_slots(const JoinArgs& a, int64_t block, int dp, int dim,
+                                           float scale) {
+    const int64_t i = (block * kBlock + threadIdx.x) / LANES;
     const int lane = threadIdx.x % LANES;
     const int q = dim / 4;
-    if (out != nullptr && i < rows * q) {
+    if (a.out != nullptr && i < a.rows * q) {
         const int64_t row = i / q;
         const int col = (int)(i % q) * 4;
         float4 v = zero4();
 #pragma unroll 4
-        for (int s = lane; s < splits; s += LANES)
-            v = add4(v, *reinterpret_cast<const float4*>(part + (s * rows_pad + row) * dp + col));
+        for (int s = lane; s < a.slots; s += LANES)
+            v = add4(v, *reinterpret_cast<const float4*>(a.part + (s * a.part_rows + row) * dp +
+                                                         col));
         v = make_float4(group_sum<LANES>(v.x), group_sum<LANES>(v.y), group_sum<LANES>(v.z),
                         group_sum<LANES>(v.w));
-        if (lane == 0) store_out(out + row * dim + col, v, scale, out_vec);
+        if (lane == 0) store_out(static_cast<E*>(a.out) + row * dim + col, v, scale, a.vec);
     }
-    if (bias_out != nullptr && i < rows) {
+    if (a.bias_out != nullptr && i < a.rows) {
         float v = 0.f;
 #pragma unroll 4
-        for (int s = lane; s < splits; s += LANES) v += bias_part[s * rows_pad + i];
+        for (int s = lane; s < a.slots; s += LANES) v += a.bias_part[s * a.part_rows + i];
         v = group_sum<LANES>(v);
-        if (lane == 0) bias_out[i] = v * scale;
+        if (lane == 0) a.bias_out[i] = v * scale;
     }
+}
+
+// One or two sets of partial results.
+template <typename E>
+__global__ __launch_bounds__(kBlock) void k_sm_join(JoinArgs a, JoinArgs b, int dp, int dim,
+                                                    float scale) {
+    const bool second = blockIdx.x >= a.blocks;
+    const JoinArgs& k = second ? b : a;
+    const int64_t block = second ? blockIdx.x - a.blocks : blockIdx.x;
+    if (k.lanes == 16) join_slots<E, 16>(k, block, dp, dim, scale);
+    else join_slots<E, 1>(k, block, dp, dim, scale);
 }
 
 // ---------------------------------------------------------------------------
@@ -1134,6 +1165,16 @@ struct Shape {
     static constexpr bool kStaged = ND <= kMostStaged;
 };
 
+// Rows that do not go through LDS: waves that wait for each other's loads less.
+template <typename E, int ND, bool GRAD, bool STAGED>
+constexpr int pass_occ() {
+    return STAGED ? Shape<E, ND, GRAD>::kOcc : ND > 8 ? 1 : 2;
+}
+template <typename E, int ND, bool GRAD, bool STAGED>
+constexpr int pass_waves() {
+    return STAGED ? Shape<E, ND, GRAD>::kWaves : 4 * pass_occ<E, ND, GRAD, STAGED>();
+}
+
 // Blocks of 32 columns that the kernels are made for.
 inline int made_for(int nd) {
     for (int k : {1, 2, 3, 4, 6, 8, 10, 12, 16})
@@ -1154,12 +1195,12 @@ constexpr int64_t kCus = 256;
 // Workgroups along X and splits of Y.  With x_blocks above the card's places
 // (`resident` workgroups of a CU), whole rounds of them take all of Y (where
 // `whole` allows it) and what is left over is split; else all are.  A split has at
-// least four tiles a wave; there are at most kSmPartRows partial rows (or one
+// least `least` tiles a wave; there are at most kSmPartRows partial rows (or one
 // slot's).  Of the numbers of splits, the fewest that come within 3% of the
 // shortest: r workgroups of 1 / s each take ceil(r s / places) / s, and a start that
 // costs about as much as four tiles.
 Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident, int rec_bytes,
-               bool staged, bool whole) {
+               bool staged, bool whole, int least) {
     Layout l{};
     const int64_t groups = div_up(x_tiles, xb);
     int64_t stage = staged ? kSmLds / 2 / resident / rec_bytes : waves;
@@ -1177,7 +1218,7 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
     l.part_rows = x_tiles * 32 - l.part_first;
     int64_t want = 1;
     if (left > 0) {
-        int64_t most = y_tiles / (4 * yw);
+        int64_t most = y_tiles / (least * yw);
         const int64_t room = kSmPartRows / (l.part_rows * yw);
         if (most > room) most = room;
         double best = 1e30;
@@ -1219,49 +1260,81 @@ Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident
         if (e_ != hipSuccess) return e_;    \
     } while (0)
 
-template <auto* KERNEL>
-hipError_t launch_pass(const PassArgs& a, int waves, int chunks, int lds, hipStream_t s) {
-    if (lds > 64 * 1024) SM_TRY(allow_lds<KERNEL>(kSmLds));
-    const dim3 grid((uint32_t)place_grid(a.x_blocks, a.x_whole, a.splits), (uint32_t)chunks);
-    KERNEL<<<grid, waves * 64, lds, s>>>(a);
-    return hipGetLastError();
-}
-
-// Fills in the layout and launches the pass; `fit` sets the outputs from it.
-template <typename E, int ND, bool GRAD, bool STAGED, bool ROWS, bool DIRECT, typename Fit>
-hipError_t run_pass(const SoftmaxPlan& p, PassArgs a, Fit fit, hipStream_t s) {
-    constexpr int kXB = STAGED ? Shape<E, ND, GRAD>::kXB : 1;
-    constexpr int kOcc = STAGED ? Shape<E, ND, GRAD>::kOcc : ND > 8 ? 1 : 2;
-    constexpr int kWaves = STAGED ? Shape<E, ND, GRAD>::kWaves : 4 * kOcc;
+// Fills in the layout of a pass.
+template <typename E, int ND, bool GRAD, bool STAGED, bool DIRECT>
+Layout fit_pass(const SoftmaxPlan& p, bool rows, PassArgs& a) {
+    using S = Shape<E, ND, GRAD>;
     const int rec = DIRECT ? 2 * ND * 1024 : record_bytes(p.dp / 16, p.parts, a.forms);
-    // all pieces are laid out as the first, whose partial results they add to
-    const Layout l = lay_out(a.x_tiles, ROWS ? p.piece / kSmTile : a.y_tiles, kXB, kWaves,
-                             kOcc * 4 / kWaves, rec, STAGED, GRAD && (!ROWS || p.piece >= p.classes));
+    const int occ = pass_occ<E, ND, GRAD, STAGED>(), waves = pass_waves<E, ND, GRAD, STAGED>();
+    // all pieces of the classes are laid out as the first, whose partial results they
+    // add to
+    const Layout l =
+        lay_out(a.x_tiles, rows ? p.piece / kSmTile : a.y_tiles, STAGED ? S::kXB : 1, waves,
+                occ * 4 / waves, rec, STAGED, GRAD && (!rows || p.piece >= p.classes),
+                GRAD ? 8 : 4);
     a.x_groups = l.x_groups, a.stage = l.stage, a.x_blocks = (int32_t)l.x_blocks;
     a.x_whole = (int32_t)l.x_whole, a.splits = (int32_t)l.splits, a.per = l.per;
     a.part_first = l.part_first, a.part_rows = l.part_rows;
     a.nfrag = p.dp / 16, a.kd = p.kd, a.dp = p.dp, a.dim = p.dim;
-    fit(a, l);
-    const int lds = STAGED ? 2 * l.stage * rec : 0;
-    if constexpr (GRAD)
-        return launch_pass<&k_sm_grad<E, ND, kXB, kWaves, kOcc, STAGED, ROWS>>(a, kWaves, p.chunks, lds,
-                                                                        s);
-    else
-        return launch_pass<&k_sm_lse<E, ND, kXB, kWaves, kOcc, STAGED, DIRECT>>(a, kWaves, 1, lds,
-                                                                               s);
+    a.lds = STAGED ? 2 * l.stage * rec : 0;
+    a.grid = place_grid(l.x_blocks, l.x_whole, l.splits);
+    return l;
 }
 
-template <typename E, bool GRAD, bool ROWS, typename Fit>
-hipError_t pass(const SoftmaxPlan& p, const PassArgs& a, Fit fit, hipStream_t s) {
+template <typename E, int ND, bool STAGED, bool DIRECT>
+hipError_t lse_pass(const SoftmaxPlan& p, PassArgs a, bool rows, int64_t* slots, hipStream_t s) {
+    constexpr int kXB = STAGED ? Shape<E, ND, false>::kXB : 1;
+    constexpr int kOcc = pass_occ<E, ND, false, STAGED>();
+    constexpr int kWaves = pass_waves<E, ND, false, STAGED>();
+    constexpr auto* kKernel = &k_sm_lse<E, ND, kXB, kWaves, kOcc, STAGED, DIRECT>;
+    *slots = fit_pass<E, ND, false, STAGED, DIRECT>(p, rows, a).slots;
+    if (a.lds > 64 * 1024) SM_TRY(allow_lds<kKernel>(kSmLds));
+    kKernel<<<dim3((uint32_t)a.grid), kWaves * 64, a.lds, s>>>(a);
+    return hipGetLastError();
+}
+
+// The pass of the loss.  rows: the classes come in pieces; else all at once.
+template <typename E>
+hipError_t lse_pass(const SoftmaxPlan& p, const PassArgs& a, bool rows, int64_t* slots,
+                    hipStream_t s) {
     HUGE_SM_ND(p.nd, {
-        if constexpr (!GRAD && sizeof(E) == 2)
-            if (a.y_rows != nullptr)
-                return run_pass<E, ND, GRAD, true, ROWS, true>(p, a, fit, s);
-        if constexpr (Shape<E, ND, GRAD>::kStaged)
-            if (p.chunks == 1) return run_pass<E, ND, GRAD, true, ROWS, false>(p, a, fit, s);
-        // wider rows: at least half of the largest ND in each of two chunks or more
-        if constexpr (GRAD ? ND >= 6 && Shape<E, ND, GRAD>::kStaged : ND == 8)
-            return run_pass<E, ND, GRAD, false, ROWS, false>(p, a, fit, s);
+        if constexpr (sizeof(E) == 2)
+            if (a.y_rows != nullptr) return lse_pass<E, ND, true, true>(p, a, rows, slots, s);
+        if (p.chunks == 1) return lse_pass<E, ND, true, false>(p, a, rows, slots, s);
+        if constexpr (ND == 8) return lse_pass<E, ND, false, false>(p, a, rows, slots, s);
+    })
+    return hipErrorInvalidValue;
+}
+
+template <typename E, int ND, bool STAGED, typename Fit>
+hipError_t grad_pass(const SoftmaxPlan& p, PassArgs classes, PassArgs rows, Fit fit,
+                     hipStream_t s) {
+    constexpr int kXB = STAGED ? Shape<E, ND, true>::kXB : 1;
+    constexpr int kOcc = pass_occ<E, ND, true, STAGED>();
+    constexpr int kWaves = pass_waves<E, ND, true, STAGED>();
+    constexpr auto* kKernel = &k_sm_grad<E, ND, kXB, kWaves, kOcc, STAGED>;
+    Layout lc{}, lr{};
+    if (classes.x != nullptr) lc = fit_pass<E, ND, true, STAGED, false>(p, false, classes);
+    if (rows.x != nullptr) lr = fit_pass<E, ND, true, STAGED, false>(p, true, rows);
+    fit(classes, lc, rows, lr);
+    const int lds = classes.lds > rows.lds ? classes.lds : rows.lds;
+    if (lds > 64 * 1024) SM_TRY(allow_lds<kKernel>(kSmLds));
+    const dim3 grid((uint32_t)(classes.grid + rows.grid), (uint32_t)p.chunks);
+    kKernel<<<grid, kWaves * 64, lds, s>>>(classes, rows, (int32_t)classes.grid);
+    return hipGetLastError();
+}
+
+// The passes of the gradients; one whose x is null is left out.  fit sets the places
+// of the partial results from the layouts.
+template <typename E, typename Fit>
+hipError_t grad_pass(const SoftmaxPlan& p, const PassArgs& classes, const PassArgs& rows, Fit fit,
+                     hipStream_t s) {
+    HUGE_SM_ND(p.nd, {
+        if constexpr (Shape<E, ND, true>::kStaged) {
+            if (p.chunks == 1) return grad_pass<E, ND, true>(p, classes, rows, fit, s);
+            // wider rows: at least half of the largest ND in each of two chunks or more
+            if constexpr (ND >= 6) return grad_pass<E, ND, false>(p, classes, rows, fit, s);
+        }
     })
     return hipErrorInvalidValue;
 }
@@ -1340,7 +1413,7 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
         l.x = a.ws + p.h, l.forms = 1, l.first = true, l.lse_part = part;
         l.y_rows = static_cast<const bf16_t*>(a.w), l.ld = a.ld_w, l.classes = a.classes;
         l.x_tiles = p.rows_pad / kSmTile, l.y_tiles = div_up(a.classes, kSmTile);
-        SM_TRY((pass<E, false, false>(p, l, [&](PassArgs&, const Layout& o) { slots = o.slots; }, s)));
+        SM_TRY(lse_pass<E>(p, l, false, &slots, s));
     }
     for (int64_t c0 = 0; few == 0 && !direct && c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
@@ -1349,7 +1422,7 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
         l.x = a.ws + p.h, l.y = a.ws + p.w, l.forms = 1;
         l.x_tiles = p.rows_pad / kSmTile, l.y_tiles = div_up(count, kSmTile);
         l.first = c0 == 0, l.lse_part = part;
-        SM_TRY((pass<E, false, true>(p, l, [&](PassArgs&, const Layout& o) { slots = o.slots; }, s)));
+        SM_TRY(lse_pass<E>(p, l, true, &slots, s));
     }
     if (a.n < 4096)
         k_sm_loss<E, 64><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, pad);
@@ -1363,25 +1436,30 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
     return hipSuccess;
 }
 
-// Joins the partial results of the rows from lay.part_first on, of `rows`.
+// The partial results of the rows from lay.part_first on, of `rows`.
 template <typename E>
-hipError_t join(const SoftmaxPlan& p, const float* part, const Layout& lay, int64_t rows,
-                float scale, void* out, const float* bias_part, float* bias_out, hipStream_t s) {
-    rows -= lay.part_first;
-    if (rows <= 0) return hipSuccess;
-    const int64_t work = out != nullptr ? rows * (p.dim / 4) : rows;
-    E* o = out == nullptr ? nullptr : static_cast<E*>(out) + lay.part_first * p.dim;
-    if (bias_out != nullptr) bias_out += lay.part_first;
-    const bool vec = fours(o, 0, sizeof(E));
-    // few outputs of many splits: 16 threads each
-    if (work < (1 << 18) && lay.slots >= 16)
-        k_sm_join<E, 16><<<dim3((uint32_t)div_up(work * 16, kBlock)), kBlock, 0, s>>>(
-            part, (int)lay.slots, lay.part_rows, p.dp, rows, p.dim, scale, o, vec, bias_part,
-            bias_out);
-    else
-        k_sm_join<E, 1><<<dim3((uint32_t)div_up(work, kBlock)), kBlock, 0, s>>>(
-            part, (int)lay.slots, lay.part_rows, p.dp, rows, p.dim, scale, o, vec, bias_part,
-            bias_out);
+JoinArgs to_join(const SoftmaxPlan& p, const float* part, const Layout& lay, int64_t rows,
+                 void* out, const float* bias_part, float* bias_out) {
+    JoinArgs j{};
+    j.rows = rows - lay.part_first;
+    if (j.rows <= 0) return JoinArgs{};
+    j.part = part, j.bias_part = bias_part, j.part_rows = lay.part_rows;
+    j.out = out == nullptr ? nullptr : static_cast<E*>(out) + lay.part_first * p.dim;
+    j.bias_out = bias_out == nullptr ? nullptr : bias_out + lay.part_first;
+    j.vec = fours(j.out, 0, sizeof(E));
+    j.slots = (int32_t)lay.slots;
+    const int64_t work = out != nullptr ? j.rows * (p.dim / 4) : j.rows;
+    // few outputs of many slots: 16 threads each
+    j.lanes = work < (1 << 18) && lay.slots >= 16 ? 16 : 1;
+    j.blocks = div_up(work * j.lanes, kBlock);
+    return j;
+}
+
+template <typename E>
+hipError_t join(const SoftmaxPlan& p, const JoinArgs& a, const JoinArgs& b, float scale,
+                hipStream_t s) {
+    if (a.blocks + b.blocks == 0) return hipSuccess;
+    k_sm_join<E><<<dim3((uint32_t)(a.blocks + b.blocks)), kBlock, 0, s>>>(a, b, p.dp, p.dim, scale);
     return hipGetLastError();
 }
 
@@ -1391,49 +1469,44 @@ hipError_t softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
     const int64_t x_tiles = p.rows_pad / kSmTile;
     float* class_part = reinterpret_cast<float*>(a.ws + p.part);
     float* row_part = reinterpret_cast<float*>(a.ws + p.row_part);
-    Layout row_lay{};
-    bool row_parts = false;
+    JoinArgs row_join{};
     for (int64_t c0 = 0; c0 < a.classes; c0 += p.piece) {
         const int64_t count = a.classes - c0 < p.piece ? a.classes - c0 : p.piece;
         const int64_t w_tiles = div_up(count, kSmTile);
         SM_TRY(pack<E>(p, a, c0, count, 2, s));
-        PassArgs g{};
-        g.class0 = c0, g.scale = a.scale, g.forms = 2;
+        PassArgs c{}, r{};
+        c.class0 = r.class0 = c0, c.scale = r.scale = a.scale, c.forms = r.forms = 2;
         if (a.dw != nullptr || a.dbias != nullptr) {
             // the second product is formed also where only the bias is wanted
-            E* out = a.dw == nullptr ? nullptr : static_cast<E*>(a.dw) + c0 * p.dim;
-            float* bias_out = a.dbias == nullptr ? nullptr : a.dbias + c0;
-            g.x = a.ws + p.w, g.y = a.ws + p.h, g.x_tiles = w_tiles, g.y_tiles = x_tiles;
-            g.x_rows = count, g.first = true, g.out = out, g.bias_out = bias_out;
-            g.out_vec = fours(out, 0, sizeof(E));
-            g.want_bias = bias_out != nullptr;
-            Layout lay{};
-            float* bias_part = nullptr;
-            SM_TRY((pass<E, true, false>(p, g, [&](PassArgs& q, const Layout& o) {
-                lay = o;
-                if (o.slots <= 1) return;
-                q.part = class_part;
-                bias_part = class_part + o.slots * o.part_rows * p.dp;
-                q.bias_part = bias_part;
-            }, s)));
-            if (lay.slots > 1)
-                SM_TRY(join<E>(p, class_part, lay, count, a.scale, out, bias_part, bias_out, s));
+            c.x = a.ws + p.w, c.y = a.ws + p.h, c.x_tiles = w_tiles, c.y_tiles = x_tiles;
+            c.x_rows = count, c.first = true, c.want_bias = a.dbias != nullptr;
+            c.out = a.dw == nullptr ? nullptr : static_cast<E*>(a.dw) + c0 * p.dim;
+            c.bias_out = a.dbias == nullptr ? nullptr : a.dbias + c0;
+            c.out_vec = fours(c.out, 0, sizeof(E));
         }
         if (a.dh != nullptr) {
-            g.x = a.ws + p.h, g.y = a.ws + p.w, g.x_tiles = x_tiles, g.y_tiles = w_tiles;
-            g.x_rows = a.n, g.first = c0 == 0, g.out = a.dh, g.bias_out = nullptr;
-            g.out_vec = fours(a.dh, 0, sizeof(E));
-            g.want_bias = false;
-            SM_TRY((pass<E, true, true>(p, g, [&](PassArgs& q, const Layout& o) {
-                row_lay = o;
-                // sums that stay from piece to piece
-                row_parts = o.slots > 1 || p.piece < a.classes;
-                if (row_parts) q.part = row_part;
-            }, s)));
+            r.x = a.ws + p.h, r.y = a.ws + p.w, r.x_tiles = x_tiles, r.y_tiles = w_tiles;
+            r.x_rows = a.n, r.first = c0 == 0, r.out = a.dh, r.out_vec = fours(a.dh, 0, sizeof(E));
         }
+        JoinArgs class_join{};
+        SM_TRY(grad_pass<E>(
+            p, c, r,
+            [&](PassArgs& q, const Layout& lc, PassArgs& t, const Layout& lr) {
+                if (lc.slots > 1) {
+                    q.part = class_part;
+                    q.bias_part = class_part + lc.slots * lc.part_rows * p.dp;
+                    class_join = to_join<E>(p, q.part, lc, count, q.out, q.bias_part, q.bias_out);
+                }
+                // the rows' sums stay from piece to piece
+                if (lr.slots > 1 || (t.x != nullptr && p.piece < a.classes)) {
+                    t.part = row_part;
+                    row_join = to_join<E>(p, row_part, lr, a.n, a.dh, nullptr, nullptr);
+                }
+            },
+            s));
+        const bool last = c0 + p.piece >= a.classes;
+        SM_TRY(join<E>(p, class_join, last ? row_join : JoinArgs{}, a.scale, s));
     }
-    if (row_parts)
-        SM_TRY(join<E>(p, row_part, row_lay, a.n, a.scale, a.dh, nullptr, nullptr, s));
     return hipSuccess;
 }
 
@@ -1479,6 +1552,7 @@ hipError_t launch_softmax_loss(const SoftmaxArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_softmax_grad(const SoftmaxArgs& a, hipStream_t s) {
+    if (a.dh == nullptr && a.dw == nullptr && a.dbias == nullptr) return hipSuccess;
     return a.dtype == kDtypeBf16 ? softmax_grad<bf16_t>(a, s) : softmax_grad<float>(a, s);
 }
 
