@@ -914,7 +914,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
         xl[b] = (int32_t)(ROWS ? (label < 0 ? -1 : label - a.class0)
                                : a.class0 + xt.t[b] * 32 + r);
         bias[b] = 0.f;
-        pscale[b] = 0x1p100f;
+        pscale[b] = 0.f;  // until an element is not 0
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[b][d] = f32x16{};
     }
@@ -1015,12 +1015,17 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
                     }
                     // the halves share the sums of a row: they share its scale
                     big = fmaxf(big, __shfl_xor(big, 32));
-                    if (__ballot(big * pscale[b] > 0x1p15f) != 0) {
-                        float s = pscale[b];
-                        if (big * s > 0x1p15f)
-                            s = fminf(s, ldexpf(1.f, 15 - __builtin_amdgcn_frexp_expf(big)));
-                        const float ratio = s / pscale[b];
-                        pscale[b] = s;
+                    const bool scale_anew = big * pscale[b] > 0x1p15f ||
+                                            (pscale[b] == 0.f && big > 0.f);
+                    if (__ballot(scale_anew) != 0) {
+                        // big is below 2^e: the largest element is brought below 2^15
+                        float ratio = 1.f;
+                        if (scale_anew) {
+                            const int e = __builtin_amdgcn_frexp_expf(big);
+                            const float s = ldexpf(1.f, e < -105 ? 120 : 15 - e);
+                            ratio = pscale[b] > 0.f ? fminf(s / pscale[b], 1.f) : 0.f;
+                            pscale[b] = pscale[b] > 0.f ? fminf(s, pscale[b]) : s;
+                        }
 #pragma unroll
                         for (int d = 0; d < ND; ++d) acc[b][d] *= ratio;
                     }
@@ -1049,7 +1054,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
         const int64_t xi = xt.t[b] * 32 + (lane & 31);
         const int64_t row = ((int64_t)at.split * yw + yg) * a.part_rows + xi - a.part_first;
         const bool direct = at.whole || a.part == nullptr;
-        const float back = kScaled ? 1.f / pscale[b] : 1.f;
+        const float back = kScaled && pscale[b] > 0.f ? 1.f / pscale[b] : kScaled ? 0.f : 1.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll

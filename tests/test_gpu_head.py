@@ -476,6 +476,56 @@ def test_softmax_on_another_stream_and_in_a_graph():
         torch.randn(100, 100, device="cuda").sum().item()
 
 
+@pytest.mark.parametrize("dtype,classes", [("f32", 300_001), ("bf16", 560_003)])
+def test_softmax_table_in_pieces(dtype, classes):
+    """A table whose packed rows exceed what is packed at once: labels, sums and partial
+    results across the pieces."""
+    n, dim = 90, 1024
+    say(f"softmax {n} x {classes} x {dim} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(7)
+    new = lambda *s: torch.randn(s, device="cuda", generator=g)  # noqa: E731
+    h = new(n, dim).to(TYPES[dtype])
+    w = (new(classes, dim) * 1.5 / math.sqrt(dim)).to(TYPES[dtype])
+    labels = torch.randint(-1, classes, (n,), device="cuda", generator=g).to(torch.int32)
+    labels[:4] = torch.tensor([0, classes - 1, classes // 2, 262_144], dtype=torch.int32)
+    bias, c = new(classes), torch.rand(n, device="cuda", generator=g) + 0.5
+    op = P.SoftmaxLoss(n, classes, dim, dtype=dtype)
+    loss, lse = op.loss(h, w, labels, bias, c)
+    got = (loss, lse, *op.grad(h, w, labels, lse, bias, c, scale=1.0))
+    for name, x, y in zip(("loss", "lse", "dh", "dw", "db"), got,
+                          softmax_on_device(h, w, labels, bias, c, 1.0)):
+        tol = 2.0 ** -8 if dtype == "bf16" and name in ("dh", "dw") else 2e-6
+        err = ((x.double() - y).norm() / y.norm()).item()
+        say(f"  {name}: {err:.3g} of the norm")
+        assert err <= tol, name
+    op.check()
+
+
+@pytest.mark.parametrize("hs,ws", [(1e15, 1e-15), (1e-18, 1e18), (1e-30, 1e29), (1e35, 1e-36)])
+def test_softmax_fp32_scales(hs, ws):
+    """Rows of very large and very small values whose products are ordinary, and
+    rows in which few elements are much larger than the others."""
+    rng = np.random.default_rng(18)
+    n, classes, dim = 80, 150, 64
+    k = softmax_case(n, classes, dim, "f32", rng, unlabelled=0.0)
+    h = k["hv"] * np.where(rng.random((n, dim)) < 0.05, 30.0, 0.1)
+    w = k["wv"] * np.where(rng.random((classes, dim)) < 0.05, 3.0, 1.0)
+    k["h"], k["hv"] = rows(h * hs, "f32")
+    k["w"], k["wv"] = rows(w * ws, "f32")
+    op = P.SoftmaxLoss(n, classes, dim)
+    loss, lse = op.loss(k["h"], k["w"], k["tl"], k["tb"], k["tc"])
+    dh, dw, db = op.grad(k["h"], k["w"], k["tl"], lse, k["tb"], k["tc"], scale=0.5)
+    want, wlse, _ = ref.softmax_loss(k["hv"], k["wv"], k["labels"], k["b"], k["c"])
+    (wh, ww, wb), _ = ref.softmax_grad(k["hv"], k["wv"], k["labels"], k["b"], k["c"], 0.5)
+    # an element keeps 22 bits, or 2^-40 of its row's largest: logits of at most a few
+    # tens are within 1e-5
+    for name, x, y in (("loss", loss, want), ("lse", lse, wlse), ("dh", dh, wh), ("dw", dw, ww),
+                       ("db", db, wb)):
+        d = np.linalg.norm(x.double().cpu().numpy() / np.abs(y).max() - y / np.abs(y).max())
+        say(f"  {name}: {d / np.linalg.norm(y / np.abs(y).max()):.3g} of the norm")
+        assert d <= 2e-5 * np.linalg.norm(y / np.abs(y).max()), name
+
+
 # --------------------------------------------------------------------------- #
 # AdamW
 # --------------------------------------------------------------------------- #
@@ -670,6 +720,16 @@ def test_head_gradient_of_the_rows():
         lo[at] -= 1e-5
         hi[at] += 1e-5
         assert abs(dx[at].item() - (total(hi) - total(lo)) / 2e-5) < 1e-5
+
+
+@pytest.mark.parametrize("states", ["f32", "q8"])
+def test_example_finds_the_blocks(states):
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                                    "examples"))
+    import classify_blocks
+    assert classify_blocks.main(["--epochs", "2", "--states", states], log=say) > 0.9
 
 
 # --------------------------------------------------------------------------- #
