@@ -1,6 +1,6 @@
 // Layer norm of rows and its backward pass.
 //
-// A group of TPR threads holds a row in registers, NV times VEC elements a
+// A group of TPR threads holds a row in registers, NV times four elements a
 // thread: the mean, then the sum of squares about it, each one reduction over
 // the group, so the variance loses nothing to a large mean and the row is read
 // once.  TPR is the smallest power of two that covers the row at NV = 1, then NV
@@ -16,34 +16,71 @@ namespace huge {
 
 namespace {
 
-template <int VEC>
+// Four elements of a row.
 struct Few {
-    float v[VEC];
+    float v[4];
 };
 
-template <int VEC, typename E>
-__device__ __forceinline__ Few<VEC> load_few(const E* __restrict__ row, int c) {
-    Few<VEC> f;
-    if constexpr (VEC == 4) {
+typedef float raw_f4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t raw_h4 __attribute__((ext_vector_type(4), aligned(2)));
+
+// Chunk c of a row of D elements.  WHOLE: D is a multiple of four and the rows lie
+// on whole chunks.  Otherwise the load needs no more than the element's alignment,
+// and the row's last chunk is read one by one, with zeros past the end.
+template <bool WHOLE, typename E>
+__device__ __forceinline__ Few load_few(const E* __restrict__ row, int c, int D) {
+    Few f{};
+    if constexpr (WHOLE) {
         const float4 q = load_chunk(row, c);
         f.v[0] = q.x, f.v[1] = q.y, f.v[2] = q.z, f.v[3] = q.w;
-    } else if constexpr (sizeof(E) == 4) {
-        f.v[0] = row[c];
+    } else if (4 * c + 4 <= D) {
+        if constexpr (sizeof(E) == 4) {
+            const raw_f4 q = *reinterpret_cast<const raw_f4*>(row + 4 * c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = q[e];
+        } else {
+            const raw_h4 q = *reinterpret_cast<const raw_h4*>(row + 4 * c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = __uint_as_float((uint32_t)q[e] << 16);
+        }
     } else {
-        f.v[0] = __uint_as_float((uint32_t)row[c] << 16);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            if (4 * c + e >= D) continue;
+            if constexpr (sizeof(E) == 4) f.v[e] = row[4 * c + e];
+            else f.v[e] = __uint_as_float((uint32_t)row[4 * c + e] << 16);
+        }
     }
     return f;
 }
 
-template <int VEC, typename E>
-__device__ __forceinline__ void store_few(E* __restrict__ row, int c, const Few<VEC>& f) {
-    if constexpr (VEC == 4) {
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void store_few(E* __restrict__ row, int c, int D, const Few& f) {
+    if constexpr (WHOLE) {
         store_chunk(row, c, make_float4(f.v[0], f.v[1], f.v[2], f.v[3]));
-    } else if constexpr (sizeof(E) == 4) {
-        row[c] = f.v[0];
+    } else if (4 * c + 4 <= D) {
+        if constexpr (sizeof(E) == 4) {
+            *reinterpret_cast<raw_f4*>(row + 4 * c) = raw_f4{f.v[0], f.v[1], f.v[2], f.v[3]};
+        } else {
+            raw_h4 q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[e] = (bf16_t)float_to_bf16_bits(f.v[e]);
+            *reinterpret_cast<raw_h4*>(row + 4 * c) = q;
+        }
     } else {
-        row[c] = (bf16_t)float_to_bf16_bits(f.v[0]);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            if (4 * c + e >= D) continue;
+            if constexpr (sizeof(E) == 4) row[4 * c + e] = f.v[e];
+            else row[4 * c + e] = (bf16_t)float_to_bf16_bits(f.v[e]);
+        }
     }
+}
+
+// Whether element e of chunk c is one of the row's.
+template <bool WHOLE>
+__device__ __forceinline__ bool inside(int c, int e, int D) {
+    return WHOLE ? 4 * c < D : 4 * c + e < D;
 }
 
 // Sum over the TPR threads of a row.  Above a wave the four waves' sums meet in
@@ -61,35 +98,35 @@ __device__ __forceinline__ float row_sum(float v, float* s_sum, int& turn) {
     }
 }
 
-template <typename E, int TPR, int NV, int VEC>
+template <typename E, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a) {
     __shared__ float s_sum[8];
     int turn = 0;
     constexpr int kRows = kBlock / TPR;
-    const int t = threadIdx.x % TPR, D = a.dim, chunks = D / VEC;
+    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + 3) / 4;
     const E* x = static_cast<const E*>(a.x);
     E* y = static_cast<E*>(a.y);
     const float inv = 1.0f / (float)D;
     for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
          r += (int64_t)gridDim.x * kRows) {
-        Few<VEC> f[NV];
+        Few f[NV];
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
-            f[i] = c < chunks ? load_few<VEC>(x + r * a.ld_x, c) : Few<VEC>{};
+            f[i] = c < chunks ? load_few<WHOLE>(x + r * a.ld_x, c, D) : Few{};
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum += f[i].v[e];
+            for (int e = 0; e < 4; ++e) sum += f[i].v[e];
         }
         const float mean = row_sum<TPR>(sum, s_sum, turn) * inv;
         float sq = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const bool in = t + TPR * i < chunks;
+            const int c = t + TPR * i;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
+            for (int e = 0; e < 4; ++e) {
                 f[i].v[e] -= mean;
-                if (in) sq = fmaf(f[i].v[e], f[i].v[e], sq);
+                if (inside<WHOLE>(c, e, D)) sq = fmaf(f[i].v[e], f[i].v[e], sq);
             }
         }
         const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s_sum, turn) * inv + a.eps);
@@ -97,10 +134,10 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a) {
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
             if (c >= chunks) continue;
-            const Few<VEC> g = load_few<VEC>(a.gamma, c), b = load_few<VEC>(a.beta, c);
+            const Few g = load_few<WHOLE>(a.gamma, c, D), b = load_few<WHOLE>(a.beta, c, D);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[i].v[e] = fmaf(f[i].v[e] * rstd, g.v[e], b.v[e]);
-            store_few<VEC>(y + r * a.ld_y, c, f[i]);
+            for (int e = 0; e < 4; ++e) f[i].v[e] = fmaf(f[i].v[e] * rstd, g.v[e], b.v[e]);
+            store_few<WHOLE>(y + r * a.ld_y, c, D, f[i]);
         }
         if (t == 0 && a.mean != nullptr) {
             a.mean[r] = mean;
@@ -109,42 +146,42 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a) {
     }
 }
 
-template <typename E, int TPR, int NV, int VEC>
+template <typename E, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_norm_backward(NormArgs a) {
     __shared__ float s_sum[8];
     int turn = 0;
     constexpr int kRows = kBlock / TPR;
     constexpr int kHeld = TPR < 64 ? TPR : 64;  // lanes of a wave that hold different columns
-    const int t = threadIdx.x % TPR, D = a.dim, chunks = D / VEC;
+    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + 3) / 4;
     const E* x = static_cast<const E*>(a.x);
     const E* dy = static_cast<const E*>(a.dy);
     E* dx = static_cast<E*>(a.y);
     const float inv = 1.0f / (float)D;
-    Few<VEC> g[NV], dg[NV], db[NV];
+    Few g[NV], dg[NV], db[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = t + TPR * i;
-        g[i] = c < chunks ? load_few<VEC>(a.gamma, c) : Few<VEC>{};
-        dg[i] = db[i] = Few<VEC>{};
+        g[i] = c < chunks ? load_few<WHOLE>(a.gamma, c, D) : Few{};
+        dg[i] = db[i] = Few{};
     }
     for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
          r += (int64_t)gridDim.x * kRows) {
         const float mean = a.mean[r], rstd = a.rstd[r];
-        Few<VEC> xh[NV], d[NV];
+        Few xh[NV], d[NV];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
             const bool in = c < chunks;
-            xh[i] = in ? load_few<VEC>(x + r * a.ld_x, c) : Few<VEC>{};
-            d[i] = in ? load_few<VEC>(dy + r * a.ld_dy, c) : Few<VEC>{};
+            xh[i] = in ? load_few<WHOLE>(x + r * a.ld_x, c, D) : Few{};
+            d[i] = in ? load_few<WHOLE>(dy + r * a.ld_dy, c, D) : Few{};
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const bool in = t + TPR * i < chunks;
+            const int c = t + TPR * i;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                xh[i].v[e] = in ? (xh[i].v[e] - mean) * rstd : 0.f;
+            for (int e = 0; e < 4; ++e) {
+                xh[i].v[e] = inside<WHOLE>(c, e, D) ? (xh[i].v[e] - mean) * rstd : 0.f;
                 dg[i].v[e] = fmaf(d[i].v[e], xh[i].v[e], dg[i].v[e]);
                 db[i].v[e] += d[i].v[e];
                 d[i].v[e] *= g[i].v[e];
@@ -160,33 +197,33 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(NormArgs a) {
             const int c = t + TPR * i;
             if (c >= chunks) continue;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
+            for (int e = 0; e < 4; ++e)
                 d[i].v[e] = rstd * (d[i].v[e] - s1 - xh[i].v[e] * s2);
-            store_few<VEC>(dx + r * a.ld_y, c, d[i]);
+            store_few<WHOLE>(dx + r * a.ld_y, c, D, d[i]);
         }
     }
     if (a.partial == nullptr) return;
     // the groups of a wave, then the waves
-    __shared__ float s_part[TPR <= 64 ? 4 * kHeld * NV * VEC : 1];
+    __shared__ float s_part[TPR <= 64 ? 4 * kHeld * NV * 4 : 1];
     float* out = a.partial + (int64_t)blockIdx.x * 2 * D;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        Few<VEC>* p = which == 0 ? dg : db;
+        Few* p = which == 0 ? dg : db;
         if constexpr (TPR <= 64) {
             const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
+                for (int e = 0; e < 4; ++e) {
                     float v = p[i].v[e];
 #pragma unroll
                     for (int off = TPR; off < 64; off <<= 1) v += __shfl_xor(v, off);
-                    if (lane < kHeld) s_part[((wave * NV + i) * VEC + e) * kHeld + lane] = v;
+                    if (lane < kHeld) s_part[((wave * NV + i) * 4 + e) * kHeld + lane] = v;
                 }
             __syncthreads();
             for (int j = threadIdx.x; j < D; j += kBlock) {
-                const int c = j / VEC, at = ((c / TPR) * VEC + j % VEC) * kHeld + c % TPR;
-                constexpr int kWave = NV * VEC * kHeld;
+                const int c = j / 4, at = ((c / TPR) * 4 + j % 4) * kHeld + c % TPR;
+                constexpr int kWave = NV * 4 * kHeld;
                 out[(int64_t)which * D + j] = (s_part[at] + s_part[kWave + at]) +
                                               (s_part[2 * kWave + at] + s_part[3 * kWave + at]);
             }
@@ -197,7 +234,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(NormArgs a) {
                 const int c = t + TPR * i;
                 if (c >= chunks) continue;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) out[(int64_t)which * D + c * VEC + e] = p[i].v[e];
+                for (int e = 0; e < 4; ++e)
+                    if (inside<WHOLE>(c, e, D)) out[(int64_t)which * D + c * 4 + e] = p[i].v[e];
             }
         }
     }
@@ -230,57 +268,43 @@ struct NormShape {
     int tpr, nv;
 };
 
-// Threads of a row and vectors a thread, of `units` vectors (or elements).
-inline NormShape norm_shape(int units, bool vec) {
-    const int one = vec ? 8 : 64;  // fewest threads of a row
-    int tpr = one;
-    while (tpr < 64 && tpr < units) tpr <<= 1;
-    int nv = 1;
-    const int most = vec ? 8 : 32;
-    while (tpr * nv < units && nv < most) nv <<= 1;
-    return tpr * nv < units ? NormShape{kBlock, most} : NormShape{tpr, nv};
+// Threads of a row and chunks a thread, of `chunks` chunks.
+inline NormShape norm_shape(int chunks) {
+    int tpr = 8, nv = 1;
+    while (tpr < 64 && tpr < chunks) tpr <<= 1;
+    while (tpr * nv < chunks && nv < 8) nv <<= 1;
+    return tpr * nv < chunks ? NormShape{kBlock, 8} : NormShape{tpr, nv};
 }
 
-template <typename E, int TPR, int NV, int VEC>
+template <typename E, int TPR, int NV, bool WHOLE>
 void norm_one(const NormArgs& a, bool backward, hipStream_t s) {
     const int64_t rows = kBlock / TPR, need = (a.n + rows - 1) / rows;
     if (!backward) {
         const int64_t grid = need < 65536 ? need : 65536;
-        k_norm<E, TPR, NV, VEC><<<dim3((uint32_t)grid), kBlock, 0, s>>>(a);
+        k_norm<E, TPR, NV, WHOLE><<<dim3((uint32_t)grid), kBlock, 0, s>>>(a);
     } else {
-        k_norm_backward<E, TPR, NV, VEC>
+        k_norm_backward<E, TPR, NV, WHOLE>
             <<<dim3((uint32_t)norm_blocks(a.n, a.dim)), kBlock, 0, s>>>(a);
     }
 }
 
 template <typename E>
 hipError_t norm_dispatch(const NormArgs& a, bool backward, hipStream_t s) {
-    const NormShape p = norm_shape(a.vec ? a.dim / 4 : a.dim, a.vec);
-#define HUGE_NORM_CASE(T, N, V) \
-    case (T) * 64 + (N):        \
-        norm_one<E, T, N, V>(a, backward, s); \
+    const NormShape p = norm_shape((a.dim + 3) / 4);
+#define HUGE_NORM_CASE(T, N)                           \
+    case (T) * 64 + (N):                               \
+        if (a.vec) norm_one<E, T, N, true>(a, backward, s); \
+        else norm_one<E, T, N, false>(a, backward, s); \
         return hipGetLastError();
-    if (a.vec) {
-        switch (p.tpr * 64 + p.nv) {
-            HUGE_NORM_CASE(8, 1, 4)
-            HUGE_NORM_CASE(16, 1, 4)
-            HUGE_NORM_CASE(32, 1, 4)
-            HUGE_NORM_CASE(64, 1, 4)
-            HUGE_NORM_CASE(64, 2, 4)
-            HUGE_NORM_CASE(64, 4, 4)
-            HUGE_NORM_CASE(64, 8, 4)
-            HUGE_NORM_CASE(256, 8, 4)
-        }
-    } else {
-        switch (p.tpr * 64 + p.nv) {
-            HUGE_NORM_CASE(64, 1, 1)
-            HUGE_NORM_CASE(64, 2, 1)
-            HUGE_NORM_CASE(64, 4, 1)
-            HUGE_NORM_CASE(64, 8, 1)
-            HUGE_NORM_CASE(64, 16, 1)
-            HUGE_NORM_CASE(64, 32, 1)
-            HUGE_NORM_CASE(256, 32, 1)
-        }
+    switch (p.tpr * 64 + p.nv) {
+        HUGE_NORM_CASE(8, 1)
+        HUGE_NORM_CASE(16, 1)
+        HUGE_NORM_CASE(32, 1)
+        HUGE_NORM_CASE(64, 1)
+        HUGE_NORM_CASE(64, 2)
+        HUGE_NORM_CASE(64, 4)
+        HUGE_NORM_CASE(64, 8)
+        HUGE_NORM_CASE(256, 8)
     }
 #undef HUGE_NORM_CASE
     return hipErrorInvalidValue;
