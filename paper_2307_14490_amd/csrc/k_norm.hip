@@ -4,7 +4,7 @@
 // thread: the mean, then the sum of squares about it, each one reduction over
 // the group, so the variance loses nothing to a large mean and the row is read
 // once.  TPR is the smallest power of two that covers the row at NV = 1, then NV
-// grows; rows above 2048 elements take a whole workgroup.  The weight gradients
+// grows; rows above 1024 elements take a whole workgroup.  The weight gradients
 // are sums over all rows: a group adds its rows' terms in registers, a workgroup
 // its groups', and a second kernel the workgroups' rows of `partial`, always in
 // the same order.  Both kernels are bound by memory: a row is moved once in each
@@ -272,8 +272,10 @@ struct NormShape {
 inline NormShape norm_shape(int chunks) {
     int tpr = 8, nv = 1;
     while (tpr < 64 && tpr < chunks) tpr <<= 1;
-    while (tpr * nv < chunks && nv < 8) nv <<= 1;
-    return tpr * nv < chunks ? NormShape{kBlock, 8} : NormShape{tpr, nv};
+    while (tpr * nv < chunks && nv < 4) nv <<= 1;
+    if (tpr * nv >= chunks) return {tpr, nv};
+    for (nv = 2; kBlock * nv < chunks; nv <<= 1) {}
+    return {kBlock, nv};
 }
 
 template <typename E, int TPR, int NV, bool WHOLE>
@@ -303,7 +305,8 @@ hipError_t norm_dispatch(const NormArgs& a, bool backward, hipStream_t s) {
         HUGE_NORM_CASE(64, 1)
         HUGE_NORM_CASE(64, 2)
         HUGE_NORM_CASE(64, 4)
-        HUGE_NORM_CASE(64, 8)
+        HUGE_NORM_CASE(256, 2)
+        HUGE_NORM_CASE(256, 4)
         HUGE_NORM_CASE(256, 8)
     }
 #undef HUGE_NORM_CASE
@@ -315,7 +318,7 @@ hipError_t norm_dispatch(const NormArgs& a, bool backward, hipStream_t s) {
 // A workgroup sums at least 16 rows a group, so that small calls have few rows of
 // partial sums.
 int norm_blocks(int64_t n, int32_t dim) {
-    const int64_t rows = dim > 2048 ? 1 : 4;
+    const int64_t rows = dim > 1024 ? 1 : 4;
     const int64_t b = (n + 16 * rows - 1) / (16 * rows);
     return (int)(b < kNormBlocks ? b : kNormBlocks);
 }
