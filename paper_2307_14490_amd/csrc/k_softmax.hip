@@ -1027,7 +1027,14 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
                             pscale[b] = pscale[b] > 0.f ? fminf(s, pscale[b]) : s;
                         }
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) acc[b][d] *= ratio;
+                        for (int d = 0; d < ND; ++d) {
+                            // a wave alone on its SIMD keeps the sums in accumulation
+                            // registers; unless that is said here, the compiler copies
+                            // them for this product in every tile
+                            if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
+                            acc[b][d] *= ratio;
+                            if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
+                        }
                     }
                     c[b] *= pscale[b];
                 }
