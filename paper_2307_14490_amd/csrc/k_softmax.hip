@@ -426,10 +426,11 @@ __device__ __forceinline__ void stream_records(const PassArgs& a, const Place& a
 
 // Operands of a form that a wave reads ahead of the products that use them.  An LDS
 // read takes as long as two to four products; left alone the compiler reads one or
-// two ahead.
-template <typename E, int N>
+// two ahead.  DEEP: there are registers for twice as many (fp32 gradients of 160 to 256
+// columns, one wave per SIMD: 1074 -> 1048 us for 3001 x 50021 x 256).
+template <typename E, int N, bool DEEP = false>
 struct Ahead {
-    static constexpr int kMost = 4 / Kind<E>::kParts;
+    static constexpr int kMost = (DEEP ? 8 : 4) / Kind<E>::kParts;
     static constexpr int kCount = N < kMost ? N : kMost;
     Operand<E> q[kCount];
 
@@ -467,7 +468,7 @@ __device__ __forceinline__ void tile_products(const uint8_t* rec, const Operand<
     const uint8_t* form = rec + kHeader;
     if constexpr (STAGED) {
         auto load = [&](int k) { return load_operand<E>(form, k, 2 * ND, lane); };
-        Ahead<E, 2 * ND> y;
+        Ahead<E, 2 * ND, Kind<E>::kScaled && (ND > 4)> y;
         y.start(load);
         __builtin_amdgcn_sched_barrier(0);
         y.template run<kProducts<E> * XB>(load, [&](int k, const Operand<E>& q) {
@@ -945,7 +946,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
             auto load = [&](int f) {
                 return load_operand<E>(form, (f / ND) * nd + db0 + f % ND, nfrag, lane);
             };
-            Ahead<E, 2 * ND> y;
+            Ahead<E, 2 * ND, STAGED && kScaled && (ND > 4)> y;
             y.start(load);
             __builtin_amdgcn_sched_barrier(0);
             // probabilities times the weight
