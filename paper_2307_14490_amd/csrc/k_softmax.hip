@@ -619,11 +619,20 @@ void k_sm_lse(PassArgs a) {
 // 16 classes at a time, each lane 16 bytes of one class's row, which are an operand
 // of a 16x16 product as they lie (fp32: exact fp32 products); the rows h are the
 // other operand, from LDS.  A lane then holds four classes' logits of one row.
-// Loads run one group of kFewGroup operands ahead.  Bound by memory: 1e6 x 128
-// fp32, one row, see the measurement at launch_few.
+// Loads run one group of kFewGroup operands ahead.  One row is bound by memory: 1e6 x
+// 128 fp32 take 87 us of the kernel, 5.9 TB/s.  From 33 rows up the exact fp32
+// products bind, 64 x 300000 x 256 at 69 TFLOP/s with the host's work.
+//
+// h takes LDS, up to kFewLds, and so leaves a CU one workgroup where it is wide: four
+// waves of 16 rows each have to themselves, more rows get eight (38 rows, 762366 x
+// 336 fp32: 403 us against 581 with four, one row: 106 against 104).  fp32 rows that
+// do not fit go through the packed records, whose traffic is three times the table
+// (the same call: 772 us); bf16 rows do above 60 KB, where their packing costs less
+// than the one workgroup (64 rows, 300000 x 512: 88 us against 96).
 constexpr int kFewGroup = 8;
-constexpr int kFewWaves = 4;
-constexpr int kFewLds = 60 * 1024;
+constexpr int few_waves(int nb) { return nb == 1 ? 4 : 8; }
+template <typename E>
+constexpr int kFewLds = (sizeof(E) == 2 ? 60 : 144) * 1024;
 
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 
@@ -674,17 +683,19 @@ __device__ __forceinline__ typename Few<E>::Vec load_few_cols(const E* row, int 
 
 // NB blocks of 16 rows.
 template <typename E, int NB, int BYTES>
-__global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
-                                                           float2* __restrict__ part, int64_t pad) {
+__global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
+                                                               float2* __restrict__ part,
+                                                               int64_t pad) {
+    constexpr int kWaves = few_waves(NB);
     using F = Few<E>;
     using Vec = typename F::Vec;
     constexpr int kN = 16 / sizeof(E);
     extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ float2 s_part[kFewWaves][NB * 16];
+    __shared__ float2 s_part[kWaves][NB * 16];
     Vec* sh = reinterpret_cast<Vec*>(lds);  // [operand][block of rows][lane]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
     const int ops = (a.dim + F::kCols - 1) / F::kCols;
-    for (int j = threadIdx.x; j < ops * NB * 64; j += kFewWaves * 64) {
+    for (int j = threadIdx.x; j < ops * NB * 64; j += kWaves * 64) {
         const int l = j & 63, b = (j >> 6) % NB, k = (j >> 6) / NB;
         const int64_t row = 16 * b + (l & 15);
         sh[j] = row < a.n ? load_few_cols<E, BYTES>(static_cast<const E*>(a.h) + row * a.ld_h,
@@ -693,8 +704,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_
     }
     __syncthreads();
     const int groups = (ops + kFewGroup - 1) / kFewGroup;
-    const int64_t step = (int64_t)gridDim.x * kFewWaves;
-    int64_t tile = (int64_t)blockIdx.x * kFewWaves + wave;
+    const int64_t step = (int64_t)gridDim.x * kWaves;
+    int64_t tile = (int64_t)blockIdx.x * kWaves + wave;
     const E* w = static_cast<const E*>(a.w);
     auto fetch = [&](int64_t t, int g, Vec* v) {
         int64_t row = t * 16 + (lane & 15);
@@ -774,7 +785,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_sm_few(SoftmaxArgs a, int64_
     if (threadIdx.x < NB * 16) {
         float2 r = s_part[0][threadIdx.x];
 #pragma unroll
-        for (int k = 1; k < kFewWaves; ++k) {
+        for (int k = 1; k < kWaves; ++k) {
             const float2 q = s_part[k][threadIdx.x];
             const float m = fmaxf(r.x, q.x);
             r.y = r.y * exp_below(r.x, m) + q.y * exp_below(q.x, m);
@@ -1371,32 +1382,31 @@ hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t 
 
 // The loss of few rows: up to 64 whose operands fit kFewLds.  Above that the tables'
 // packing is paid for by the faster products.
+template <typename E>
 int few_blocks(const SoftmaxArgs& a) {
-    const int64_t cols = a.dtype == kDtypeBf16 ? Few<bf16_t>::kCols : Few<float>::kCols;
     for (int nb = 1; nb <= 4; nb <<= 1)
-        if (a.n <= 16 * nb) return div_up(a.dim, cols) * nb * 1024 <= kFewLds ? nb : 0;
+        if (a.n <= 16 * nb)
+            return div_up(a.dim, Few<E>::kCols) * nb * 1024 <= kFewLds<E> ? nb : 0;
     return 0;
 }
 
 template <typename E, int NB>
 hipError_t few_pass(const SoftmaxArgs& a, float2* part, int64_t* slots, hipStream_t s) {
-    const int64_t tiles = div_up(a.classes, 16);
-    const int64_t most = 2048, blocks = div_up(tiles, kFewWaves) < most ? div_up(tiles, kFewWaves) : most;
+    constexpr int kWaves = few_waves(NB);
+    const int64_t tiles = div_up(a.classes, 16), need = div_up(tiles, kWaves);
+    const int64_t blocks = need < 2048 ? need : 2048;
     const int lds = (int)div_up(a.dim, Few<E>::kCols) * NB * 1024;
-    const dim3 grid((uint32_t)blocks);
-    if (a.vec16) {
-        k_sm_few<E, NB, 16><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
-    } else {
-        if constexpr (sizeof(E) == 2)
-            if (a.vec) {
-                k_sm_few<E, NB, 8><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
-                *slots = blocks;
-                return hipGetLastError();
-            }
-        k_sm_few<E, NB, sizeof(E)><<<grid, kFewWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
-    }
+    auto go = [&](auto bytes) {
+        constexpr auto* kKernel = &k_sm_few<E, NB, decltype(bytes)::value>;
+        if (lds > 60 * 1024) SM_TRY(allow_lds<kKernel>(kFewLds<E>));
+        kKernel<<<dim3((uint32_t)blocks), kWaves * 64, lds, s>>>(a, tiles, part, 16 * NB);
+        return hipGetLastError();
+    };
     *slots = blocks;
-    return hipGetLastError();
+    if (a.vec16) return go(std::integral_constant<int, 16>{});
+    if constexpr (sizeof(E) == 2)
+        if (a.vec) return go(std::integral_constant<int, 8>{});
+    return go(std::integral_constant<int, sizeof(E)>{});
 }
 
 template <typename E>
@@ -1410,7 +1420,7 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
     };
     a.vec16 = a.dim % kN == 0 && sixteen(a.h, a.ld_h) && sixteen(a.w, a.ld_w);
     int64_t slots = 0, pad = p.rows_pad;
-    const int few = few_blocks(a);
+    const int few = few_blocks<E>(a);
     if (few != 0) {
         pad = 16 * few;
         SM_TRY((few == 1   ? few_pass<E, 1>(a, part, &slots, s)

@@ -239,6 +239,19 @@ def test_softmax_aligned_without_bias(dim, dtype):
         check_softmax(softmax_case(n, classes, dim, dtype, rng, pad=pad, bias=False), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,dim", [(16, 500, 1024), (20, 601, 1024), (38, 901, 336),
+                                           (33, 1000, 480), (64, 900, 576), (64, 900, 580),
+                                           (64, 7, 484)])
+def test_softmax_few_wide_rows(n, classes, dim, dtype):
+    """Up to 64 rows whose operands fill LDS, or just do not fit."""
+    rng = np.random.default_rng(n * 7919 + classes * 31 + dim)
+    for pad, offset in ((0, 0), (3, 1)):
+        say(f"few rows {n} x {classes} x {dim} {dtype}, pad {pad}")
+        check_softmax(softmax_case(n, classes, dim, dtype, rng, pad=pad, offset=offset), dtype,
+                      grad=False)
+
+
 def softmax_on_device(h, w, labels, bias, c, scale):
     """loss, lse, dh, dw, dbias in float64 on the GPU, for sizes beyond the oracle's."""
     h, w, labels = h.double(), w.double(), labels.long()
