@@ -456,9 +456,10 @@ huge_status huge_eval_recall(const int64_t* d_offsets, const int32_t* d_neighbor
    downstream classifier of Sec. 4.2) with its gradient, and AdamW for the
    dense gradients.  The calls take no handle.  Rows are `dim` elements of
    HUGE_DTYPE_F32 or HUGE_DTYPE_BF16 at a row stride of ld >= dim elements;
-   pointers need the alignment of their element type only (16 bytes, with ld
-   and dim multiples of 4, take the vector loads of layer norm and AdamW).
-   Everything is computed in fp32 from the stored values and rounded once to
+   pointers need the alignment of their element type only (rows that start on
+   four elements, 16 bytes in fp32 and 8 in bf16, are read fastest).  An
+   infinity or a NaN in a row that counts makes what is computed from it
+   infinite or NaN, and raises no status unless a call says so.  Everything is computed in fp32 from the stored values and rounded once to
    the type of the output.  All calls are asynchronous on `stream`; argument
    errors return before any launch.  Results are bitwise reproducible.
    d_status (device int32) is sticky: a call writes an error to it where it

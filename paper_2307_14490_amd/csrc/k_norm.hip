@@ -9,6 +9,15 @@
 // its groups', and a second kernel the workgroups' rows of `partial`, always in
 // the same order.  Both kernels are bound by memory: a row is moved once in each
 // direction.
+//
+// Measured, bytes that have to be moved over time (a copy reaches 4.8 TB/s): 262144
+// x 256 fp32 95 us forward (5.6 TB/s), 157 us backward (5.1) and 5 us for the second
+// kernel; 65536 x 128 bf16, which stays in the caches, 11, 12 and 5 us.  Rows that
+// are not whole aligned fours: 60417 x 761 both ways 188 us in fp32 (4.9 TB/s, as
+// with 760 columns), 154 us in bf16 (3.0; 760 columns: 101 us), where an 8-byte
+// access at an odd address is taken apart; one element a thread took 279 us.  Rows
+// above 1024 columns by a wave alone would hold 8 chunks of three arrays a thread,
+// two waves per SIMD: 60417 x 2048 bf16 387 us against 286 by a workgroup.
 #include "device.hpp"
 #include "head.hpp"
 
