@@ -308,6 +308,30 @@ __global__ __launch_bounds__(kBlock) void k_sm_pack(SoftmaxArgs a, PackArgs w, P
     }
 }
 
+// Waves per SIMD, waves of a workgroup and tiles of X per wave, as the registers of
+// X, the sums and a tile allow.
+template <typename E, int ND, bool GRAD>
+struct Shape {
+    static constexpr bool kTwo = sizeof(E) == 4;  // fp32: two parts
+    static constexpr int kXB = !GRAD && !kTwo && ND <= 4 ? 2 : 1;
+    static constexpr int loss_occ() {
+        if (kTwo) return ND <= 4 ? 4 : ND <= 8 ? 2 : 1;
+        return ND <= 8 ? 4 : ND <= 12 ? 3 : 2;
+    }
+    static constexpr int grad_occ() {
+        if (kTwo) return ND <= 1 ? 4 : ND <= 2 ? 3 : ND <= 4 ? 2 : 1;
+        return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 8 ? 2 : 1;
+    }
+    static constexpr int kOcc = GRAD ? grad_occ() : loss_occ();
+    static constexpr int kWaves = kOcc == 4 ? 8 : 4 * kOcc;
+    // Rows of up to this many blocks go through LDS whole: two records, X, the sums
+    // and a tile within a wave's 512 registers.
+    static constexpr int kMostStaged = !GRAD ? 16 : 12;
+    static constexpr bool kStaged = ND <= kMostStaged;
+    // ... one record, brought in halves, where two do not fit
+    static constexpr bool kHalves = GRAD && kTwo && ND > 8;
+};
+
 // ---------------------------------------------------------------------------
 // What the two kernels share: X in registers, Y's records through LDS
 // ---------------------------------------------------------------------------
@@ -364,7 +388,7 @@ inline int64_t place_grid(int64_t x_blocks, int64_t x_whole, int64_t splits) {
     return (x_whole + 7) / 8 * 8 + ((x_blocks - x_whole) * splits + 7) / 8 * 8;
 }
 
-// Copies n KB to LDS, a wave 1 KB at a time; arrived after the next barrier.
+// Copies n KB to LDS, a wave 1 KB at a time.
 template <int WAVES>
 __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to, int n, int wave,
                                             int lane) {
@@ -397,6 +421,14 @@ __device__ __forceinline__ void gather_to_lds(const bf16_t* m, int64_t ld, int64
     }
 }
 
+// Waits for this wave's copies to LDS, then for all waves: what they copied has
+// arrived.  A barrier by itself waits for them only where the compiler sees a read of
+// theirs behind it.
+__device__ __forceinline__ void copies_arrived() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // Calls body(record) for this wave's Y tiles of the split: tiles yg, yg + yw, ... of
 // each stage.  copy(tile, buffer, n) brings n of them to LDS.
 template <int WAVES, bool STAGED, typename Copy, typename Body>
@@ -411,17 +443,38 @@ __device__ __forceinline__ void stream_records(const PassArgs& a, const Place& a
         uint8_t* buf = lds;
         uint8_t* next = lds + a.stage * rec_bytes;
         if (y0 < y1) copy(y0, buf, tiles(y0));
-        __syncthreads();
+        copies_arrived();
         for (int64_t at = y0; at < y1; at += a.stage) {
             const int64_t after = at + a.stage;
             if (after < y1) copy(after, next, tiles(after));
             const int n = tiles(at);
             for (int t = yg; t < n; t += yw) body(buf + t * rec_bytes, at + t);
-            __syncthreads();
+            copies_arrived();
             uint8_t* b = buf;
             buf = next;
             next = b;
         }
+    }
+}
+
+// The same where LDS has room for one record: it is brought in halves.  The T form of
+// a tile comes while S is formed, the header and the R form of the next one while the
+// second product runs; between() stands between the two, after the last read of the
+// header, and every wave calls it for every tile.
+// fp32 gradients, 3001 x 50021 x 384: 1526 us, 302 TFLOP/s; without LDS 6547.
+template <int WAVES, typename Copy, typename Body>
+__device__ __forceinline__ void stream_halves(const PassArgs& a, const Place& at_, int first_kb,
+                                              int kb, uint8_t* lds, Copy copy, Body body) {
+    const int64_t y0 = (int64_t)at_.split * a.per;
+    const int64_t y1 = !at_.whole && y0 + a.per < a.y_tiles ? y0 + a.per : a.y_tiles;
+    if (y0 < y1) copy(y0, 0, first_kb);
+    for (int64_t yt = y0; yt < y1; ++yt) {
+        copies_arrived();
+        copy(yt, first_kb, kb);
+        body(lds, yt, [&] {
+            copies_arrived();
+            if (yt + 1 < y1) copy(yt + 1, 0, first_kb);
+        });
     }
 }
 
@@ -901,6 +954,7 @@ __device__ __forceinline__ void store_out(E* p, float4 v, float scale, bool vec)
 template <typename E, int ND, int XB, int WAVES, bool STAGED, bool ROWS>
 __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uint8_t* lds) {
     constexpr bool kScaled = Kind<E>::kScaled;
+    constexpr bool HALVES = STAGED && Shape<E, ND, true>::kHalves;
     const Place at = place(a, block);
     if (at.none) return;
     const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -937,143 +991,161 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[b][d] = f32x16{};
     }
-    stream_records<WAVES, STAGED>(
-        a, at, yg, yw, rec_bytes, lds,
-        [&](int64_t tile, uint8_t* to, int n) {
-            copy_to_lds<WAVES>(a.y + tile * rec_bytes, to, n * (rec_bytes / 1024), wave, lane);
-        },
-        [&](const uint8_t* rec, int64_t yt) {
-            f32x16 c[XB];
+    auto body = [&](const uint8_t* rec, int64_t yt, auto between) {
+        f32x16 c[XB];
 #pragma unroll
-            for (int b = 0; b < XB; ++b) {
-                if constexpr (kScaled) {
-                    c[b] = f32x16{};
-                } else if constexpr (ROWS) {
-                    c[b] = row_values(rec, kTerm, half);
-                } else {
-                    // written anew for every tile: kept, it would take 16 registers
-                    float bias0 = xterm[b];
-                    asm("" : "+v"(bias0));
+        for (int b = 0; b < XB; ++b) {
+            if constexpr (kScaled) {
+                c[b] = f32x16{};
+            } else if constexpr (ROWS) {
+                c[b] = row_values(rec, kTerm, half);
+            } else {
+                // written anew for every tile: kept, it would take 16 registers
+                float bias0 = xterm[b];
+                asm("" : "+v"(bias0));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) c[b][i] = bias0;
-                }
+                for (int i = 0; i < 16; ++i) c[b][i] = bias0;
             }
-            tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
-            // the first operands of the second product are read behind the exponentials
-            const uint8_t* form = rec + kHeader + Kind<E>::kParts * nfrag * 1024;
-            auto load = [&](int f) {
-                return load_operand<E>(form, (f / ND) * nd + db0 + f % ND, nfrag, lane);
-            };
-            Ahead<E, 2 * ND, STAGED && kScaled && (ND > 4)> y;
+        }
+        tile_products<E, ND, XB, STAGED>(rec, x, xt.rec, nfrag, a.kd, lane, c);
+        // the first operands of the second product are read behind the exponentials
+        const uint8_t* form = rec + kHeader + Kind<E>::kParts * nfrag * 1024;
+        auto load = [&](int f) {
+            return load_operand<E>(form, (f / ND) * nd + db0 + f % ND, nfrag, lane);
+        };
+        Ahead<E, 2 * ND, STAGED && kScaled && (ND > 4)> y;
+        if constexpr (!HALVES) {
             y.start(load);
             __builtin_amdgcn_sched_barrier(0);
-            // probabilities times the weight
-            if constexpr (kScaled) {
-                const f32x16 ymul = row_values(rec, kMul, half);
-                const f32x16 yterm = row_values(rec, kTerm2, half);
-#pragma unroll
-                for (int b = 0; b < XB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        c[b][i] = __builtin_amdgcn_exp2f(
-                            fmaf(c[b][i] * ymul[i], xmul[b], yterm[i]) + xterm[b]);
-            } else if constexpr (ROWS) {
-#pragma unroll
-                for (int b = 0; b < XB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, xterm[b]));
-            } else {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 yterm = row_four(rec, kTerm2, half, g);
-#pragma unroll
-                    for (int b = 0; b < XB; ++b)
-#pragma unroll
-                        for (int i = 4 * g; i < 4 * g + 4; ++i)
-                            c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, yterm[i - 4 * g]));
-                }
-            }
-            // the labels' elements, in the tiles that hold one
-#pragma unroll
-            for (int b = 0; b < XB; ++b) {
-                if constexpr (ROWS) {
-                    const int32_t d = xl[b] - (int32_t)yt * 32;
-                    if (__ballot((uint32_t)d < 32u) != 0) {
-                        const int32_t e = d - 4 * half;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (e == tile_row(i, 0)) c[b][i] -= xw[b];
-                    }
-                } else {
-                    const int32_t d = lane_label(rec, lane) - (int32_t)(a.class0 + xt.t[b] * 32);
-                    if (__ballot((uint32_t)d < 32u) != 0) {
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const f32x4 label = row_four(rec, kLabel, half, g);
-                            const f32x4 weight = row_four(rec, kWeight, half, g);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (__float_as_int(label[i]) == xl[b]) c[b][4 * g + i] -= weight[i];
-                        }
-                    }
-                    if (a.want_bias) {
-                        bias[b] += sum16(c[b]);
-                    }
-                }
-            }
-            if constexpr (kScaled) {
-                const f32x16 ymul = row_values(rec, kMul, half);
-#pragma unroll
-                for (int b = 0; b < XB; ++b) {
-                    float big = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        c[b][i] *= ymul[i];
-                        big = fmaxf(big, fabsf(c[b][i]));
-                    }
-                    // the halves share the sums of a row: they share its scale
-                    big = fmaxf(big, __shfl_xor(big, 32));
-                    const bool scale_anew = big * pscale[b] > 0x1p15f ||
-                                            (pscale[b] == 0.f && big > 0.f);
-                    if (__ballot(scale_anew) != 0) {
-                        // big is below 2^e: the largest element is brought below 2^15
-                        float ratio = 1.f;
-                        if (scale_anew) {
-                            const int e = __builtin_amdgcn_frexp_expf(big);
-                            const float s = ldexpf(1.f, e < -105 ? 120 : 15 - e);
-                            ratio = pscale[b] > 0.f ? fminf(s / pscale[b], 1.f) : 0.f;
-                            pscale[b] = pscale[b] > 0.f ? fminf(s, pscale[b]) : s;
-                        }
-#pragma unroll
-                        for (int d = 0; d < ND; ++d) {
-                            // a wave alone on its SIMD keeps the sums in accumulation
-                            // registers; unless that is said here, the compiler copies
-                            // them for this product in every tile
-                            if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
-                            acc[b][d] *= ratio;
-                            if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
-                        }
-                    }
-                    c[b] *= pscale[b];
-                }
-            }
-            Operand<E> p[XB][2];
+        }
+        // probabilities times the weight
+        if constexpr (kScaled) {
+            const f32x16 ymul = row_values(rec, kMul, half);
+            const f32x16 yterm = row_values(rec, kTerm2, half);
 #pragma unroll
             for (int b = 0; b < XB; ++b)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    f32x8 v;
+                for (int i = 0; i < 16; ++i)
+                    c[b][i] = __builtin_amdgcn_exp2f(
+                        fmaf(c[b][i] * ymul[i], xmul[b], yterm[i]) + xterm[b]);
+        } else if constexpr (ROWS) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = c[b][8 * t + j];
-                    p[b][t] = split<E>(v);
-                }
-            y.template run<kProducts<E> * XB>(load, [&](int f, const Operand<E>& q) {
+            for (int b = 0; b < XB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, xterm[b]));
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 yterm = row_four(rec, kTerm2, half, g);
 #pragma unroll
                 for (int b = 0; b < XB; ++b)
-                    acc[b][f % ND] = product<E>(q, p[b][f / ND], acc[b][f % ND]);
-            });
+#pragma unroll
+                    for (int i = 4 * g; i < 4 * g + 4; ++i)
+                        c[b][i] = __builtin_amdgcn_exp2f(fmaf(c[b][i], kLog2e, yterm[i - 4 * g]));
+            }
+        }
+        // the labels' elements, in the tiles that hold one
+#pragma unroll
+        for (int b = 0; b < XB; ++b) {
+            if constexpr (ROWS) {
+                const int32_t d = xl[b] - (int32_t)yt * 32;
+                if (__ballot((uint32_t)d < 32u) != 0) {
+                    const int32_t e = d - 4 * half;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (e == tile_row(i, 0)) c[b][i] -= xw[b];
+                }
+            } else {
+                const int32_t d = lane_label(rec, lane) - (int32_t)(a.class0 + xt.t[b] * 32);
+                if (__ballot((uint32_t)d < 32u) != 0) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 label = row_four(rec, kLabel, half, g);
+                        const f32x4 weight = row_four(rec, kWeight, half, g);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (__float_as_int(label[i]) == xl[b]) c[b][4 * g + i] -= weight[i];
+                    }
+                }
+                if (a.want_bias) {
+                    bias[b] += sum16(c[b]);
+                }
+            }
+        }
+        if constexpr (kScaled) {
+            const f32x16 ymul = row_values(rec, kMul, half);
+#pragma unroll
+            for (int b = 0; b < XB; ++b) {
+                float big = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    c[b][i] *= ymul[i];
+                    big = fmaxf(big, fabsf(c[b][i]));
+                }
+                // the halves share the sums of a row: they share its scale
+                big = fmaxf(big, __shfl_xor(big, 32));
+                const bool scale_anew = big * pscale[b] > 0x1p15f ||
+                                        (pscale[b] == 0.f && big > 0.f);
+                if (__ballot(scale_anew) != 0) {
+                    // big is below 2^e: the largest element is brought below 2^15
+                    float ratio = 1.f;
+                    if (scale_anew) {
+                        const int e = __builtin_amdgcn_frexp_expf(big);
+                        const float s = ldexpf(1.f, e < -105 ? 120 : 15 - e);
+                        ratio = pscale[b] > 0.f ? fminf(s / pscale[b], 1.f) : 0.f;
+                        pscale[b] = pscale[b] > 0.f ? fminf(s, pscale[b]) : s;
+                    }
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        // a wave alone on its SIMD keeps the sums in accumulation
+                        // registers; unless that is said here, the compiler copies
+                        // them for this product in every tile
+                        if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
+                        acc[b][d] *= ratio;
+                        if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
+                    }
+                }
+                c[b] *= pscale[b];
+            }
+        }
+        Operand<E> p[XB][2];
+#pragma unroll
+        for (int b = 0; b < XB; ++b)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x8 v;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = c[b][8 * t + j];
+                p[b][t] = split<E>(v);
+            }
+        if constexpr (HALVES) {
+            between();
+            y.start(load);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        y.template run<kProducts<E> * XB>(load, [&](int f, const Operand<E>& q) {
+#pragma unroll
+            for (int b = 0; b < XB; ++b)
+                acc[b][f % ND] = product<E>(q, p[b][f / ND], acc[b][f % ND]);
         });
+    };
+    if constexpr (HALVES) {
+        stream_halves<WAVES>(
+            a, at, rec_bytes / 1024 - Kind<E>::kParts * nfrag, rec_bytes / 1024, lds,
+            [&](int64_t tile, int kb0, int kb1) {
+                copy_to_lds<WAVES>(a.y + tile * rec_bytes + kb0 * 1024, lds + kb0 * 1024, kb1 - kb0,
+                                   wave, lane);
+            },
+            body);
+    } else {
+        stream_records<WAVES, STAGED>(
+            a, at, yg, yw, rec_bytes, lds,
+            [&](int64_t tile, uint8_t* to, int n) {
+                copy_to_lds<WAVES>(a.y + tile * rec_bytes, to, n * (rec_bytes / 1024), wave, lane);
+            },
+            [&](const uint8_t* rec, int64_t yt) { body(rec, yt, [] {}); });
+    }
 #pragma unroll
     for (int b = 0; b < XB; ++b) {
         if (!xt.in[b]) continue;
@@ -1189,28 +1261,6 @@ __global__ __launch_bounds__(kBlock) void k_sm_join(JoinArgs a, JoinArgs b, int 
 // ---------------------------------------------------------------------------
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Waves per SIMD, waves of a workgroup and tiles of X per wave, as the registers of
-// X, the sums and a tile allow.
-template <typename E, int ND, bool GRAD>
-struct Shape {
-    static constexpr bool kTwo = sizeof(E) == 4;  // fp32: two parts
-    static constexpr int kXB = !GRAD && !kTwo && ND <= 4 ? 2 : 1;
-    static constexpr int loss_occ() {
-        if (kTwo) return ND <= 4 ? 4 : ND <= 8 ? 2 : 1;
-        return ND <= 8 ? 4 : ND <= 12 ? 3 : 2;
-    }
-    static constexpr int grad_occ() {
-        if (kTwo) return ND <= 1 ? 4 : ND <= 2 ? 3 : ND <= 4 ? 2 : 1;
-        return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 8 ? 2 : 1;
-    }
-    static constexpr int kOcc = GRAD ? grad_occ() : loss_occ();
-    static constexpr int kWaves = kOcc == 4 ? 8 : 4 * kOcc;
-    // Rows of up to this many blocks go through LDS whole: two records, and X, the sums
-    // and a tile within a wave's 512 registers.
-    static constexpr int kMostStaged = !GRAD ? 16 : kTwo ? 8 : 12;
-    static constexpr bool kStaged = ND <= kMostStaged;
-};
-
 // Rows that do not go through LDS: waves that wait for each other's loads less.
 template <typename E, int ND, bool GRAD, bool STAGED>
 constexpr int pass_occ() {
@@ -1322,7 +1372,7 @@ Layout fit_pass(const SoftmaxPlan& p, bool rows, PassArgs& a) {
     a.x_whole = (int32_t)l.x_whole, a.splits = (int32_t)l.splits, a.per = l.per;
     a.part_first = l.part_first, a.part_rows = l.part_rows;
     a.nfrag = p.dp / 16, a.kd = p.kd, a.dp = p.dp, a.dim = p.dim;
-    a.lds = STAGED ? 2 * l.stage * rec : 0;
+    a.lds = !STAGED ? 0 : S::kHalves ? rec : 2 * l.stage * rec;
     a.grid = place_grid(l.x_blocks, l.x_whole, l.splits);
     return l;
 }
@@ -1379,7 +1429,8 @@ hipError_t grad_pass(const SoftmaxPlan& p, const PassArgs& classes, const PassAr
         if constexpr (Shape<E, ND, true>::kStaged) {
             if (p.chunks == 1) return grad_pass<E, ND, true>(p, classes, rows, fit, s);
             // wider rows: at least half of the largest ND in each of two chunks or more
-            if constexpr (ND >= 6) return grad_pass<E, ND, false>(p, classes, rows, fit, s);
+            if constexpr (ND >= 6 && !Shape<E, ND, true>::kHalves)
+                return grad_pass<E, ND, false>(p, classes, rows, fit, s);
         }
     })
     return hipErrorInvalidValue;
@@ -1563,7 +1614,7 @@ SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype,
     p.dim = dim;
     p.parts = dtype == kDtypeBf16 ? Kind<bf16_t>::kParts : Kind<float>::kParts;
     const int nd = (int)div_up(dim, 32);
-    const int most = !grad ? 16 : p.parts == 2 ? 8 : 12;
+    const int most = !grad ? 16 : p.parts == 2 && nd > 12 ? 8 : 12;
     p.chunks = (int)div_up(nd, nd > most && !grad ? 8 : most);
     p.nd = nd > most && !grad ? 8 : made_for((int)div_up(nd, p.chunks));
     p.dp = 32 * p.nd * p.chunks;

@@ -294,6 +294,13 @@ def test_softmax_many_tiles(n, classes, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,classes,dim", [(4_100, 9_001, 384), (9_001, 3_001, 320), (33, 40_001, 288)])
+def test_softmax_many_tiles_of_wide_rows(n, classes, dim, dtype):
+    """Rows of which LDS takes one record: every tile comes in halves (fp32)."""
+    test_softmax_many_tiles(n, classes, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_softmax_many_rows_few_classes_and_few_rows_many_classes(dtype):
     rng = np.random.default_rng(11)
     check_softmax(softmax_case(20_011, 37, 32, dtype, rng), dtype)
