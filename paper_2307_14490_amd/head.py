@@ -392,7 +392,9 @@ class SoftmaxHead:
     or the exact softmax over all nodes that negative sampling stands in for.
 
     step(x, labels) trains the head on rows x (n x dim) and returns the mean loss
-    (device) and the gradient of x, for a caller that trains the rows too."""
+    (device) and the gradient of x, for a caller that trains the rows too.  Steps and
+    losses on different streams wait for each other; what a call returns is ready
+    on its own stream."""
 
     def __init__(self, num_classes, dim, max_rows, dtype="f32", lr=1e-3, weight_decay=0.01,
                  states="f32", eps=1e-5, seed=0, device="cuda"):
@@ -410,14 +412,21 @@ class SoftmaxHead:
                          weight_decay=weight_decay, states=states)
         self.total = torch.zeros(1, dtype=torch.float64, device=dev)
 
+    def _ordered(self, stream):
+        # before the first kernel: layer norm, which waits for nothing, reads parameters
+        self.op._ordered(stream)
+        self.opt._ordered(stream)
+
     def loss(self, x, labels, weights=None, stream=None):
         """Loss per row, forward only."""
+        self._ordered(stream)
         y, _, _ = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
         return self.op.loss(y, self.w, labels, self.bias, weights, stream=stream)[0]
 
     def step(self, x, labels, weights=None, lr=None, want_dx=True, stream=None):
         """One training step on the mean over the rows of their losses."""
         scale = 1.0 / max(1, x.shape[0])
+        self._ordered(stream)
         y, mean, rstd = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
         _, lse = self.op.loss(y, self.w, labels, self.bias, weights, total=self.total,
                               stream=stream)
@@ -426,7 +435,8 @@ class SoftmaxHead:
         dx, dgamma, dbeta = layer_norm_backward(dy, x, self.gamma, mean, rstd, want_dx=want_dx,
                                                 stream=stream)
         self.opt.step([dgamma, dbeta, dw, db], lr=lr, stream=stream)
-        return self.total * scale, dx
+        with _on(self.op.device, stream, ()):
+            return self.total * scale, dx
 
     def check(self):
         """Raise the first device-side error since the last check."""

@@ -1,0 +1,57 @@
+"""The softmax head on more than one stream: the same bits as on one.  The streams are
+kept busy with other work, so that what is not ordered would come too early."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2307_14490_amd as P  # noqa: E402
+from gpu_common import say  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    yield
+    torch.cuda.synchronize()
+
+
+def busy(stream=None):
+    """Some milliseconds of work on a stream."""
+    with torch.cuda.stream(stream or torch.cuda.current_stream()):
+        a = torch.ones((2048, 2048), device="cuda")
+        for _ in range(20):
+            a = a @ a * 1e-4
+
+
+def head_case(dtype, n=300, classes=700, dim=64):
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(n, dim, device="cuda", generator=g)
+    lab = torch.randint(0, classes, (n,), device="cuda", generator=g).to(torch.int32)
+    torch.cuda.synchronize()
+    return x.to(torch.bfloat16 if dtype == "bf16" else torch.float32), lab
+
+
+@pytest.mark.parametrize("dtype,states", [("f32", "f32"), ("bf16", "q8")])
+def test_head_takes_turns_between_streams(dtype, states):
+    x, lab = head_case(dtype)
+    torch.cuda.synchronize()
+    say(f"head on two streams, {dtype}, moments {states}")
+
+    def train(streams):
+        busy()
+        head = P.SoftmaxHead(700, 64, 300, dtype=dtype, lr=1e-2, states=states, seed=2)
+        got = []
+        for s in streams:
+            busy(s)
+            got.append(head.step(x, lab, stream=s))
+        torch.cuda.synchronize()
+        head.check()
+        return [t for pair in got for t in pair] + list(head.opt.params)
+
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    want = train([None] * 6)
+    for u, v in zip(want, train([a, b, None, a, None, b])):
+        assert torch.equal(u, v)

@@ -1,0 +1,70 @@
+"""The softmax head on more than one stream, without a GPU: what its classes launch is
+ordered, on whatever stream they are called (stream_order records and checks it)."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2307_14490_amd as P  # noqa: E402
+from stream_order import Order, Race  # noqa: E402
+
+
+@pytest.fixture
+def order(monkeypatch):
+    o = Order(monkeypatch)
+    o.seen = [o.stream(), o.stream()]
+    return o
+
+
+def batch(order, stream):
+    """Rows and labels made on the stream that the head is to use."""
+    with order.on(stream):
+        return torch.randn(6, 8), torch.zeros(6, dtype=torch.int32)
+
+
+def test_the_record_finds_a_missing_wait(order):
+    a, b = order.seen
+    with order.on(a):
+        t = torch.zeros(4)
+    with order.on(b):
+        with pytest.raises(Race):
+            t + 1
+        b.wait_stream(a)
+        t + 1
+    with order.on(a), pytest.raises(Race):
+        t.zero_()  # b still reads
+    b.synchronize()
+    with order.on(a):
+        t.zero_()
+    assert order.owned_elsewhere(t) == {b.cuda_stream}
+    t.record_stream(b)
+    assert not order.owned_elsewhere(t)
+
+
+def test_head_steps_on_a_stream_of_the_callers(order):
+    """Its parameters were filled on the constructor's stream; the mean loss that a step
+    returns is formed on the step's stream."""
+    a, _ = order.seen
+    head = P.SoftmaxHead(5, 8, 6)
+    x, lab = batch(order, a)
+    for _ in range(2):
+        loss, dx = head.step(x, lab, stream=a)
+        with order.on(a):
+            loss + 1, dx + 1
+    assert head.loss(x, lab, stream=a).shape == (6,)
+
+
+@pytest.mark.parametrize("states", ["f32", "q8"])
+def test_head_takes_turns_between_streams(order, states):
+    a, b = order.seen
+    head = P.SoftmaxHead(5, 8, 6, states=states)
+    data = {s: batch(order, s) for s in (a, b, order.default)}
+    for s in (a, b, order.default, a, order.default, b):
+        loss, _ = head.step(*data[s], stream=s)
+        with order.on(s):
+            loss + 1
+        with order.on(s):  # ... and as the current stream
+            head.step(*data[s])
+    for s in (order.default, a):  # the parameters of the last step
+        head.loss(*data[s], stream=s)
+        with order.on(s):
+            head.gamma + 1
