@@ -4,8 +4,10 @@ loss with its gradient, AdamW, and a head that trains with them.
 Argument marshalling for the calls of ``include/huge.h``, as in ``binding``.
 Rows may be any two-dimensional GPU tensors whose columns are adjacent (a slice
 of a wider buffer among them).  Work runs on ``stream`` (default: torch's
-current stream); outputs and workspaces are allocated for that stream, and
-arguments that live on another one are kept until the call's work is done.
+current stream), and outputs are allocated for that stream.  A stream that is
+given keeps the arguments until the call's work on it is done; on the current
+one torch's own rule holds, that who uses a tensor of another stream there
+records it.  What the classes hold is kept on either.
 Errors that only the device can see are kept in a status word until ``check``.
 """
 from __future__ import annotations
@@ -102,8 +104,9 @@ class _on:
 
 
 class _Status:
-    """The sticky status word of an operator, and its workspace's last stream: a
-    call on another stream first waits for the work on that one."""
+    """The sticky status word of an operator, the memory of its own, and the stream
+    of its last call: a call on another stream first waits for the work on that one,
+    and the memory is not given to others before the work on any of them is done."""
 
     def __init__(self, device):
         import torch
@@ -112,6 +115,7 @@ class _Status:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._status_ptr = self.status.data_ptr()
+        self._own = [self.status]
         self._last = torch.cuda.current_stream(self.device)
         self._last_ptr = self._last.cuda_stream
 
@@ -121,6 +125,8 @@ class _Status:
         if now != self._last_ptr:
             stream = torch.cuda.current_stream(self.device) if stream is None else stream
             stream.wait_stream(self._last)
+            for t in self._own:
+                t.record_stream(stream)
             self._last, self._last_ptr = stream, now
 
     def check(self):
@@ -201,6 +207,7 @@ class SoftmaxLoss(_Status):
             raise HugeError(HUGE_ERR_INVALID_ARG, "huge_softmax_workspace_bytes")
         super().__init__(device)
         self._ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
+        self._own.append(self._ws)
         self._ws_ptr = self._ws.data_ptr() + ((-self._ws.data_ptr()) % 256)
 
     def _inputs(self, what, h, w, labels, bias, weights):
@@ -291,6 +298,7 @@ class AdamW(_Status):
             self._state_at.append(at)
             at += -(-L.huge_adamw_state_bytes(p.numel(), self.kind) // 256) * 256
         self.states = torch.zeros(at + 256, dtype=torch.uint8, device=self.device)
+        self._own += [self.states, *self.params]
         self._skip = (-self.states.data_ptr()) % 256
         for k, p in enumerate(self.params):
             t = self._tensors[k]
@@ -411,6 +419,7 @@ class SoftmaxHead:
         self.opt = AdamW([self.gamma, self.beta, self.w, self.bias], lr=lr,
                          weight_decay=weight_decay, states=states)
         self.total = torch.zeros(1, dtype=torch.float64, device=dev)
+        self.op._own.append(self.total)
 
     def _ordered(self, stream):
         # before the first kernel: layer norm, which waits for nothing, reads parameters

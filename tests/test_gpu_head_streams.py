@@ -55,3 +55,26 @@ def test_head_takes_turns_between_streams(dtype, states):
     want = train([None] * 6)
     for u, v in zip(want, train([a, b, None, a, None, b])):
         assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_workspace_of_a_dropped_operator_is_not_given_away_early(given):
+    """The operator goes while its call waits on a busy stream: tensors made after it
+    keep their values."""
+    x, lab = head_case("f32")
+    w = torch.randn(700, 64, device="cuda")
+    side = torch.cuda.Stream()
+    op = P.SoftmaxLoss(300, 700, 64)
+    size = op.ws_bytes
+    op.loss(x, w, lab)
+    torch.cuda.synchronize()
+    busy(side)
+    if given:
+        op.loss(x, w, lab, stream=side)
+    else:
+        with torch.cuda.stream(side):
+            op.loss(x, w, lab)
+    del op
+    after = torch.full((size + 256,), 77, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert bool((after == 77).all())

@@ -68,3 +68,31 @@ def test_head_takes_turns_between_streams(order, states):
         head.loss(*data[s], stream=s)
         with order.on(s):
             head.gamma + 1
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_memory_of_the_operators_is_kept_for_every_stream(order, given):
+    """Workspace, status word, moments and parameters, whether the stream is an argument
+    or the current one: dropped, they are given to others only behind its work."""
+    a, b = order.seen
+    head = P.SoftmaxHead(5, 8, 6)
+    for s in (a, b):
+        x, lab = batch(order, s)
+        if given:
+            head.step(x, lab, stream=s)
+        else:
+            with order.on(s):
+                head.step(x, lab)
+    own = [head.op._ws, head.op.status, head.opt.states, head.opt.status, head.total,
+           *head.opt.params]
+    assert len(own) == 9
+    assert not order.owned_elsewhere(*own)
+
+
+def test_arguments_are_kept_for_the_stream_that_is_given(order):
+    a, _ = order.seen
+    x, lab = batch(order, order.default)
+    head = P.SoftmaxHead(5, 8, 6)
+    a.wait_stream(order.default)
+    head.step(x, lab, stream=a)
+    assert not order.owned_elsewhere(x, lab)
