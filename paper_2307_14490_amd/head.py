@@ -358,12 +358,13 @@ class AdamW(_Status):
         return (ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
 
     def values(self, stream=None):
-        """(m, v): lists of float32 tensors shaped like the parameters.  States "f32":
-        the moments themselves, as views of the states; "q8": what they stand for."""
+        """(m, v): lists of float32 tensors shaped like the parameters, ready on the
+        stream.  States "f32": the moments themselves, as views that the next step
+        changes (clone what is to stay); "q8": what they stand for, in new tensors."""
         import torch
+        self._ordered(stream)
         if self.kind == HUGE_STATE_F32:
             return [list(ts) for ts in self._views]
-        self._ordered(stream)
         with _on(self.device, stream, (self.states,)) as st:
             flat = torch.empty(self._flat, dtype=torch.float32, device=self.device)
             base, count = flat.data_ptr(), len(self.params)

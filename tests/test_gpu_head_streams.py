@@ -78,3 +78,20 @@ def test_workspace_of_a_dropped_operator_is_not_given_away_early(given):
     after = torch.full((size + 256,), 77, dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     assert bool((after == 77).all())
+
+
+@pytest.mark.parametrize("states", ["f32", "q8"])
+def test_moments_are_those_of_the_last_step(states):
+    p, g = torch.zeros(5000, device="cuda"), torch.randn(5000, device="cuda")
+    want = P.AdamW([p], states=states)
+    want.step([g])
+    m, v = want.values()
+    opt = P.AdamW([p.clone()], states=states)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy(side)
+    opt.step([g], stream=side)
+    m2, v2 = opt.values()
+    m2, v2 = m2[0].clone(), v2[0].clone()
+    torch.cuda.synchronize()
+    assert torch.equal(m2, m[0]) and torch.equal(v2, v[0])

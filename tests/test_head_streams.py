@@ -96,3 +96,18 @@ def test_arguments_are_kept_for_the_stream_that_is_given(order):
     a.wait_stream(order.default)
     head.step(x, lab, stream=a)
     assert not order.owned_elsewhere(x, lab)
+
+
+@pytest.mark.parametrize("states", ["f32", "q8"])
+def test_moments_are_those_of_the_last_step(order, states):
+    """values() on one stream after a step on another, and a step after values()."""
+    a, b = order.seen
+    with order.on(a):
+        opt = P.AdamW([torch.zeros(300)], states=states)
+        grad = torch.ones(300)
+    opt.step([grad], stream=a)
+    for s in (b, None):
+        m, v = opt.values(stream=s)
+        with order.on(s or order.default):
+            m[0] + v[0]
+    opt.step([grad], stream=a)
