@@ -132,10 +132,12 @@ class _Status:
     def check(self):
         """Raise HugeError if a call since the last check met a device-side error
         (synchronises); the status is cleared."""
-        self._last.synchronize()
-        st = int(self.status.item())
+        import torch
+        with torch.cuda.stream(self._last):  # the clearing comes before a next call
+            st = int(self.status.item())
+            if st != 0:
+                self.status.zero_()
         if st != 0:
-            self.status.zero_()
             raise HugeError(st, type(self).__name__ + " (device)")
 
 

@@ -95,3 +95,23 @@ def test_moments_are_those_of_the_last_step(states):
     m2, v2 = m2[0].clone(), v2[0].clone()
     torch.cuda.synchronize()
     assert torch.equal(m2, m[0]) and torch.equal(v2, v[0])
+
+
+def test_an_error_on_another_stream_is_reported_once():
+    x, lab = head_case("f32")
+    w = torch.randn(700, 64, device="cuda")
+    op, side = P.SoftmaxLoss(300, 700, 64), torch.cuda.Stream()
+    bad = lab.clone()
+    bad[5] = 700
+    torch.cuda.synchronize()
+    for _ in range(3):
+        busy(side)
+        op.loss(x, w, bad, stream=side)
+        busy()
+        with pytest.raises(P.HugeError):
+            op.check()
+        op.loss(x, w, lab, stream=side)
+        op.check()
+        op.loss(x, w, bad, stream=side)
+        with pytest.raises(P.HugeError):
+            op.check()

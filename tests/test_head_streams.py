@@ -111,3 +111,19 @@ def test_moments_are_those_of_the_last_step(order, states):
         with order.on(s or order.default):
             m[0] + v[0]
     opt.step([grad], stream=a)
+
+
+def test_a_reported_error_is_cleared_before_the_next_call(order):
+    """check() on one stream between two calls on another."""
+    a, _ = order.seen
+    op = P.SoftmaxLoss(6, 5, 8)
+    x, lab = batch(order, a)
+    w, _ = batch(order, a)
+    w = w[:5]
+    with order.on(a):
+        op.loss(x, w, lab)
+        op.status.fill_(-2)  # as a kernel would
+    with pytest.raises(P.HugeError):
+        op.check()
+    op.loss(x, w, lab, stream=a)
+    op.check()
