@@ -103,6 +103,16 @@ class _on:
                     t.record_stream(self.stream)
 
 
+def _capturing(stream):
+    """Whether a stream's work is being captured into a graph (the default stream's
+    never is)."""
+    import torch
+    if stream.cuda_stream == 0:
+        return False
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _Status:
     """The sticky status word of an operator, the memory of its own, and the stream
     of its last call: a call on another stream first waits for the work on that one,
@@ -124,7 +134,10 @@ class _Status:
         now = _current(self.device) if stream is None else stream.cuda_stream
         if now != self._last_ptr:
             stream = torch.cuda.current_stream(self.device) if stream is None else stream
-            stream.wait_stream(self._last)
+            # a graph waits for nothing outside of it: what came before its capture is
+            # done when that begins, and its replays are the caller's to order
+            if not _capturing(stream) or _capturing(self._last):
+                stream.wait_stream(self._last)
             for t in self._own:
                 t.record_stream(stream)
             self._last, self._last_ptr = stream, now

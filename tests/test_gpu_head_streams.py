@@ -115,3 +115,29 @@ def test_an_error_on_another_stream_is_reported_once():
         op.loss(x, w, bad, stream=side)
         with pytest.raises(P.HugeError):
             op.check()
+
+
+def test_capture_after_work_on_the_current_stream():
+    """Recorded on a stream that the operator has not seen, replayed between the
+    program's own calls of it."""
+    x, lab = head_case("bf16")
+    w = (torch.randn(700, 64, device="cuda") * 0.2).bfloat16()
+    op = P.SoftmaxLoss(300, 700, 64, dtype="bf16")
+
+    def both():
+        loss, lse = op.loss(x, w, lab)
+        return (loss, *op.grad(x, w, lab, lse))
+
+    want = [t.clone() for t in both()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    for _ in range(3):
+        for t in held:
+            t.fill_(0)
+        graph.replay()
+        for u, v in zip(want, held):
+            assert torch.equal(u, v)
+        for u, v in zip(want, both()):
+            assert torch.equal(u, v)
+    op.check()

@@ -127,3 +127,22 @@ def test_a_reported_error_is_cleared_before_the_next_call(order):
         op.check()
     op.loss(x, w, lab, stream=a)
     op.check()
+
+
+def test_capture_on_a_stream_of_its_own(order):
+    """A call recorded into a graph waits for no work outside of it, and for the other
+    streams of the same graph."""
+    a, b = order.seen
+    op = P.SoftmaxLoss(6, 5, 8)
+    x, lab = batch(order, order.default)
+    w = batch(order, order.default)[0][:5]
+    op.loss(x, w, lab)
+    order.default.synchronize()  # as before any capture
+    a.capturing = True
+    op.loss(x, w, lab, stream=a)
+    b.capturing = True  # forked from a
+    op.loss(x, w, lab, stream=b)
+    op.loss(x, w, lab, stream=a)
+    a.capturing = b.capturing = False
+    op.loss(x, w, lab)
+    op.check()
