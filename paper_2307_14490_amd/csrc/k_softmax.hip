@@ -208,15 +208,16 @@ __device__ __forceinline__ float max4(float m, float4 v) {
 // row, 5.4 TB/s.
 template <typename E>
 __global__ __launch_bounds__(kBlock) void k_sm_pack(SoftmaxArgs a, PackArgs w, PackArgs h,
-                                                    int nfrag, int forms) {
+                                                    int nfrag, int forms, int64_t first) {
     constexpr int kParts = Kind<E>::kParts;
     using Vec = typename Kind<E>::Vec;
     __shared__ float s[32][kPackCols + 4];
     __shared__ bool s_out[32];
     __shared__ float s_mul[32];
-    const bool second = blockIdx.x >= w.tiles;
+    const int64_t block = first + blockIdx.x;
+    const bool second = block >= w.tiles;
     const PackArgs& k = second ? h : w;
-    const int64_t tile = second ? blockIdx.x - w.tiles : blockIdx.x;
+    const int64_t tile = second ? block - w.tiles : block;
     uint8_t* rec = k.out + tile * record_bytes(nfrag, kParts, forms);
     float* head = reinterpret_cast<float*>(rec);
     if (threadIdx.x < 32) {
@@ -859,9 +860,9 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
 // the sizes fix, and the label's logit is formed from the rows themselves.
 template <typename E, int LANES>
 __global__ __launch_bounds__(kBlock) void k_sm_loss(SoftmaxArgs a, const float2* __restrict__ part,
-                                                    int splits, int64_t pad) {
+                                                    int splits, int64_t pad, int64_t first) {
     const int lane = threadIdx.x % LANES;
-    const int64_t i = (int64_t)blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES;
+    const int64_t i = (first + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
     if (i >= a.n) return;
     const int32_t y = a.labels[i];
     const float c = a.weight == nullptr ? 1.f : a.weight[i];
@@ -1248,10 +1249,11 @@ __device__ __forceinline__ void join_slots(const JoinArgs& a, int64_t block, int
 // One or two sets of partial results.
 template <typename E>
 __global__ __launch_bounds__(kBlock) void k_sm_join(JoinArgs a, JoinArgs b, int dp, int dim,
-                                                    float scale) {
-    const bool second = blockIdx.x >= a.blocks;
+                                                    float scale, int64_t first) {
+    int64_t block = first + blockIdx.x;
+    const bool second = block >= a.blocks;
     const JoinArgs& k = second ? b : a;
-    const int64_t block = second ? blockIdx.x - a.blocks : blockIdx.x;
+    if (second) block -= a.blocks;
     if (k.lanes == 16) join_slots<E, 16>(k, block, dp, dim, scale);
     else join_slots<E, 1>(k, block, dp, dim, scale);
 }
@@ -1436,6 +1438,21 @@ hipError_t grad_pass(const SoftmaxPlan& p, const PassArgs& classes, const PassAr
     return hipErrorInvalidValue;
 }
 
+// Work that may be more than the 2^32 - 1 threads of a launch (2^28 rows of 16, 2^24 rows
+// of 1024 columns) goes in launches of up to kLaunchBlocks workgroups of kBlock
+// threads, each told its first.
+constexpr int64_t kLaunchBlocks = (int64_t)1 << 23;
+
+template <typename Launch>
+hipError_t in_launches(int64_t blocks, Launch launch) {
+    for (int64_t first = 0; first < blocks; first += kLaunchBlocks) {
+        const int64_t left = blocks - first;
+        launch(dim3((uint32_t)(left < kLaunchBlocks ? left : kLaunchBlocks)), first);
+        SM_TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
 bool fours(const void* m, int64_t ld, size_t elem) {
     return (reinterpret_cast<uintptr_t>(m) & (4 * elem - 1)) == 0 && ld % 4 == 0;
 }
@@ -1449,8 +1466,9 @@ hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t 
     w.out = a.ws + p.w, w.classes = true, w.vec = fours(a.w, a.ld_w, sizeof(E));
     h.m = a.h, h.ld = a.ld_h, h.count = a.n, h.tiles = c0 == 0 ? p.rows_pad / kSmTile : 0;
     h.out = a.ws + p.h, h.vec = fours(a.h, a.ld_h, sizeof(E));
-    k_sm_pack<E><<<dim3((uint32_t)(w.tiles + h.tiles)), kBlock, 0, s>>>(a, w, h, p.dp / 16, forms);
-    return hipGetLastError();
+    return in_launches(w.tiles + h.tiles, [&](dim3 grid, int64_t first) {
+        k_sm_pack<E><<<grid, kBlock, 0, s>>>(a, w, h, p.dp / 16, forms, first);
+    });
 }
 
 // The loss of few rows: up to 64 whose operands fit kFewLds.  Above that the tables'
@@ -1521,9 +1539,11 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
         SM_TRY(lse_pass<E>(p, l, true, &slots, s));
     }
     if (a.n < 4096)
-        k_sm_loss<E, 64><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, pad);
+        k_sm_loss<E, 64><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, pad, 0);
     else
-        k_sm_loss<E, 16><<<dim3((uint32_t)div_up(a.n, 16)), kBlock, 0, s>>>(a, part, (int)slots, pad);
+        SM_TRY(in_launches(div_up(a.n, 16), [&](dim3 grid, int64_t first) {
+            k_sm_loss<E, 16><<<grid, kBlock, 0, s>>>(a, part, (int)slots, pad, first);
+        }));
     SM_TRY(hipGetLastError());
     if (a.loss_sum != nullptr) {
         k_sm_sum<<<1, 1024, 0, s>>>(a.loss, a.n, a.loss_sum);
@@ -1554,9 +1574,9 @@ JoinArgs to_join(const SoftmaxPlan& p, const float* part, const Layout& lay, int
 template <typename E>
 hipError_t join(const SoftmaxPlan& p, const JoinArgs& a, const JoinArgs& b, float scale,
                 hipStream_t s) {
-    if (a.blocks + b.blocks == 0) return hipSuccess;
-    k_sm_join<E><<<dim3((uint32_t)(a.blocks + b.blocks)), kBlock, 0, s>>>(a, b, p.dp, p.dim, scale);
-    return hipGetLastError();
+    return in_launches(a.blocks + b.blocks, [&](dim3 grid, int64_t first) {
+        k_sm_join<E><<<grid, kBlock, 0, s>>>(a, b, p.dp, p.dim, scale, first);
+    });
 }
 
 template <typename E>
