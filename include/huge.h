@@ -545,8 +545,8 @@ huge_status huge_softmax_grad(const huge_softmax_config* cfg, const void* d_h, i
      m' = beta1 m + (1 - beta1) g, v' = beta2 v + (1 - beta2) g g,  g = grad_scale grad
      param = param (1 - lr weight_decay)
              - (m' lr / (1 - beta1^step)) / (sqrt(v') / sqrt(1 - beta2^step) + eps)
-   An element whose m' or v' is not finite keeps its param, m and v, and
-   HUGE_ERR_NOT_FINITE is written to d_status.
+   An element whose m', v' or new parameter (in its type) is not finite keeps its
+   param, m and v, and HUGE_ERR_NOT_FINITE is written to d_status.
    States: HUGE_STATE_F32 keeps m and v as floats.  HUGE_STATE_Q8 keeps them
    in 8 bits, in blocks of 256 consecutive elements of a tensor: m as
    s sgn(q) (q / 127)^2 with q in -127 .. 127 and s the block's largest |m|,

@@ -75,18 +75,21 @@ def adamw(p, g, m, v, step, lr, beta1, beta2, eps, weight_decay, grad_scale=1.0)
     return p - lr * (mh / (np.sqrt(vh) + eps) + weight_decay * p), m, v
 
 
-def adamw_f32(p, g, m, v, step, lr, beta1, beta2, eps, weight_decay, grad_scale=1.0):
+def adamw_f32(p, g, m, v, step, lr, beta1, beta2, eps, weight_decay, grad_scale=1.0,
+              largest=np.float32(np.inf)):
     """The same with every product and sum rounded to float32, in the order of
-    include/huge.h: the kernels' states are these bit for bit."""
+    include/huge.h: the kernels' states are these bit for bit.  An element keeps its
+    values where one of the new ones is not finite (the parameter: not below `largest`,
+    which a narrower type of parameters rounds to infinity)."""
     f = np.float32
     p, g, m, v = (np.asarray(t, f) for t in (p, g, m, v))
     with np.errstate(over="ignore", invalid="ignore"):
         g = g * f(grad_scale)
         mn = m * f(beta1) + g * f(1 - beta1)
         vn = v * f(beta2) + (g * g) * f(1 - beta2)
-        ok = np.isfinite(mn) & np.isfinite(vn)
         rate, fix = f(lr / (1 - beta1 ** step)), f(1 / np.sqrt(1 - beta2 ** step))
         new = p * f(1 - lr * weight_decay) - (mn * rate) / (np.sqrt(vn) * fix + f(eps))
+        ok = np.isfinite(mn) & np.isfinite(vn) & (np.abs(new) < largest)
     return np.where(ok, new, p), np.where(ok, mn, m), np.where(ok, vn, v), ok
 
 

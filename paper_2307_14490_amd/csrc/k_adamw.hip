@@ -212,24 +212,31 @@ __device__ __forceinline__ bool update_chunk(const AdamArgs& a, const AdamTensor
             low = min(low, vb - 1u);
         }
         constexpr uint32_t kInf = 0x7F800000u, kLeast = (127u - 100u) << 23;
-        if (__ballot(top >= kInf || low < kLeast - 1u) == 0) {
+        // the new parameter: from half a step above the largest bf16 it would be infinite
+        constexpr uint32_t kTop = sizeof(P) == 2 ? 0x7F7F8000u : kInf;
+        float y[4];
+        uint32_t far = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                m[e] = mn[e];
-                v[e] = vn[e];
-                r[e] = root(v[e]);
-                x[e] = x[e] * a.keep - quotient(m[e] * a.rate, r[e] * a.fix + a.eps);
-            }
+        for (int e = 0; e < 4; ++e) {
+            r[e] = root(vn[e]);
+            y[e] = x[e] * a.keep - quotient(mn[e] * a.rate, r[e] * a.fix + a.eps);
+            far = max(far, __float_as_uint(fabsf(y[e])));
+        }
+        if (__ballot(top >= kInf || low < kLeast - 1u || far >= kTop) == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = mn[e], v[e] = vn[e], x[e] = y[e];
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
+                const float rn = sqrtf(vn[e]);
+                const float z = x[e] * a.keep - (mn[e] * a.rate) / (rn * a.fix + a.eps);
                 // |.| < inf is false for NaN too
-                const bool ok = fabsf(mn[e]) < INFINITY && vn[e] < INFINITY;
-                v[e] = ok ? vn[e] : v[e];
-                r[e] = sqrtf(v[e]);
-                const float step = (mn[e] * a.rate) / (r[e] * a.fix + a.eps);
-                x[e] = ok ? x[e] * a.keep - step : x[e];
+                const bool ok = fabsf(mn[e]) < INFINITY && vn[e] < INFINITY &&
+                                fabsf(z) < __uint_as_float(kTop);
+                r[e] = ok ? rn : sqrtf(v[e]);
                 m[e] = ok ? mn[e] : m[e];
+                v[e] = ok ? vn[e] : v[e];
+                x[e] = ok ? z : x[e];
                 bad |= !ok && (FULL || i + e < n);
             }
         }
