@@ -577,7 +577,7 @@ typedef struct huge_adamw_config {
 size_t huge_adamw_state_bytes(int64_t n, int32_t state_kind);
 
 /* One step over h_tensors[0 .. count) (a host array, read before the call
-   returns). */
+   returns), whose memory must not overlap. */
 huge_status huge_adamw_step(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
                             int32_t count, int32_t* d_status, void* stream);
 

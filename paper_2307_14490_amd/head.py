@@ -284,8 +284,10 @@ class SoftmaxLoss(_Status):
 # --------------------------------------------------------------------------- #
 class AdamW(_Status):
     """AdamW over a list of contiguous float32 or bfloat16 GPU tensors of one
-    device, updated in place by huge_adamw_step.  states: "f32", or "q8" for
-    moments in 8 bits.  The parameters' storage must stay where it is."""
+    device that share no memory, updated in place by huge_adamw_step.  states:
+    "f32", or "q8" for moments in 8 bits.  The parameters' storage must stay where
+    it is.  bfloat16 parameters have no copy in 32 bits: a step below half of their
+    last bit, 2^-9 to 2^-8 of the value, does not move them."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
                  states="f32"):
@@ -300,6 +302,10 @@ class AdamW(_Status):
             if p.device != self.params[0].device:
                 raise ValueError(f"AdamW params[{k}]: on {p.device}, expected "
                                  f"{self.params[0].device}")
+        ends = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size())
+                      for p in self.params if p.numel())
+        if any(a[1] > b[0] for a, b in zip(ends, ends[1:])):
+            raise ValueError("AdamW: parameters that share memory")
         super().__init__(self.params[0].device)
         self.steps = 0
         self.lr = float(lr)

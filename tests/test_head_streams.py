@@ -146,3 +146,13 @@ def test_capture_on_a_stream_of_its_own(order):
     a.capturing = b.capturing = False
     op.loss(x, w, lab)
     op.check()
+
+
+def test_parameters_that_share_memory_are_refused(order):
+    """One launch updates all: elements listed twice would be read and written by two
+    workgroups at once."""
+    t = torch.zeros(300)
+    for params in ([t, t], [t[:200], t[199:]], [t[100:101], torch.zeros(5), t]):
+        with pytest.raises(ValueError):
+            P.AdamW(params)
+    P.AdamW([t[:200], t[200:], torch.zeros(0), torch.zeros(0)])
