@@ -1472,12 +1472,11 @@ hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t 
 }
 
 // The loss of few rows: up to 64 whose operands fit kFewLds.  Above that the tables'
-// packing is paid for by the faster products.
+// packing is paid for by the faster products.  Where n rows are few, fewer are too.
 template <typename E>
-int few_blocks(const SoftmaxArgs& a) {
+int few_blocks(int64_t n, int32_t dim) {
     for (int nb = 1; nb <= 4; nb <<= 1)
-        if (a.n <= 16 * nb)
-            return div_up(a.dim, Few<E>::kCols) * nb * 1024 <= kFewLds<E> ? nb : 0;
+        if (n <= 16 * nb) return div_up(dim, Few<E>::kCols) * nb * 1024 <= kFewLds<E> ? nb : 0;
     return 0;
 }
 
@@ -1511,7 +1510,7 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
     };
     a.vec16 = a.dim % kN == 0 && sixteen(a.h, a.ld_h) && sixteen(a.w, a.ld_w);
     int64_t slots = 0, pad = p.rows_pad;
-    const int few = few_blocks<E>(a);
+    const int few = few_blocks<E>(a.n, a.dim);
     if (few != 0) {
         pad = 16 * few;
         SM_TRY((few == 1   ? few_pass<E, 1>(a, part, &slots, s)
@@ -1650,8 +1649,11 @@ SoftmaxPlan softmax_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype,
         off += ((size_t)bytes + 255) & ~(size_t)255;
         return o;
     };
-    p.h = take(p.rows_pad / kSmTile * rec);
-    p.w = take(p.piece / kSmTile * rec);
+    // losses of few rows pack nothing
+    const bool packs = grad || (dtype == kDtypeBf16 ? few_blocks<bf16_t>(n, dim)
+                                                    : few_blocks<float>(n, dim)) == 0;
+    p.h = take(packs ? p.rows_pad / kSmTile * rec : 0);
+    p.w = take(packs ? p.piece / kSmTile * rec : 0);
     const int64_t rows = p.rows_pad > kSmPartRows ? p.rows_pad : kSmPartRows;
     p.part = take(grad ? 4 * kSmPartRows * (int64_t)(p.dp + 1) : 8 * rows);
     p.row_part = take(grad ? 4 * rows * (int64_t)p.dp : 0);

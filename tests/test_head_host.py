@@ -155,3 +155,28 @@ def test_adamw_state_calls_refuse():
         assert fn(ts, 1, 7, good, good, None) == B.HUGE_ERR_INVALID_ARG
         assert fn(ts, 1, 0, None, good, None) == B.HUGE_ERR_INVALID_ARG
         assert fn(None, 1, 0, good, good, None) == B.HUGE_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype,rows,dim", [(0, 1, 128), (0, 64, 512), (0, 16, 1024), (1, 64, 448),
+                                            (1, 1, 1024)])
+def test_losses_of_few_rows_keep_no_copy_of_the_table(dtype, rows, dim):
+    """They read it as it lies: what is left are the partial sums."""
+    size = lambda **kw: P.load().huge_softmax_workspace_bytes(  # noqa: E731
+        ctypes.byref(_soft(num_classes=1_000_000, dim=dim, dtype=dtype, **kw)))
+    assert 0 < size(max_rows=rows, grad=0) <= 8 * 131072
+    assert size(max_rows=65, grad=0) > 2 * 10 ** 8 < size(max_rows=rows, grad=1)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_softmax_workspace_never_shrinks_with_rows(dtype):
+    """A call of fewer rows than planned needs no more, a loss no more than a gradient."""
+    for dim in (4, 32, 128, 260, 384, 388, 512, 772, 1024):
+        for classes in (1, 50_021, 3_000_000):
+            last = {0: 0, 1: 0}
+            for rows in (1, 16, 17, 32, 33, 64, 65, 4096, 131072, 200_000):
+                for grad in (0, 1):
+                    now = P.load().huge_softmax_workspace_bytes(ctypes.byref(
+                        _soft(num_classes=classes, dim=dim, dtype=dtype, max_rows=rows, grad=grad)))
+                    assert now >= last[grad]
+                    last[grad] = now
+                assert last[0] <= last[1]
