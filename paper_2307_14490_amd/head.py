@@ -72,6 +72,11 @@ def _current(device):
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _same_device(stream, device):
+    if stream.device != device:
+        raise ValueError(f"stream: of {stream.device}, expected {device}")
+
+
 class _on:
     """``with _on(device, stream, tensors) as pointer``: the device is current, and
     the pointer is the stream to launch on.  With a stream of the caller's, what is
@@ -89,6 +94,7 @@ class _on:
         if torch.cuda.current_device() != self.device.index:
             self.guards.append(torch.cuda.device(self.device))
         if self.stream is not None:
+            _same_device(self.stream, self.device)
             self.guards.append(torch.cuda.stream(self.stream))
         for g in self.guards:
             g.__enter__()
@@ -134,6 +140,7 @@ class _Status:
         now = _current(self.device) if stream is None else stream.cuda_stream
         if now != self._last_ptr:
             stream = torch.cuda.current_stream(self.device) if stream is None else stream
+            _same_device(stream, self.device)
             # a graph waits for nothing outside of it: what came before its capture is
             # done when that begins, and its replays are the caller's to order
             if not _capturing(stream) or _capturing(self._last):

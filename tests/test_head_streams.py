@@ -156,3 +156,20 @@ def test_parameters_that_share_memory_are_refused(order):
         with pytest.raises(ValueError):
             P.AdamW(params)
     P.AdamW([t[:200], t[200:], torch.zeros(0), torch.zeros(0)])
+
+
+def test_a_stream_of_another_device_is_refused(order):
+    """Before anything is launched or allocated there."""
+    far = order.stream()
+    order.seen.append(far)
+    far.device = torch.device("cuda", 1)
+    x, lab = batch(order, order.default)
+    g = torch.ones(8)
+    head = P.SoftmaxHead(5, 8, 6)
+    opt = P.AdamW([torch.zeros(6, 8)])
+    for call in (lambda: P.layer_norm(x, g, g, stream=far), lambda: head.loss(x, lab, stream=far),
+                 lambda: head.step(x, lab, stream=far), lambda: opt.step([x], stream=far),
+                 lambda: opt.values(stream=far), lambda: head.op.loss(x, x[:5], lab, stream=far)):
+        with pytest.raises(ValueError):
+            call()
+    assert not far.clock and opt.steps == 0
