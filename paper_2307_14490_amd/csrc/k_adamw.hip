@@ -7,8 +7,9 @@
 // scales are a maximum over the wave's registers.  Bound by memory: 129 million
 // fp32 elements with fp32 moments take 680 us, 28 bytes each, 5.3 TB/s (a copy
 // reaches 4.8).  256 million bf16 ones with moments in 8 bits move 10 bytes each and
-// take 604 us, 4.3 TB/s: there the vector work of the exact roots and quotients and
-// of the codes shows (0.4 of the time of four fp32 elements).  Reading the
+// take 603 to 630 us, 4.2 TB/s: there the vector work of the exact roots and quotients and
+// of the codes shows (0.4 of the time of four fp32 elements; the test of the new
+// parameter is 3 to 5% of the whole).  Reading the
 // moments out takes 466 us, 10 bytes an element, 5.5 TB/s.  A table of up to 64
 // tensors goes in the kernel's arguments: four small tensors are one launch of 3 us.
 //

@@ -12,7 +12,7 @@
 //
 // Measured, bytes that have to be moved over time (a copy reaches 4.8 TB/s): 262144
 // x 256 fp32 95 us forward (5.6 TB/s), 157 us backward (5.1) and 5 us for the second
-// kernel; 65536 x 128 bf16, which stays in the caches, 11, 12 and 5 us.  Rows that
+// kernel; 65536 x 128 bf16, which stays in the caches, 12, 13 and 5 us.  Rows that
 // are not whole aligned fours: 60417 x 761 both ways 188 us in fp32 (4.9 TB/s, as
 // with 760 columns), 154 us in bf16 (3.0; 760 columns: 101 us), where an 8-byte
 // access at an odd address is taken apart; one element a thread took 279 us.  Rows

@@ -28,7 +28,10 @@
 // Precision.  bf16 rows enter as they are, and the tile is rounded to bf16 after
 // the label is subtracted, so that a probability near one keeps its small
 // complement: an error of 2^-8 of each term at most, as in the rounding of the
-// result.  fp32 rows are scaled by a power of two per row and split into two fp16
+// result (2.0e-3 to 2.3e-3 of the gradients' norm in all, of which that rounding
+// alone is 1.7e-3).  Two bf16 parts of the tile would leave the latter only, for a
+// second product twice as long: 4096 x 1e6 x 128 3731 -> 5197 us, 100003 x 1000 x
+// 128 164 -> 199, 4096 x 50021 x 384 728 -> 904.  fp32 rows are scaled by a power of two per row and split into two fp16
 // parts, hi + lo (22 bits of an element within 2^-17 of the row's largest, and
 // 2^-40 of that for smaller ones), and the products hi hi + hi lo + lo hi are
 // summed in fp32; the tile is split the same way under a scale per X row that
@@ -572,12 +575,11 @@ __device__ __forceinline__ float exp_below(float a, float b) {
 
 constexpr float kRise = 8.f;
 
-//
 // Bound by the vector units, which take the exponential, its argument and the sum of
-// every element: 4096 x 1e6 x 128 bf16 985 to 1040 us from records (1.0 PFLOP/s; 72%
-// of the time a SIMD issues vector instructions, 52% its matrix core works), 985 to
-// 1155 us from the rows as they lie, which saves the packing (70 us and a pass over
-// the table).  3001 x 50021 x 256 fp32: 210 us, 366 TFLOP/s.
+// every element: 4096 x 1e6 x 128 bf16 from records 960 to 1040 us (1.0 PFLOP/s; 72%
+// of the time a SIMD issues vector instructions, 52% its matrix core works), by the
+// clock, which falls under it.  3001 x 50021 x 256 fp32: 194 to 204 us, 377 to 396
+// TFLOP/s.
 template <typename E, int ND, int XB, int WAVES, int OCC, bool STAGED, bool DIRECT>
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void k_sm_lse(PassArgs a) {
@@ -681,7 +683,8 @@ void k_sm_lse(PassArgs a) {
 // of a 16x16 product as they lie (fp32: exact fp32 products); the rows h are the
 // other operand, from LDS.  A lane then holds four classes' logits of one row.
 // Loads run one group of kFewGroup operands ahead.  One row is bound by memory: 1e6 x
-// 128 fp32 take 87 us of the kernel, 5.9 TB/s.  From 33 rows up the exact fp32
+// 128 fp32 take 87 us of the kernel, 5.9 TB/s; up to 16 rows' whole call 100 us (bf16
+// 54), 64 rows of bf16 67.  From 33 rows up the exact fp32
 // products bind, 64 x 300000 x 256 at 69 TFLOP/s with the host's work.
 //
 // h takes LDS, up to kFewLds, and so leaves a CU one workgroup where it is wide: four
@@ -1183,13 +1186,14 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
 // share the card with the other's first.
 //
 // Bound by the matrix cores and what stands between their products.  4096 x 1e6 x
-// 128 bf16: 3760 us, 1.12 PFLOP/s over the four products (S twice); the matrix cores
+// 128 bf16: 3540 to 3730 us by machine and data, 1.12 to 1.18 PFLOP/s over the four
+// products (S twice); the matrix cores
 // are busy 61% of the time, a SIMD issues vector instructions for another 47% of it
 // (they overlap across three waves), and the clock stands at about 1.8 GHz under
 // that load: the same calls on zeros take 22% less.  A library product of bf16
 // matrices of 8192 reaches 1.4 to 1.6 PFLOP/s.  fp32, three products of halves for
-// each: 3001 x 50021 x 256 about 1000 us, 310 TFLOP/s (the library's fp32 product:
-// 154).  One wave per SIMD is all that X and the sums leave there, so that the
+// each: 3001 x 50021 x 256 1046 to 1196 us, 257 to 294 TFLOP/s (the library's fp32
+// product: 154).  One wave per SIMD is all that X and the sums leave there, so that the
 // exponentials run with the matrix cores idle: 42% busy.
 //
 // Measured against: workgroups of 4 waves with 128-column bf16 rows, dw and dh 2054 and
@@ -1296,7 +1300,8 @@ constexpr int64_t kCus = 256;
 // least `least` tiles a wave; there are at most kSmPartRows partial rows (or one
 // slot's).  Of the numbers of splits, the fewest that come within 3% of the
 // shortest: r workgroups of 1 / s each take ceil(r s / places) / s, and a start that
-// costs about as much as four tiles.
+// costs about as much as four tiles.  Each gradient is laid out as if it had the card
+// to itself, though both share a launch and one's end overlaps the other's start.
 Layout lay_out(int64_t x_tiles, int64_t y_tiles, int xb, int waves, int resident, int rec_bytes,
                bool staged, bool whole, int least) {
     Layout l{};
@@ -1517,7 +1522,13 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
                 : few == 2 ? few_pass<E, 2>(a, part, &slots, s)
                            : few_pass<E, 4>(a, part, &slots, s)));
     }
-    // bf16 classes without a bias whose rows are whole operands are used as they lie
+    // bf16 classes without a bias whose rows are whole operands are used as they lie:
+    // no packing, for addresses per operand in a kernel that the vector units bind (1031
+    // to 1131 us for 4096 x 1e6 x 128 against 960 to 1040).  Whole calls on one machine,
+    // as they lie / through records: 4096 rows of that 1015 / 1104 us, 1024 rows 275 /
+    // 390, 96 rows 82 / 207; 4096 x 50021 x 256 110 / 118.  The rows' share grows with
+    // n: 8192 x 50021 x 128 119 / 123 us, x 512 397 / 382, 32768 x 50021 x 128 419 / 412,
+    // x 512 1495 / 1386.
     const bool direct = few == 0 && sizeof(E) == 2 && a.bias == nullptr && a.vec16 &&
                         p.chunks == 1 && a.dim == p.dp;
     if (direct) {
@@ -1537,7 +1548,10 @@ hipError_t softmax_loss(SoftmaxArgs a, hipStream_t s) {
         l.first = c0 == 0, l.lse_part = part;
         SM_TRY(lse_pass<E>(p, l, true, &slots, s));
     }
-    if (a.n < 4096)
+    // a wave a row until there are four for each SIMD, then 16 lanes.  16 / 64 lanes:
+    // 256 rows behind 50021 classes of 128 fp32 columns 10.2 / 4.6 us, 1024 5.9 / 4.2, 4000 4.1
+    // / 4.5 (of 384 bf16 columns 7.0 / 5.2), 16384 behind 1000 4.4 / 9.0, 100003 13.0 / 46.9
+    if (a.n < 16 * kCus)
         k_sm_loss<E, 64><<<dim3((uint32_t)div_up(a.n, 4)), kBlock, 0, s>>>(a, part, (int)slots, pad, 0);
     else
         SM_TRY(in_launches(div_up(a.n, 16), [&](dim3 grid, int64_t first) {
@@ -1564,7 +1578,9 @@ JoinArgs to_join(const SoftmaxPlan& p, const float* part, const Layout& lay, int
     j.vec = fours(j.out, 0, sizeof(E));
     j.slots = (int32_t)lay.slots;
     const int64_t work = out != nullptr ? j.rows * (p.dim / 4) : j.rows;
-    // few outputs of many slots: 16 threads each
+    // few outputs of many slots: 16 threads each.  Both joins of 100003 x 100 x 32 bf16
+    // take 8 us, 52 with one thread each; of 16384 x 1000 x 128 11 us, 16 with one each
+    // and 29 with 16 each; of 8192 x 8192 x 64, where it errs, 15 with 12 and 15
     j.lanes = work < (1 << 18) && lay.slots >= 16 ? 16 : 1;
     j.blocks = div_up(work * j.lanes, kBlock);
     return j;

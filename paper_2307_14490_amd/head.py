@@ -9,6 +9,8 @@ given keeps the arguments until the call's work on it is done; on the current
 one torch's own rule holds, that who uses a tensor of another stream there
 records it.  What the classes hold is kept on either.
 Errors that only the device can see are kept in a status word until ``check``.
+Nothing here is part of torch's autograd: results do not require a gradient,
+also where arguments do; the gradients are calls of their own.
 """
 from __future__ import annotations
 
