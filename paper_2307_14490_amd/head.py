@@ -369,7 +369,8 @@ class AdamW(_Status):
         return ts
 
     def step(self, grads, lr=None, grad_scale=1.0, stream=None):
-        """One step with these gradients (float32 or bfloat16, one per parameter)."""
+        """One step with these gradients (float32 or bfloat16, one per parameter).  In
+        a graph's capture its learning rate and bias corrections are recorded too."""
         grads = self._list(grads, ("float32", "bfloat16"), "AdamW.step grads")
         c = self.cfg
         c.lr = self.lr if lr is None else float(lr)
