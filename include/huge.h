@@ -618,6 +618,154 @@ huge_status huge_adamw_set_state(const huge_adamw_tensor* h_tensors, int32_t cou
                                  int32_t state_kind, const float* const* h_m,
                                  const float* const* h_v, void* stream);
 
+/* RMS norm of n rows, 1 <= dim <= 8192, with the residual's addition:
+     total = x + residual, rounded to `dtype` (without a residual: x),
+     rstd = 1 / sqrt(sum total^2 / dim + eps), y = total rstd gamma.
+     d_x                : rows of `dtype`
+     d_residual, d_total: rows of `dtype`, both or neither NULL.  d_total may be
+                          the array of d_x or of d_residual (at its stride)
+     d_gamma            : dim floats
+     d_y                : rows of `dtype`, which may be the array of d_x if there
+                          is no residual; or NULL, and y in 8 bits to
+     d_codes, d_scales  : as huge_quantise_rows writes them from the y in 32 bits
+     d_rstd             : n floats, or NULL
+   eps > 0.  Squares are summed in fp32: a row whose sum of them passes 3.4e38 has
+   rstd 0. */
+huge_status huge_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual,
+                          int64_t n, int32_t dim, int32_t dtype, const float* d_gamma, float eps,
+                          void* d_total, int64_t ld_total, void* d_y, int64_t ld_y,
+                          uint8_t* d_codes, int64_t ld_codes, uint8_t* d_scales, int64_t ld_scales,
+                          float* d_rstd, void* stream);
+
+/* Its gradient, with z = total rstd and a = dy gamma:
+     dx = dtotal + rstd (a - z sum (a z) / dim), which is the gradient of x and of
+     the residual, dgamma = sum over rows of dy z.
+     d_dtotal           : rows, the gradient that reaches total past the norm, or NULL
+     d_dx               : rows, which may be the array of d_dy or d_dtotal, or NULL
+     d_dgamma           : dim floats, or NULL.  n = 0 writes zeros
+   d_workspace (for dgamma): huge_rms_norm_workspace_bytes(n, dim) bytes, 16-byte
+   aligned. */
+size_t huge_rms_norm_workspace_bytes(int64_t n, int32_t dim);
+huge_status huge_rms_norm_backward(const void* d_dy, int64_t ld_dy, const void* d_total,
+                                   int64_t ld_total, const void* d_dtotal, int64_t ld_dtotal,
+                                   int64_t n, int32_t dim, int32_t dtype, const float* d_gamma,
+                                   const float* d_rstd, void* d_dx, int64_t ld_dx, float* d_dgamma,
+                                   void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Rows in 8 bits (HUGE_DTYPE_Q8): dim codes of e4m3 (sign, 4 bits of exponent, 3 of
+   mantissa, no infinity, 448 the largest) at a stride of ld_codes >= dim bytes,
+   and ceil(dim / 32) scales at a stride of ld_scales bytes, one for each 32
+   columns: a byte b stands for 2^(b - 127), 255 for NaN.  huge_quantise_rows takes
+   the smallest power, 2^-100 or more, under which no element of the block is above
+   448, and the nearest code, ties to even: an error of 2^-4 of an element at most,
+   or of 2^-10 of the scale where that is more, which is below 2^-17 of the block's
+   largest element (or 2^-110).  A block with an infinity or a NaN is NaN.  1 <= dim <= 8192.
+   huge_dequantise_rows gives the values, which bf16 holds exactly for scales from
+   2^-117 to 2^119 (one above 248 2^120 is nearest to 2^128, an infinity in 32 bits). */
+#define HUGE_DTYPE_Q8 2
+huge_status huge_quantise_rows(const void* d_x, int64_t ld_x, int64_t n, int32_t dim, int32_t dtype,
+                               uint8_t* d_codes, int64_t ld_codes, uint8_t* d_scales,
+                               int64_t ld_scales, void* stream);
+huge_status huge_dequantise_rows(const uint8_t* d_codes, int64_t ld_codes, const uint8_t* d_scales,
+                                 int64_t ld_scales, int64_t n, int32_t dim, void* d_y, int64_t ld_y,
+                                 int32_t dtype, void* stream);
+
+typedef struct huge_log_probs_config {
+    int64_t num_classes; /* V: rows of the output table, 1 .. 2^31-1                   */
+    int64_t max_rows;    /* largest n per call, 1 .. 2^31-1                            */
+    int32_t dim;         /* D: multiple of 4, 4 .. 1024                                */
+    int32_t dtype;       /* of h and of the gradients                                  */
+    int32_t table_dtype; /* of w: dtype, or HUGE_DTYPE_Q8 with h in bf16 (no gradient) */
+    int32_t top;         /* most likely classes to find, 0 .. min(V, 64)               */
+    int32_t grad;        /* 1: the workspace also serves huge_log_probs_grad           */
+} huge_log_probs_config;
+
+/* Bytes of device workspace of the two calls below (256-byte aligned); 0 if the
+   config is invalid.  It holds what huge_softmax_loss packs and, with top > 0, the
+   largest logit of each tile of 16 or 32 classes, for as many rows and classes at a time as
+   take 1 GiB. */
+size_t huge_log_probs_workspace_bytes(const huge_log_probs_config* cfg);
+
+/* Log probabilities, entropies and the most likely classes of n rows h (n x D) over
+   all rows of w (V x D), without keeping the n x V logits:
+     x_ij = <h_i, w_j> + bias_j, lse_i = log sum_j exp x_ij, p_ij = exp(x_ij - lse_i),
+     logp_i = x_ij - lse_i with j = label_i, entropy_i = - sum_j p_ij log p_ij.
+     d_w        : V x D of dtype, or codes, with d_w_scales (NULL otherwise)
+     d_bias     : V floats, or NULL (zeros).  A bias below -1e28 takes a class out, be
+                  it -inf or a type's lowest value: it counts in no sum, is not found,
+                  and nothing in its row of w, NaN included, is used
+     d_labels   : n int32 classes, -1 = no label; or NULL
+     d_logp     : n floats (NULL without labels).  0 without a label, -inf where the
+                  label is out
+     d_entropy  : n floats, or NULL
+     d_lse      : n floats
+     d_ids, d_top_logp : n x top, the classes of the largest logits, the largest first
+                  and the lowest class first among equals, and their log probabilities
+                  (NULL with top = 0).  -1 and -inf behind the last class that is in
+   Logits are below 1e28 in magnitude.  Where every class is out, lse is -inf, the entropy 0
+   and no class is found; where lse is no finite number (a NaN or an infinity in h, or in a
+   class that counts) ids are -1 and the rest NaN.
+   Sums, maxima and exponentials are fp32 on logits as in huge_softmax_loss.  The classes
+   found, and the order among them, are those of logits in fp64 (from the stored values), formed
+   again for all classes of the top + 4 tiles of 16 or 32 classes with the largest logits:
+   a class is missed only if more than 4 tiles' largest are within a rounding of the logits of
+   the last one found.  logp is from an fp64 logit as well.
+   A label outside [-1, V) writes HUGE_ERR_ID_OUT_OF_RANGE to d_status, and its logp is
+   NaN. */
+huge_status huge_log_probs(const huge_log_probs_config* cfg, const void* d_h, int64_t ld_h,
+                           int64_t n, const void* d_w, int64_t ld_w, const uint8_t* d_w_scales,
+                           int64_t ld_scales, const float* d_bias, const int32_t* d_labels,
+                           float* d_logp, float* d_entropy, float* d_lse, int32_t* d_ids,
+                           float* d_top_logp, int32_t* d_status, void* d_workspace, size_t ws_bytes,
+                           void* stream);
+
+/* The gradient of sum_i dlogp_i logp_i + dentropy_i entropy_i, of either sign:
+     g_ij = dlogp_i ([j = label_i] - p_ij) - dentropy_i p_ij (log p_ij + entropy_i),
+     dh_i = sum_j g_ij w_j, dw_j = sum_i g_ij h_i, dbias_j = sum_i g_ij.
+     d_lse, d_entropy : as huge_log_probs wrote them for the same inputs (d_entropy may
+                        be NULL without d_dentropy)
+     d_dlogp          : n floats, or NULL (zeros; labels may then be NULL).  Counts as 0 for
+                        a row without a label or whose label is out
+     d_dentropy       : n floats, or NULL (zeros)
+     d_dh, d_dw, d_dbias : as in huge_softmax_grad
+   A row whose weights are 0, or which has no class, has no gradient, whatever its h
+   holds.  Roundings, time and the status are those of huge_softmax_grad. */
+huge_status huge_log_probs_grad(const huge_log_probs_config* cfg, const void* d_h, int64_t ld_h,
+                                int64_t n, const void* d_w, int64_t ld_w, const float* d_bias,
+                                const int32_t* d_labels, const float* d_lse, const float* d_entropy,
+                                const float* d_dlogp, const float* d_dentropy, void* d_dh,
+                                void* d_dw, float* d_dbias, int32_t* d_status, void* d_workspace,
+                                size_t ws_bytes, void* stream);
+
+typedef struct huge_grad_tensor {
+    void* d_grad;   /* n elements of dtype            */
+    int64_t n;      /* 0 .. 2^40                      */
+    int32_t dtype;  /* HUGE_DTYPE_F32 or HUGE_DTYPE_BF16 */
+} huge_grad_tensor;
+
+/* The 2-norm over all elements of h_tensors[0 .. count) (a host array, read before
+   the call returns), summed in fp64 and rounded to the float d_norm.  d_workspace:
+   huge_grad_norm_workspace_bytes(count) bytes, 16-byte aligned. */
+size_t huge_grad_norm_workspace_bytes(int32_t count);
+huge_status huge_grad_norm(const huge_grad_tensor* h_tensors, int32_t count, float* d_norm,
+                           void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Scales all elements by max_norm / norm where the norm is above max_norm > 0 (which may
+   be infinite), in place; d_norm, or NULL, receives the norm before.  The tensors must
+   not overlap, and stay as they are where the norm is not finite. */
+huge_status huge_clip_grads(const huge_grad_tensor* h_tensors, int32_t count, double max_norm,
+                            float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* huge_adamw_step with gradients so clipped: in place of grad_scale they are multiplied
+   by grad_scale or, where the norm of all grad_scale g is above max_norm > 0, by grad_scale
+   max_norm / norm.  The gradients are not written.  d_norm, or NULL, receives the
+   norm of grad_scale g.  Where that is not finite no element moves, and
+   HUGE_ERR_NOT_FINITE is written to d_status.  d_workspace as for huge_grad_norm. */
+huge_status huge_adamw_step_clipped(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
+                                    int32_t count, double max_norm, float* d_norm,
+                                    int32_t* d_status, void* d_workspace, size_t ws_bytes,
+                                    void* stream);
+
 void huge_destroy(huge_handle* h);
 const char* huge_status_string(huge_status s);
 

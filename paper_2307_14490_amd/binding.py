@@ -29,6 +29,7 @@ HUGE_SCATTER_SORTED = 0
 HUGE_SCATTER_ATOMIC = 1
 HUGE_DTYPE_F32 = 0
 HUGE_DTYPE_BF16 = 1
+HUGE_DTYPE_Q8 = 2
 HUGE_STATE_F32 = 0
 HUGE_STATE_Q8 = 1
 
@@ -44,6 +45,11 @@ EXPORTED = [
     "huge_layer_norm", "huge_layer_norm_workspace_bytes", "huge_layer_norm_backward",
     "huge_softmax_workspace_bytes", "huge_softmax_loss", "huge_softmax_grad",
     "huge_adamw_state_bytes", "huge_adamw_step", "huge_adamw_get_state", "huge_adamw_set_state",
+    "huge_rms_norm", "huge_rms_norm_workspace_bytes", "huge_rms_norm_backward",
+    "huge_quantise_rows", "huge_dequantise_rows",
+    "huge_log_probs_workspace_bytes", "huge_log_probs", "huge_log_probs_grad",
+    "huge_grad_norm_workspace_bytes", "huge_grad_norm", "huge_clip_grads",
+    "huge_adamw_step_clipped",
 ]
 HUGE_PHASES = 6
 
@@ -104,6 +110,26 @@ class HugeAdamwConfig(ctypes.Structure):
         ("grad_scale", ctypes.c_double),
         ("step", ctypes.c_int64),
         ("state_kind", ctypes.c_int32),
+    ]
+
+
+class HugeLogProbsConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_classes", ctypes.c_int64),
+        ("max_rows", ctypes.c_int64),
+        ("dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("table_dtype", ctypes.c_int32),
+        ("top", ctypes.c_int32),
+        ("grad", ctypes.c_int32),
+    ]
+
+
+class HugeGradTensor(ctypes.Structure):
+    _fields_ = [
+        ("d_grad", ctypes.c_void_p),
+        ("n", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
     ]
 
 
@@ -199,6 +225,33 @@ def load() -> ctypes.CDLL:
     for name in ("huge_layer_norm", "huge_layer_norm_backward", "huge_softmax_loss",
                  "huge_softmax_grad", "huge_adamw_step", "huge_adamw_get_state",
                  "huge_adamw_set_state"):
+        getattr(L, name).restype = ctypes.c_int32
+    f64 = ctypes.c_double
+    L.huge_rms_norm.argtypes = [_vp, i64, _vp, i64, i64, i32, i32, _vp, f32, _vp, i64, _vp, i64,
+                                _vp, i64, _vp, i64, _vp, _vp]
+    L.huge_rms_norm_workspace_bytes.argtypes = [i64, i32]
+    L.huge_rms_norm_workspace_bytes.restype = szt
+    L.huge_rms_norm_backward.argtypes = [_vp, i64, _vp, i64, _vp, i64, i64, i32, i32, _vp, _vp,
+                                         _vp, i64, _vp, _vp, szt, _vp]
+    L.huge_quantise_rows.argtypes = [_vp, i64, i64, i32, i32, _vp, i64, _vp, i64, _vp]
+    L.huge_dequantise_rows.argtypes = [_vp, i64, _vp, i64, i64, i32, _vp, i64, i32, _vp]
+    lcfgp = ctypes.POINTER(HugeLogProbsConfig)
+    L.huge_log_probs_workspace_bytes.argtypes = [lcfgp]
+    L.huge_log_probs_workspace_bytes.restype = szt
+    L.huge_log_probs.argtypes = [lcfgp, _vp, i64, i64, _vp, i64, _vp, i64, _vp, _vp, _vp, _vp,
+                                 _vp, _vp, _vp, _vp, _vp, szt, _vp]
+    L.huge_log_probs_grad.argtypes = [lcfgp, _vp, i64, i64, _vp, i64, _vp, _vp, _vp, _vp, _vp,
+                                      _vp, _vp, _vp, _vp, _vp, _vp, szt, _vp]
+    gradsp = ctypes.POINTER(HugeGradTensor)
+    L.huge_grad_norm_workspace_bytes.argtypes = [i32]
+    L.huge_grad_norm_workspace_bytes.restype = szt
+    L.huge_grad_norm.argtypes = [gradsp, i32, _vp, _vp, szt, _vp]
+    L.huge_clip_grads.argtypes = [gradsp, i32, f64, _vp, _vp, szt, _vp]
+    L.huge_adamw_step_clipped.argtypes = [ctypes.POINTER(HugeAdamwConfig), tensorsp, i32, f64, _vp,
+                                          _vp, _vp, szt, _vp]
+    for name in ("huge_rms_norm", "huge_rms_norm_backward", "huge_quantise_rows",
+                 "huge_dequantise_rows", "huge_log_probs", "huge_log_probs_grad",
+                 "huge_grad_norm", "huge_clip_grads", "huge_adamw_step_clipped"):
         getattr(L, name).restype = ctypes.c_int32
     L.huge_destroy.argtypes = [_vp]
     L.huge_destroy.restype = None

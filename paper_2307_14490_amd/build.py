@@ -20,6 +20,7 @@ BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["api.hip", "api_head.hip", "k_tables.hip", "k_sort.hip", "k_step.hip", "k_atomic.hip", "k_walk.hip",
            "k_eval.hip", "k_norm.hip", "k_softmax.hip", "k_adamw.hip",
+           "api_answer.hip", "k_rms.hip", "k_answer.hip", "k_clip.hip",
            "alias.cpp"]
 ARCH = "gfx950"
 

@@ -3,30 +3,11 @@
 // to the next.
 #include <math.h>
 
-#include "../../include/huge.h"
-#include "head.hpp"
+#include "api_head.hpp"
 
 using namespace huge;
 
 namespace {
-
-constexpr int64_t kMaxRows = 0x7FFFFFFF;
-
-#define HEAD_TRY(expr)                                  \
-    do {                                                \
-        if ((expr) != hipSuccess) return HUGE_ERR_HIP;  \
-    } while (0)
-
-bool dtype_ok(int32_t t) { return t == HUGE_DTYPE_F32 || t == HUGE_DTYPE_BF16; }
-
-size_t elem(int32_t dtype) { return dtype == HUGE_DTYPE_BF16 ? 2 : 4; }
-
-bool on(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
-// Whether rows can be read four elements at a time.
-bool fours(const void* p, int64_t ld, int32_t dtype) {
-    return on(p, 4 * elem(dtype)) && ld % 4 == 0;
-}
 
 bool softmax_ok(const huge_softmax_config* c) {
     return c != nullptr && c->num_classes >= 1 && c->num_classes <= kMaxRows && c->max_rows >= 1 &&
@@ -110,6 +91,64 @@ huge_status state_call(const huge_adamw_tensor* ts, int32_t count, int32_t kind,
 }
 
 }  // namespace
+
+namespace huge {
+
+huge_status adamw_args(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
+                       int32_t count, const int32_t* d_status) {
+    if (!cfg || count < 0 || (count > 0 && !h_tensors) || !d_status || !on(d_status, 4) ||
+        !state_ok(cfg->state_kind) || cfg->step < 1 || !rate_ok(cfg->lr) ||
+        !rate_ok(cfg->weight_decay) || !isfinite(cfg->grad_scale) ||
+        !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) ||
+        !(cfg->eps >= 1e-30 && isfinite((float)cfg->eps)))
+        return HUGE_ERR_INVALID_ARG;
+    for (int32_t k = 0; k < count; ++k) {
+        const huge_adamw_tensor& t = h_tensors[k];
+        if (t.n < 0 || t.n > kAdamMaxElements || !dtype_ok(t.param_dtype) ||
+            !dtype_ok(t.grad_dtype) ||
+            (t.n > 0 && (!t.d_param || !t.d_grad || !t.d_state || !on(t.d_state, 16) ||
+                         !on(t.d_param, elem(t.param_dtype)) ||
+                         !on(t.d_grad, elem(t.grad_dtype)))))
+            return HUGE_ERR_INVALID_ARG;
+    }
+    return HUGE_OK;
+}
+
+huge_status adamw_step(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
+                       int32_t count, const float* d_factor, int32_t* d_status, void* stream) {
+    AdamArgs a{};
+    const double b1 = cfg->beta1, b2 = cfg->beta2, steps = (double)cfg->step;
+    a.beta1 = (float)b1, a.one_beta1 = (float)(1.0 - b1);
+    a.beta2 = (float)b2, a.one_beta2 = (float)(1.0 - b2);
+    a.rate = (float)(cfg->lr / (1.0 - pow(b1, steps)));
+    a.fix = (float)(1.0 / sqrt(1.0 - pow(b2, steps)));
+    a.eps = (float)cfg->eps;
+    a.keep = (float)(1.0 - cfg->lr * cfg->weight_decay);
+    a.grad_scale = (float)cfg->grad_scale;
+    a.factor = d_factor;
+    a.status = d_status;
+    for (int32_t types = 0; types < 4; ++types) {
+        const int32_t pt = types >> 1, gt = types & 1;
+        const huge_status st = in_launches(
+            a, count,
+            [&](int32_t k, AdamTensor& t) {
+                const huge_adamw_tensor& u = h_tensors[k];
+                if (u.param_dtype != pt || u.grad_dtype != gt) return false;
+                t.p = u.d_param, t.g = u.d_grad, t.n = u.n;
+                t.state = static_cast<uint8_t*>(u.d_state);
+                t.vec = on(u.d_param, 4 * elem(pt)) && on(u.d_grad, 4 * elem(gt));
+                return true;
+            },
+            [&](const AdamArgs& b, int64_t chunks) {
+                return launch_adamw(b, chunks, pt, gt, cfg->state_kind,
+                                    static_cast<hipStream_t>(stream));
+            });
+        if (st != HUGE_OK) return st;
+    }
+    return HUGE_OK;
+}
+
+}  // namespace huge
 
 extern "C" {
 
@@ -217,50 +256,8 @@ size_t huge_adamw_state_bytes(int64_t n, int32_t state_kind) {
 
 huge_status huge_adamw_step(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
                             int32_t count, int32_t* d_status, void* stream) {
-    if (!cfg || count < 0 || (count > 0 && !h_tensors) || !d_status || !on(d_status, 4) ||
-        !state_ok(cfg->state_kind) || cfg->step < 1 || !rate_ok(cfg->lr) ||
-        !rate_ok(cfg->weight_decay) || !isfinite(cfg->grad_scale) ||
-        !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) ||
-        !(cfg->eps >= 1e-30 && isfinite((float)cfg->eps)))
-        return HUGE_ERR_INVALID_ARG;
-    for (int32_t k = 0; k < count; ++k) {
-        const huge_adamw_tensor& t = h_tensors[k];
-        if (t.n < 0 || t.n > kAdamMaxElements || !dtype_ok(t.param_dtype) ||
-            !dtype_ok(t.grad_dtype) ||
-            (t.n > 0 && (!t.d_param || !t.d_grad || !t.d_state || !on(t.d_state, 16) ||
-                         !on(t.d_param, elem(t.param_dtype)) ||
-                         !on(t.d_grad, elem(t.grad_dtype)))))
-            return HUGE_ERR_INVALID_ARG;
-    }
-    AdamArgs a{};
-    const double b1 = cfg->beta1, b2 = cfg->beta2, steps = (double)cfg->step;
-    a.beta1 = (float)b1, a.one_beta1 = (float)(1.0 - b1);
-    a.beta2 = (float)b2, a.one_beta2 = (float)(1.0 - b2);
-    a.rate = (float)(cfg->lr / (1.0 - pow(b1, steps)));
-    a.fix = (float)(1.0 / sqrt(1.0 - pow(b2, steps)));
-    a.eps = (float)cfg->eps;
-    a.keep = (float)(1.0 - cfg->lr * cfg->weight_decay);
-    a.grad_scale = (float)cfg->grad_scale;
-    a.status = d_status;
-    for (int32_t types = 0; types < 4; ++types) {
-        const int32_t pt = types >> 1, gt = types & 1;
-        const huge_status st = in_launches(
-            a, count,
-            [&](int32_t k, AdamTensor& t) {
-                const huge_adamw_tensor& u = h_tensors[k];
-                if (u.param_dtype != pt || u.grad_dtype != gt) return false;
-                t.p = u.d_param, t.g = u.d_grad, t.n = u.n;
-                t.state = static_cast<uint8_t*>(u.d_state);
-                t.vec = on(u.d_param, 4 * elem(pt)) && on(u.d_grad, 4 * elem(gt));
-                return true;
-            },
-            [&](const AdamArgs& b, int64_t chunks) {
-                return launch_adamw(b, chunks, pt, gt, cfg->state_kind,
-                                    static_cast<hipStream_t>(stream));
-            });
-        if (st != HUGE_OK) return st;
-    }
-    return HUGE_OK;
+    const huge_status st = adamw_args(cfg, h_tensors, count, d_status);
+    return st != HUGE_OK ? st : adamw_step(cfg, h_tensors, count, nullptr, d_status, stream);
 }
 
 huge_status huge_adamw_get_state(const huge_adamw_tensor* h_tensors, int32_t count,

@@ -191,6 +191,7 @@ __device__ __forceinline__ bool update_chunk(const AdamArgs& a, const AdamTensor
     P* p = static_cast<P*>(T.p);
     const G* g = static_cast<const G*>(T.g);
     const int64_t n = T.n, padded = adam_padded(n);
+    const float scale = a.factor != nullptr ? *a.factor : a.grad_scale;
     bool bad = false;
 #pragma unroll
     for (int k = 0; k < kAdamChunk; k += kBlock * 4) {
@@ -204,7 +205,7 @@ __device__ __forceinline__ bool update_chunk(const AdamArgs& a, const AdamTensor
         uint32_t top = 0, low = 0xFFFFFFFFu;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float ge = d[e] * a.grad_scale;
+            const float ge = d[e] * scale;
             mn[e] = m[e] * a.beta1 + ge * a.one_beta1;
             vn[e] = v[e] * a.beta2 + (ge * ge) * a.one_beta2;
             // as integers, infinities and NaN are above all numbers; 0 - 1 is too

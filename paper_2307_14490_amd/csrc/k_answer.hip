@@ -1,0 +1,552 @@
+// Log probabilities of given classes over a large vocabulary, with the entropy and the
+// most likely classes, and their gradient, without the logits in memory.
+//
+// One pass over the logits (softmax.hpp) leaves a maximum, a sum of exponentials and
+// their first moment per row and, where classes are to be found, the largest logit of
+// each tile of 32 classes (16 for few rows): 1/32 of the logits' bytes.  The best `top`
+// classes lie in the best `top` tiles, lowest first among equals, for a class outside
+// of them has `top` tiles' largest before it.  So k_lp_select finds the best tiles of
+// each row, kSlack more than that, for the matrix cores' logits are a rounding away from the ones
+// that decide, and k_lp_top forms the logits of their classes again in fp64, in which
+// products of bf16 or fp32 numbers are exact, and orders those.
+#include "softmax.hpp"
+
+namespace huge {
+
+namespace {
+
+typedef unsigned long long u64;
+
+constexpr int kSlack = 4;
+constexpr int kTopThreads = 256;
+constexpr int64_t kBestFloats = (int64_t)1 << 28;  // tile maxima at a time: 1 GiB
+constexpr int64_t kBestRows = 8192;                // rows that have room for any piece
+constexpr int64_t kListRows = 32768;               // rows times splits of k_lp_select
+constexpr int kMostSplits = 64;
+constexpr int64_t kMostRows = (int64_t)1 << 22;    // rows at a time: a workgroup each
+
+// A tile's key: its largest logit, then the lower tile.  0 is below all keys.
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t b = __float_as_uint(v);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ u64 tile_key(uint32_t order, uint32_t tile) {
+    return (u64)order << 32 | (uint32_t)~tile;
+}
+__device__ __forceinline__ int64_t key_tile(u64 key) { return (int64_t)(uint32_t)~(uint32_t)key; }
+
+// Dot product of a row h (fp64 in LDS) with a class's row, by the LANES threads of a group.
+template <typename E, bool CODES, int LANES>
+__device__ __forceinline__ double dot64(const SoftmaxArgs& a, const double* h, int64_t cls, int lane) {
+    double s = 0.0;
+#pragma unroll 4
+    for (int d = 4 * lane; d < a.dim; d += 4 * LANES) {
+        float4 v;
+        if constexpr (CODES)
+            v = load_code_cols(static_cast<const uint8_t*>(a.w) + cls * a.ld_w,
+                               a.w_scales + cls * a.ld_scales, d, a.dim, a.vec);
+        else
+            v = load_cols(static_cast<const E*>(a.w) + cls * a.ld_w, d, a.dim, a.vec);
+        s = fma(h[d], (double)v.x, s);
+        s = fma(h[d + 1], (double)v.y, s);
+        s = fma(h[d + 2], (double)v.z, s);
+        s = fma(h[d + 3], (double)v.w, s);
+    }
+#pragma unroll
+    for (int off = 1; off < LANES; off <<= 1) s += __shfl_xor(s, off);
+    return s;
+}
+
+// ---------------------------------------------------------------------------
+// lse, entropy and the label's log probability of a row, LANES threads each
+// ---------------------------------------------------------------------------
+template <typename E, bool CODES, int LANES>
+__global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, const float4* __restrict__ part,
+                                                    int slots, int64_t pad, int64_t rows,
+                                                    int64_t first) {
+    const int lane = threadIdx.x % LANES;
+    const int64_t i = (first + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
+    if (i >= rows) return;
+    Stats s{kLeast, 0.f, 0.f};
+    for (int k = lane; k < slots; k += LANES) {
+        const float4 p = part[(int64_t)k * pad + i];
+        s = join(s, {p.x, p.y, p.z});
+    }
+#pragma unroll
+    for (int off = 1; off < LANES; off <<= 1)
+        s = join(s, {__shfl_xor(s.top, off), __shfl_xor(s.sum, off), __shfl_xor(s.first, off)});
+    const float logs = logf(s.sum);
+    const float lse = s.sum == 0.f ? -INFINITY : s.top + logs;
+    float entropy = s.sum == 0.f ? 0.f : logs - 0.69314718055994531f * (s.first / s.sum);
+    entropy = entropy < 0.f ? 0.f : entropy;  // rounding alone takes it below 0
+    float logp = 0.f;
+    if (a.labels != nullptr) {
+        const int32_t y = a.labels[i];
+        if (y < -1 || y >= a.classes) {
+            logp = NAN;
+            if (lane == 0) set_status(a.status, -2);
+        } else if (y >= 0) {
+            const float b = a.bias == nullptr ? 0.f : a.bias[y];
+            if (b < kLeast) {
+                logp = -INFINITY;
+            } else {
+                const E* h = static_cast<const E*>(a.h) + i * a.ld_h;
+                double dot = 0.0;
+#pragma unroll 4
+                for (int d = 4 * lane; d < a.dim; d += 4 * LANES) {
+                    const float4 u = load_cols(h, d, a.dim, a.vec_h);
+                    float4 v;
+                    if constexpr (CODES)
+                        v = load_code_cols(static_cast<const uint8_t*>(a.w) + y * a.ld_w,
+                                           a.w_scales + y * a.ld_scales, d, a.dim, a.vec);
+                    else
+                        v = load_cols(static_cast<const E*>(a.w) + y * a.ld_w, d, a.dim, a.vec);
+                    dot = fma((double)u.x, (double)v.x, dot);
+                    dot = fma((double)u.y, (double)v.y, dot);
+                    dot = fma((double)u.z, (double)v.z, dot);
+                    dot = fma((double)u.w, (double)v.w, dot);
+                }
+#pragma unroll
+                for (int off = 1; off < LANES; off <<= 1) dot += __shfl_xor(dot, off);
+                logp = (float)(dot + (double)b - (double)lse);
+                logp = logp > 0.f ? 0.f : logp;  // as above
+            }
+        }
+    }
+    if (lane == 0) {
+        a.lse[i] = lse;
+        if (a.entropy != nullptr) a.entropy[i] = entropy;
+        if (a.logp != nullptr) a.logp[i] = logp;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The best tiles of each row
+// ---------------------------------------------------------------------------
+// A workgroup takes RW rows and a split of the tiles, in rounds of four tiles a thread.
+// What is above a row's threshold goes to its list in LDS, whose order does not
+// matter; a list that the next round could overfill is cut to its best `keep`, the
+// last of which is the new threshold.  Tiles come in rising order from round to round, so
+// that an equal one of a later round is not better.
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectKeys = 10496;
+template <int RW>
+struct Select {
+    static constexpr int kSubs = kSelectThreads / RW;   // threads of a row
+    static constexpr int kRound = 4 * kSubs;            // tiles of a round
+    static constexpr int kRoom = kSelectKeys / RW;      // keys of a row's list
+    static_assert(kRoom >= kRound + kMostTop + kSlack, "a round fits behind a cut list");
+};
+
+// Cuts each list to its best `keep`, in order.
+template <int RW>
+__device__ __forceinline__ void cut_lists(u64* keys, int* count, uint32_t* least, int keep) {
+    using S = Select<RW>;
+    constexpr int kOwn = (S::kRoom + S::kSubs - 1) / S::kSubs;
+    const int row = threadIdx.x / S::kSubs, lane = threadIdx.x % S::kSubs;
+    u64* list = keys + row * S::kRoom;
+    const int n = count[row];
+    u64 own[kOwn];
+    int rank[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        own[k] = lane + k * S::kSubs < n ? list[lane + k * S::kSubs] : 0;
+        rank[k] = 0;
+    }
+    for (int j = 0; j < n; ++j) {
+        const u64 key = list[j];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) rank[k] += key > own[k] ? 1 : 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+        if (own[k] != 0 && rank[k] < keep) {
+            list[rank[k]] = own[k];
+            if (rank[k] == keep - 1) least[row] = (uint32_t)(own[k] >> 32);
+        }
+    if (lane == 0) count[row] = n < keep ? n : keep;
+    __syncthreads();
+}
+
+template <int RW>
+__global__ __launch_bounds__(kSelectThreads) void k_lp_select(const float* __restrict__ best,
+                                                              int64_t ld, int64_t rows,
+                                                              int64_t tiles, int64_t tile0,
+                                                              int64_t per, int keep,
+                                                              u64* __restrict__ lists) {
+    using S = Select<RW>;
+    extern __shared__ __align__(16) uint8_t lds[];
+    u64* keys = reinterpret_cast<u64*>(lds);  // [RW][kRoom]
+    __shared__ int count[RW];
+    __shared__ uint32_t least[RW];
+    const int r = threadIdx.x % RW, sub = threadIdx.x / RW;
+    const int64_t row = (int64_t)blockIdx.x * RW + r;
+    const bool in = row < rows;
+    if (threadIdx.x < RW) count[threadIdx.x] = 0, least[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t t0 = (int64_t)blockIdx.y * per;
+    const int64_t t1 = t0 + per < tiles ? t0 + per : tiles;
+    auto load = [&](int64_t at, float* v) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t t = at + sub + k * S::kSubs;
+            v[k] = in && t < t1 ? best[t * ld + row] : NAN;
+        }
+    };
+    float now[4], next[4];
+    load(t0, now);
+    for (int64_t at = t0; at < t1; at += S::kRound) {
+        load(at + S::kRound, next);
+        const uint32_t bar = least[r];
+        bool full = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t o = ordered(now[k]);
+            if (now[k] == now[k] && o > bar) {
+                const int slot = atomicAdd(&count[r], 1);
+                keys[r * S::kRoom + slot] =
+                    tile_key(o, (uint32_t)(tile0 + at + sub + k * S::kSubs));
+                full |= slot >= S::kRoom - S::kRound - 1;
+            }
+            now[k] = next[k];
+        }
+        if (__syncthreads_or(full)) cut_lists<RW>(keys, count, least, keep);
+    }
+    cut_lists<RW>(keys, count, least, keep);
+    for (int j = threadIdx.x; j < RW * keep; j += kSelectThreads) {
+        const int k = j / keep;
+        const int64_t out = (int64_t)blockIdx.x * RW + k;
+        if (out < rows)
+            lists[(out * gridDim.y + blockIdx.y) * keep + j % keep] =
+                j % keep < count[k] ? keys[k * S::kRoom + j % keep] : 0;
+    }
+}
+
+// The best `keep` of n keys in LDS, in order, to `out` (LDS too).
+__device__ __forceinline__ void best_keys(const u64* keys, int n, int keep, u64* out) {
+    for (int e = threadIdx.x; e < keep; e += kTopThreads) out[e] = 0;
+    __syncthreads();
+    for (int e = threadIdx.x; e < n; e += kTopThreads) {
+        const u64 own = keys[e];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) rank += keys[j] > own ? 1 : 0;
+        if (own != 0 && rank < keep) out[rank] = own;
+    }
+    __syncthreads();
+}
+
+constexpr int kMostKeep = kMostTop + kSlack;
+
+// A row's lists of `splits`, and of the pieces of the vocabulary before, into one.
+__global__ __launch_bounds__(kTopThreads) void k_lp_merge(const u64* __restrict__ lists, int splits,
+                                                          int keep, bool first,
+                                                          u64* __restrict__ running) {
+    __shared__ u64 s_keys[(kMostSplits + 1) * kMostKeep], s_out[kMostKeep];
+    const int64_t row = blockIdx.x;
+    const int n = splits * keep;
+    for (int e = threadIdx.x; e < n; e += kTopThreads) s_keys[e] = lists[row * n + e];
+    if (!first)
+        for (int e = threadIdx.x; e < keep; e += kTopThreads) s_keys[n + e] = running[row * keep + e];
+    __syncthreads();
+    best_keys(s_keys, first ? n : n + keep, keep, s_out);
+    for (int e = threadIdx.x; e < keep; e += kTopThreads) running[row * keep + e] = s_out[e];
+}
+
+// The best classes of a row among those of its best tiles of G.
+template <typename E, bool CODES, int G>
+__global__ __launch_bounds__(kTopThreads) void k_lp_top(SoftmaxArgs a, const u64* __restrict__ lists,
+                                                        int splits, int keep) {
+    constexpr int kLanes = 8, kAtOnce = kTopThreads / kLanes;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int n = splits * keep;
+    u64* s_keys = reinterpret_cast<u64*>(lds);
+    u64* s_best = s_keys + n;
+    double* s_h = reinterpret_cast<double*>(s_best + keep);
+    double* s_x = s_h + a.dim;
+    const int64_t row = blockIdx.x;
+    const float lse = a.lse[row];
+    int32_t* ids = a.ids + row * a.top;
+    float* logp = a.top_logp + row * a.top;
+    if (!(lse > -INFINITY && lse < INFINITY)) {  // no class, or no number
+        for (int k = threadIdx.x; k < a.top; k += kTopThreads) {
+            ids[k] = -1;
+            logp[k] = lse == -INFINITY ? -INFINITY : NAN;
+        }
+        return;
+    }
+    for (int e = threadIdx.x; e < n; e += kTopThreads) s_keys[e] = lists[row * n + e];
+    const E* h = static_cast<const E*>(a.h) + row * a.ld_h;
+    for (int d = 4 * threadIdx.x; d < a.dim; d += 4 * kTopThreads) {
+        const float4 v = load_cols(h, d, a.dim, a.vec_h);
+        s_h[d] = v.x, s_h[d + 1] = v.y, s_h[d + 2] = v.z, s_h[d + 3] = v.w;
+    }
+    __syncthreads();
+    best_keys(s_keys, n, keep, s_best);
+    const int lane = threadIdx.x % kLanes, m = keep * G;
+    for (int e = threadIdx.x / kLanes; e < m; e += kAtOnce) {
+        const u64 key = s_best[e / G];
+        const int64_t cls = key_tile(key) * G + e % G;
+        double x = -INFINITY;
+        if (key != 0 && cls < a.classes) {
+            const float b = a.bias == nullptr ? 0.f : a.bias[cls];
+            if (!(b < kLeast)) x = dot64<E, CODES, kLanes>(a, s_h, cls, lane) + (double)b;
+        }
+        if (lane == 0) s_x[e] = x;
+    }
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    // a wave takes the best `top` times: each lane knows the best of its elements
+    auto better = [&](double x, int64_t c, double y, int64_t d) { return x > y || (x == y && c < d); };
+    auto of = [&](int e) { return key_tile(s_best[e / G]) * G + e % G; };
+    double x = -INFINITY;
+    int64_t cls = 0x7FFFFFFFFFFFFFFF;
+    int at = -1;
+    auto scan = [&] {
+        x = -INFINITY, cls = 0x7FFFFFFFFFFFFFFF, at = -1;
+        for (int e = threadIdx.x; e < m; e += 64) {
+            const double y = s_x[e];
+            if (y > -INFINITY && better(y, of(e), x, cls)) x = y, cls = of(e), at = e;
+        }
+    };
+    scan();
+    for (int k = 0; k < a.top; ++k) {
+        double bx = x;
+        int64_t bc = cls;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const double y = __shfl_xor(bx, off);
+            const int64_t d = __shfl_xor((long long)bc, off);
+            if (better(y, d, bx, bc)) bx = y, bc = d;
+        }
+        const bool none = bx == -INFINITY;
+        if (threadIdx.x == 0) {
+            const float l = (float)(bx - (double)lse);
+            ids[k] = none ? -1 : (int32_t)bc;
+            logp[k] = none ? -INFINITY : l > 0.f ? 0.f : l;
+        }
+        if (!none && bc == cls) {
+            s_x[at] = -INFINITY;
+            scan();
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+int64_t round_down(int64_t v, int64_t to) { return v / to * to; }
+
+// Splits of a select of `rows` padded rows over `tiles`: about two workgroups a CU, each
+// with a few rounds.
+int select_splits(int64_t rows, int64_t tiles, int rw) {
+    const int64_t blocks = div_up(rows, rw);
+    int64_t s = 512 / blocks;
+    const int64_t most = tiles / (4 * 4 * (kSelectThreads / rw));
+    if (s > most) s = most;
+    if (s > kMostSplits) s = kMostSplits;
+    if (s > kListRows / rows) s = kListRows / rows;
+    return (int)(s < 1 ? 1 : s);
+}
+
+template <int RW>
+hipError_t select(const float* best, int64_t ld, int64_t rows, int64_t tiles, int64_t tile0,
+                  int splits, int keep, u64* lists, hipStream_t s) {
+    SM_TRY(allow_lds<&k_lp_select<RW>>(kSelectKeys * 8));
+    k_lp_select<RW><<<dim3((uint32_t)div_up(rows, RW), (uint32_t)splits), kSelectThreads,
+                      kSelectKeys * 8, s>>>(best, ld, rows, tiles, tile0, div_up(tiles, splits),
+                                            keep, lists);
+    return hipGetLastError();
+}
+
+template <typename E, bool CODES, int G>
+hipError_t finish(const SoftmaxArgs& a, const AnswerPlan& p, const float4* part, int64_t slots,
+                  int64_t pad, int64_t rows, int splits, const u64* lists, hipStream_t s) {
+    if (rows < 16 * kCus)
+        k_lp_rows<E, CODES, 64><<<dim3((uint32_t)div_up(rows, 4)), kBlock, 0, s>>>(
+            a, part, (int)slots, pad, rows, 0);
+    else
+        SM_TRY(in_launches(div_up(rows, 16), [&](dim3 grid, int64_t first) {
+            k_lp_rows<E, CODES, 16><<<grid, kBlock, 0, s>>>(a, part, (int)slots, pad, rows, first);
+        }));
+    SM_TRY(hipGetLastError());
+    if (a.top == 0) return hipSuccess;
+    const int lds = 8 * (splits * p.keep + p.keep + a.dim + p.keep * G);
+    k_lp_top<E, CODES, G><<<dim3((uint32_t)rows), kTopThreads, lds, s>>>(a, lists, splits, p.keep);
+    return hipGetLastError();
+}
+
+// The same arguments for rows r0 .. of them.
+template <typename E>
+SoftmaxArgs rows_from(SoftmaxArgs a, int64_t r0) {
+    a.h = static_cast<const E*>(a.h) + r0 * a.ld_h;
+    if (a.labels != nullptr) a.labels += r0;
+    a.lse += r0;
+    if (a.entropy != nullptr) a.entropy += r0;
+    if (a.logp != nullptr) a.logp += r0;
+    if (a.top > 0) a.ids += r0 * a.top, a.top_logp += r0 * a.top;
+    return a;
+}
+
+// ... and for `count` classes from c0 on.
+template <typename E, bool CODES>
+SoftmaxArgs classes_from(SoftmaxArgs a, int64_t c0, int64_t count) {
+    if constexpr (CODES) {
+        a.w = static_cast<const uint8_t*>(a.w) + c0 * a.ld_w;
+        a.w_scales += c0 * a.ld_scales;
+    } else {
+        a.w = static_cast<const E*>(a.w) + c0 * a.ld_w;
+    }
+    if (a.bias != nullptr) a.bias += c0;
+    a.classes = count;
+    return a;
+}
+
+template <typename E, bool CODES>
+hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
+    const AnswerPlan p = answer_plan(a.classes, a.n, a.dim, a.dtype, CODES, a.top);
+    float4* part = reinterpret_cast<float4*>(a.ws + p.part);
+    float* best = a.top > 0 ? reinterpret_cast<float*>(a.ws + p.best) : nullptr;
+    u64* lists = reinterpret_cast<u64*>(a.ws + p.lists);
+    u64* running = reinterpret_cast<u64*>(a.ws + p.running);
+    constexpr int kN = CODES ? 16 : 16 / (int)sizeof(E), kNh = 16 / sizeof(E);
+    auto sixteen = [](const void* m, int64_t ld, int n) {
+        return (reinterpret_cast<uintptr_t>(m) & 15) == 0 && ld % n == 0;
+    };
+    a.vec_h = fours(a.h, a.ld_h, sizeof(E));
+    a.vec = fours(a.w, a.ld_w, CODES ? 1 : sizeof(E));
+    a.vec16 = a.dim % kN == 0 && sixteen(a.w, a.ld_w, kN);
+    if constexpr (!CODES) {
+        // the few rows' kernel reads both alike
+        a.vec16 = a.vec16 && sixteen(a.h, a.ld_h, kNh);
+    }
+    const int64_t all = div_up(a.classes, p.group), piece = p.piece / p.group;
+    if (p.few != 0) {
+        SoftmaxArgs f = a;
+        if constexpr (!CODES) f.vec = a.vec && a.vec_h;
+        const int64_t pad = 16 * p.few;
+        const bool pieces = piece < all;
+        int64_t slots = 0;
+        int splits = 1;
+        for (int64_t t0 = 0; t0 < all; t0 += piece) {
+            const int64_t tiles = all - t0 < piece ? all - t0 : piece, c0 = t0 * 16;
+            const int64_t count = a.classes - c0 < tiles * 16 ? a.classes - c0 : tiles * 16;
+            const SoftmaxArgs q = classes_from<E, CODES>(f, c0, count);
+            int64_t more = 0;
+            SM_TRY((p.few == 1   ? few_pass<E, 1, true, CODES>(q, part + slots * pad, &more, s, best)
+                    : p.few == 2 ? few_pass<E, 2, true, CODES>(q, part + slots * pad, &more, s, best)
+                                 : few_pass<E, 4, true, CODES>(q, part + slots * pad, &more, s, best)));
+            slots += more;
+            if (a.top == 0) continue;
+            splits = select_splits(pad, tiles, 16);
+            SM_TRY(select<16>(best, pad, a.n, tiles, t0, splits, p.keep, lists, s));
+            if (!pieces) continue;
+            k_lp_merge<<<dim3((uint32_t)a.n), kTopThreads, 0, s>>>(lists, splits, p.keep, t0 == 0,
+                                                                   running);
+            SM_TRY(hipGetLastError());
+        }
+        return finish<E, CODES, 16>(a, p, part, slots, pad, a.n, pieces ? 1 : splits,
+                                    pieces ? running : lists, s);
+    }
+    // bf16 classes without a bias are used as they lie, as in the loss
+    const bool direct = !CODES && sizeof(E) == 2 && a.bias == nullptr && a.vec16 &&
+                        p.sm.chunks == 1 && a.dim == p.sm.dp;
+    const bool pieces = piece < all;
+    SoftmaxPlan sm = p.sm;
+    sm.piece = p.piece;
+    const int64_t rec = record_bytes(sm.dp / 16, sm.parts, 1);
+    if (direct) SM_TRY((pack<E, true, CODES>(sm, a, 0, 0, 1, s)));  // the rows
+    for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
+        const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows;
+        const SoftmaxArgs q = rows_from<E>(a, r0);
+        int64_t slots = 0;
+        int splits = 1;
+        PassArgs l{};
+        l.x = a.ws + p.sm.h + r0 / kSmTile * rec, l.forms = 1, l.stat_part = part;
+        l.x_tiles = div_up(rows, kSmTile);
+        const int64_t pad = l.x_tiles * kSmTile;
+        l.best = best, l.best_ld = pad;
+        for (int64_t t0 = 0; t0 < all; t0 += piece) {
+            const int64_t tiles = all - t0 < piece ? all - t0 : piece, c0 = t0 * kSmTile;
+            const int64_t count = a.classes - c0 < tiles * kSmTile ? a.classes - c0 : tiles * kSmTile;
+            if (!direct && (pieces || r0 == 0))
+                SM_TRY((pack<E, true, CODES>(sm, a, c0, count, 1, s)));
+            if (direct)
+                l.y_rows = static_cast<const bf16_t*>(a.w) + c0 * a.ld_w, l.ld = a.ld_w, l.classes = count;
+            else
+                l.y = a.ws + p.sm.w;
+            l.y_tiles = tiles, l.first = t0 == 0;
+            SM_TRY((lse_pass<E, true>(sm, l, true, &slots, s)));
+            if (a.top == 0) continue;
+            splits = select_splits(pad, tiles, 32);
+            SM_TRY(select<32>(best, pad, rows, tiles, t0, splits, p.keep, lists, s));
+            if (!pieces) continue;
+            k_lp_merge<<<dim3((uint32_t)rows), kTopThreads, 0, s>>>(lists, splits, p.keep, t0 == 0,
+                                                                    running);
+            SM_TRY(hipGetLastError());
+        }
+        SM_TRY((finish<E, CODES, 32>(q, p, part, slots, pad, rows, pieces ? 1 : splits,
+                                     pieces ? running : lists, s)));
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+AnswerPlan answer_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype, bool codes,
+                       int32_t top) {
+    AnswerPlan p{};
+    const bool bf16 = dtype == kDtypeBf16;
+    p.sm = softmax_plan(classes, n, dim, dtype, false);
+    p.few = codes ? few_blocks<bf16_t, true>(n, dim)
+                  : bf16 ? few_blocks<bf16_t>(n, dim) : few_blocks<float>(n, dim);
+    p.group = p.few != 0 ? 16 : kSmTile;
+    const int64_t all = div_up(classes, p.group);
+    const int64_t pad = p.few != 0 ? 16 * p.few : p.sm.rows_pad;
+    const int64_t rec = record_bytes(p.sm.dp / 16, p.sm.parts, 1);
+    int64_t piece = all;  // tiles at a time
+    p.rows = pad;         // rows at a time
+    if (p.few == 0 && piece > kSmPieceBytes / rec) piece = kSmPieceBytes / rec;
+    if (top > 0) {
+        // the same piece for every number of rows, so that fewer never need more memory
+        const int64_t least = p.few != 0 ? pad : kBestRows;
+        if (piece > kBestFloats / least) piece = kBestFloats / least;
+        int64_t most = round_down(kBestFloats / piece, kSmTile);
+        if (most > kMostRows) most = kMostRows;
+        if (p.few == 0 && p.rows > most) p.rows = most;
+    }
+    p.piece = piece * p.group;
+    p.keep = (int32_t)(all < top + kSlack ? all : top + kSlack);
+    size_t off = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t o = off;
+        off += ((size_t)bytes + 255) & ~(size_t)255;
+        return o;
+    };
+    p.sm.h = take(p.few != 0 ? 0 : p.sm.rows_pad / kSmTile * rec);
+    p.sm.w = take(p.few != 0 ? 0 : piece * rec);
+    const int64_t slots = p.few != 0 ? 2048 * div_up(all, piece) * pad : 0;
+    const int64_t parts = p.rows > kSmPartRows ? p.rows : kSmPartRows;
+    p.part = take(16 * (slots > parts ? slots : parts));
+    if (top > 0) {
+        p.best = take(4 * p.rows * piece);
+        p.lists = take(8 * (p.rows > kListRows ? p.rows : kListRows) * p.keep);
+        p.running = take(piece < all ? 8 * p.rows * p.keep : 0);
+    }
+    p.total = off;
+    return p;
+}
+
+hipError_t launch_log_probs(const SoftmaxArgs& a, hipStream_t s) {
+    if (a.n == 0) return hipSuccess;
+    if (a.w_scales != nullptr) return log_probs<bf16_t, true>(a, s);
+    return a.dtype == kDtypeBf16 ? log_probs<bf16_t, false>(a, s) : log_probs<float, false>(a, s);
+}
+
+hipError_t launch_log_probs_grad(const SoftmaxArgs& a, hipStream_t s) {
+    if (a.dh == nullptr && a.dw == nullptr && a.dbias == nullptr) return hipSuccess;
+    return a.dtype == kDtypeBf16 ? softmax_grad<bf16_t, true>(a, s) : softmax_grad<float, true>(a, s);
+}
+
+}  // namespace huge

@@ -1,0 +1,351 @@
+// Root-mean-square norm of rows with the residual's addition, in the rows' type or in
+// 8 bits, its backward pass, and rows in 8 bits.
+//
+// A group of threads holds a row in registers, as in layer norm: the sum of the two
+// inputs is rounded to the rows' type, stored and normalised as it was stored, so that
+// the backward pass, which reads it again, sees the same row.  One reduction over the
+// group, the sum of squares; every array is moved once.  Bound by memory.
+//
+// 8 bits: e4m3 codes under a power of two for each 32 columns, which eight threads
+// hold: the largest of their absolute values, as integers, so that a NaN is above
+// everything, gives the smallest power under which no code is above 448.  A code
+// times a power of two is a bf16 number, so that what reads such rows widens them
+// without another rounding.
+#include "rows.hpp"
+
+namespace huge {
+
+namespace {
+
+// The exponent of a block's scale from the bits of its largest absolute value; kNone
+// where that is no number.
+constexpr int kNone = 128;
+__device__ __forceinline__ int scale_exponent(uint32_t big) {
+    if (big >= 0x7F800000u) return kNone;
+    // 448 = 1.75 2^8: one more above 1.75
+    const int e = (int)((big + 0x1FFFFFu) >> 23) - 127 - 8;
+    return e < kByteLeast ? kByteLeast : e;
+}
+
+// The largest over eight lanes, aligned, all of which are active (as xor_add).
+__device__ __forceinline__ uint32_t max_of_eight(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));
+    return v;
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Stores chunk c of a row in 8 bits and, from the first of eight chunks, its scale.
+// Eight lanes with adjacent chunks call together; f is 0 past the row's end.
+template <bool WHOLE>
+__device__ __forceinline__ void store_bytes(uint8_t* codes, uint8_t* scales, int c, int D,
+                                            const Few& f) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) big = max(big, abs_bits(f.v[e]));
+    const int x = scale_exponent(max_of_eight(big));
+    if (4 * c >= D) return;
+    const float mul = __uint_as_float((uint32_t)(127 - (x == kNone ? 0 : x)) << 23);
+    uint32_t q = 0x7F7F7F7Fu;  // NaN
+    if (x != kNone) {
+        q = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f.v[0] * mul, f.v[1] * mul, 0, false);
+        q = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f.v[2] * mul, f.v[3] * mul, (int)q, true);
+    }
+    if constexpr (WHOLE) {
+        *reinterpret_cast<uint32_t*>(codes + 4 * c) = q;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (4 * c + e < D) codes[4 * c + e] = (uint8_t)(q >> (8 * e));
+    }
+    if (c % 8 == 0) scales[c / 8] = (uint8_t)(x + 127);
+}
+
+template <typename E>
+__device__ __forceinline__ float rounded(float v) {
+    if constexpr (sizeof(E) == 4) return v;
+    else return __uint_as_float(float_to_bf16_bits(v) << 16);
+}
+
+template <typename E, int TPR, int NV, bool WHOLE, bool BYTES>
+__global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
+    __shared__ float s_sum[8];
+    int turn = 0;
+    constexpr int kRows = kBlock / TPR;
+    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + 3) / 4;
+    const E* x = static_cast<const E*>(a.x);
+    const E* res = static_cast<const E*>(a.res);
+    E* total = static_cast<E*>(a.total);
+    const float inv = 1.0f / (float)D;
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
+         r += (int64_t)gridDim.x * kRows) {
+        Few f[NV], o[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + TPR * i;
+            f[i] = c < chunks ? load_few<WHOLE>(x + r * a.ld_x, c, D) : Few{};
+            if (res != nullptr) o[i] = c < chunks ? load_few<WHOLE>(res + r * a.ld_res, c, D) : Few{};
+        }
+        float sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + TPR * i;
+            if (res != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[i].v[e] = rounded<E>(f[i].v[e] + o[i].v[e]);
+                if (c < chunks) store_few<WHOLE>(total + r * a.ld_total, c, D, f[i]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sq = fmaf(f[i].v[e], f[i].v[e], sq);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s_sum, turn) * inv + a.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + TPR * i;
+            const Few g = c < chunks ? load_few<WHOLE>(a.gamma, c, D) : Few{};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[i].v[e] = f[i].v[e] * rstd * g.v[e];
+            if constexpr (BYTES)
+                store_bytes<WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f[i]);
+            else if (c < chunks)
+                store_few<WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f[i]);
+        }
+        if (t == 0 && a.rstd != nullptr) a.rstd[r] = rstd;
+    }
+}
+
+template <typename E, int TPR, int NV, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_rms_backward(RmsArgs a) {
+    __shared__ float s_sum[8];
+    int turn = 0;
+    constexpr int kRows = kBlock / TPR;
+    constexpr int kHeld = TPR < 64 ? TPR : 64;  // lanes of a wave that hold different columns
+    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + 3) / 4;
+    const E* x = static_cast<const E*>(a.x);
+    const E* dy = static_cast<const E*>(a.dy);
+    const E* res = static_cast<const E*>(a.res);
+    E* dx = static_cast<E*>(a.y);
+    const float inv = 1.0f / (float)D;
+    Few g[NV], dg[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = t + TPR * i;
+        g[i] = c < chunks ? load_few<WHOLE>(a.gamma, c, D) : Few{};
+        dg[i] = Few{};
+    }
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
+         r += (int64_t)gridDim.x * kRows) {
+        const float rstd = a.rstd[r];
+        Few z[NV], d[NV], o[NV];
+        float along = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + TPR * i;
+            const bool in = c < chunks;
+            z[i] = in ? load_few<WHOLE>(x + r * a.ld_x, c, D) : Few{};
+            d[i] = in ? load_few<WHOLE>(dy + r * a.ld_dy, c, D) : Few{};
+            o[i] = in && res != nullptr ? load_few<WHOLE>(res + r * a.ld_res, c, D) : Few{};
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                z[i].v[e] *= rstd;
+                dg[i].v[e] = fmaf(d[i].v[e], z[i].v[e], dg[i].v[e]);
+                d[i].v[e] *= g[i].v[e];
+                along = fmaf(d[i].v[e], z[i].v[e], along);
+            }
+        }
+        if (dx == nullptr) continue;
+        along = row_sum<TPR>(along, s_sum, turn) * inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + TPR * i;
+            if (c >= chunks) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                d[i].v[e] = fmaf(rstd, d[i].v[e] - z[i].v[e] * along, o[i].v[e]);
+            store_few<WHOLE>(dx + r * a.ld_y, c, D, d[i]);
+        }
+    }
+    if (a.partial == nullptr) return;
+    // the groups of a wave, then the waves
+    __shared__ float s_part[TPR <= 64 ? 4 * kHeld * NV * 4 : 1];
+    float* out = a.partial + (int64_t)blockIdx.x * D;
+    if constexpr (TPR <= 64) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = dg[i].v[e];
+#pragma unroll
+                for (int off = TPR; off < 64; off <<= 1) v += __shfl_xor(v, off);
+                if (lane < kHeld) s_part[((wave * NV + i) * 4 + e) * kHeld + lane] = v;
+            }
+        __syncthreads();
+        for (int j = threadIdx.x; j < D; j += kBlock) {
+            const int c = j / 4, at = ((c / TPR) * 4 + j % 4) * kHeld + c % TPR;
+            constexpr int kWave = NV * 4 * kHeld;
+            out[j] = (s_part[at] + s_part[kWave + at]) +
+                     (s_part[2 * kWave + at] + s_part[3 * kWave + at]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + TPR * i;
+            if (c >= chunks) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (inside<WHOLE>(c, e, D)) out[c * 4 + e] = dg[i].v[e];
+        }
+    }
+}
+
+// Column sums of `partial`: a workgroup takes 16 columns, 16 threads each.
+__global__ __launch_bounds__(kBlock) void k_rms_reduce(const float* __restrict__ partial,
+                                                       int blocks, int dim,
+                                                       float* __restrict__ dgamma) {
+    __shared__ float s[16][17];
+    const int col = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
+    float v = 0.f;
+    if (col < dim) {
+#pragma unroll 8
+        for (int b = lane; b < blocks; b += 16) v += partial[(int64_t)b * dim + col];
+    }
+    s[lane][threadIdx.x & 15] = v;
+    __syncthreads();
+    if (lane == 0 && col < dim) {
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) sum += s[k][threadIdx.x & 15];
+        dgamma[col] = sum;
+    }
+}
+
+// Rows into 8 bits: eight threads a block of 32 columns, blocks in the order of rows.
+template <typename E, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_to_bytes(RmsArgs a) {
+    const int D = a.dim, blocks = (D + kByteBlock - 1) / kByteBlock;
+    const int64_t all = a.n * blocks;
+    for (int64_t b = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / 8; b < all;
+         b += (int64_t)gridDim.x * kBlock / 8) {
+        const int64_t r = b / blocks;
+        const int c = (int)(b % blocks) * 8 + (threadIdx.x & 7);
+        const Few f = 4 * c < D
+                          ? load_few<WHOLE>(static_cast<const E*>(a.x) + r * a.ld_x, c, D) : Few{};
+        store_bytes<WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f);
+    }
+}
+
+// ... and back: a thread takes four columns.
+template <typename E, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_from_bytes(RmsArgs a) {
+    const int D = a.dim, chunks = (D + 3) / 4;
+    const int64_t all = a.n * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < all;
+         i += (int64_t)gridDim.x * kBlock) {
+        const int64_t r = i / chunks;
+        const int c = (int)(i % chunks);
+        const uint8_t* row = a.codes + r * a.ld_codes;
+        uint32_t q = 0;
+        if constexpr (WHOLE) {
+            q = reinterpret_cast<const uint32_t*>(row)[c];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * c + e < D) q |= (uint32_t)row[4 * c + e] << (8 * e);
+        }
+        const float mul = byte_scale(a.scales[r * a.ld_scales + c / 8]);
+        const Few f = {{__builtin_amdgcn_cvt_f32_fp8((int)q, 0) * mul,
+                        __builtin_amdgcn_cvt_f32_fp8((int)q, 1) * mul,
+                        __builtin_amdgcn_cvt_f32_fp8((int)q, 2) * mul,
+                        __builtin_amdgcn_cvt_f32_fp8((int)q, 3) * mul}};
+        store_few<WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f);
+    }
+}
+
+template <typename E, int TPR, int NV, bool WHOLE>
+void rms_one(const RmsArgs& a, bool backward, hipStream_t s) {
+    const int64_t rows = kBlock / TPR, need = (a.n + rows - 1) / rows;
+    const dim3 grid((uint32_t)(need < 65536 ? need : 65536));
+    if (backward)
+        k_rms_backward<E, TPR, NV, WHOLE>
+            <<<dim3((uint32_t)norm_blocks(a.n, a.dim)), kBlock, 0, s>>>(a);
+    else if (a.codes != nullptr)
+        k_rms<E, TPR, NV, WHOLE, true><<<grid, kBlock, 0, s>>>(a);
+    else
+        k_rms<E, TPR, NV, WHOLE, false><<<grid, kBlock, 0, s>>>(a);
+}
+
+template <typename E>
+hipError_t rms_dispatch(const RmsArgs& a, bool backward, hipStream_t s) {
+    const NormShape p = norm_shape((a.dim + 3) / 4);
+#define HUGE_RMS_CASE(T, N)                           \
+    case (T) * 64 + (N):                              \
+        if (a.vec) rms_one<E, T, N, true>(a, backward, s); \
+        else rms_one<E, T, N, false>(a, backward, s); \
+        return hipGetLastError();
+    switch (p.tpr * 64 + p.nv) {
+        HUGE_RMS_CASE(8, 1)
+        HUGE_RMS_CASE(16, 1)
+        HUGE_RMS_CASE(32, 1)
+        HUGE_RMS_CASE(64, 1)
+        HUGE_RMS_CASE(64, 2)
+        HUGE_RMS_CASE(64, 4)
+        HUGE_RMS_CASE(256, 2)
+        HUGE_RMS_CASE(256, 4)
+        HUGE_RMS_CASE(256, 8)
+    }
+#undef HUGE_RMS_CASE
+    return hipErrorInvalidValue;
+}
+
+template <typename E>
+hipError_t bytes_dispatch(const RmsArgs& a, bool back, hipStream_t s) {
+    const int64_t work = back ? a.n * ((a.dim + 3) / 4)
+                              : a.n * ((a.dim + kByteBlock - 1) / kByteBlock) * 8;
+    const int64_t need = (work + kBlock - 1) / kBlock;
+    const dim3 grid((uint32_t)(need < 65536 ? need : 65536));
+    if (back) {
+        if (a.vec) k_from_bytes<E, true><<<grid, kBlock, 0, s>>>(a);
+        else k_from_bytes<E, false><<<grid, kBlock, 0, s>>>(a);
+    } else {
+        if (a.vec) k_to_bytes<E, true><<<grid, kBlock, 0, s>>>(a);
+        else k_to_bytes<E, false><<<grid, kBlock, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms(const RmsArgs& a, hipStream_t s) {
+    return a.dtype == kDtypeBf16 ? rms_dispatch<bf16_t>(a, false, s)
+                                 : rms_dispatch<float>(a, false, s);
+}
+
+hipError_t launch_rms_backward(const RmsArgs& a, float* dgamma, hipStream_t s) {
+    if (a.n > 0) {
+        const hipError_t e = a.dtype == kDtypeBf16 ? rms_dispatch<bf16_t>(a, true, s)
+                                                   : rms_dispatch<float>(a, true, s);
+        if (e != hipSuccess) return e;
+    }
+    if (dgamma == nullptr) return hipSuccess;
+    k_rms_reduce<<<dim3((uint32_t)((a.dim + 15) / 16)), kBlock, 0, s>>>(
+        a.partial, norm_blocks(a.n, a.dim), a.dim, dgamma);
+    return hipGetLastError();
+}
+
+hipError_t launch_to_bytes(const RmsArgs& a, hipStream_t s) {
+    return a.dtype == kDtypeBf16 ? bytes_dispatch<bf16_t>(a, false, s)
+                                 : bytes_dispatch<float>(a, false, s);
+}
+
+hipError_t launch_from_bytes(const RmsArgs& a, hipStream_t s) {
+    return a.dtype == kDtypeBf16 ? bytes_dispatch<bf16_t>(a, true, s)
+                                 : bytes_dispatch<float>(a, true, s);
+}
+
+}  // namespace huge

@@ -291,6 +291,14 @@ class SoftmaxLoss(_Status):
 # --------------------------------------------------------------------------- #
 # AdamW
 # --------------------------------------------------------------------------- #
+def _apart(tensors, what):
+    """Raise ValueError where two of a list of contiguous tensors overlap."""
+    ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                  for t in tensors if t.numel())
+    if any(a[1] > b[0] for a, b in zip(ends, ends[1:])):
+        raise ValueError(f"{what} that share memory")
+
+
 class AdamW(_Status):
     """AdamW over a list of contiguous float32 or bfloat16 GPU tensors of one
     device that share no memory, updated in place by huge_adamw_step.  states:
@@ -311,10 +319,7 @@ class AdamW(_Status):
             if p.device != self.params[0].device:
                 raise ValueError(f"AdamW params[{k}]: on {p.device}, expected "
                                  f"{self.params[0].device}")
-        ends = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size())
-                      for p in self.params if p.numel())
-        if any(a[1] > b[0] for a, b in zip(ends, ends[1:])):
-            raise ValueError("AdamW: parameters that share memory")
+        _apart(self.params, "AdamW: parameters")
         super().__init__(self.params[0].device)
         self.steps = 0
         self.lr = float(lr)
@@ -368,9 +373,14 @@ class AdamW(_Status):
                                  f"{p.numel()} on {p.device}")
         return ts
 
-    def step(self, grads, lr=None, grad_scale=1.0, stream=None):
+    def step(self, grads, lr=None, grad_scale=1.0, max_norm=None, stream=None):
         """One step with these gradients (float32 or bfloat16, one per parameter).  In
-        a graph's capture its learning rate and bias corrections are recorded too."""
+        a graph's capture its learning rate and bias corrections are recorded too.
+        max_norm: the step takes the gradients (which stay as they are) scaled so that the
+        norm over all of them, times grad_scale, is at most that; it returns the norm
+        before (one float32 element).  Where that is not finite nothing moves."""
+        if max_norm is not None and not float(max_norm) > 0:
+            raise ValueError(f"AdamW.step: max_norm {max_norm}")
         grads = self._list(grads, ("float32", "bfloat16"), "AdamW.step grads")
         c = self.cfg
         c.lr = self.lr if lr is None else float(lr)
@@ -380,10 +390,26 @@ class AdamW(_Status):
             t.d_grad = g.data_ptr()
             t.grad_dtype = _dtype_code(g, "AdamW.step grads")
         self._ordered(stream)
+        norm = None
         with _on(self.device, stream, (self.states, *self.params, *grads,)) as st:
-            _ok(load().huge_adamw_step(ctypes.byref(c), self._tensors, len(grads),
-                                       self._status_ptr, st), "huge_adamw_step")
+            if max_norm is None:
+                _ok(load().huge_adamw_step(ctypes.byref(c), self._tensors, len(grads),
+                                           self._status_ptr, st), "huge_adamw_step")
+            else:
+                norm = self._step_clipped(float(max_norm), st)
         self.steps += 1
+        return norm
+
+    def _step_clipped(self, max_norm, st):
+        import torch
+        L, count = load(), len(self.params)
+        norm = torch.empty(1, dtype=torch.float32, device=self.device)
+        bytes_ = L.huge_grad_norm_workspace_bytes(count)
+        ws = torch.empty(bytes_, dtype=torch.uint8, device=self.device)
+        _ok(L.huge_adamw_step_clipped(ctypes.byref(self.cfg), self._tensors, count, max_norm,
+                                      norm.data_ptr(), self._status_ptr, ws.data_ptr(), bytes_,
+                                      st), "huge_adamw_step_clipped")
+        return norm
 
     def _pointers(self, ts):
         return (ctypes.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
