@@ -23,6 +23,7 @@ constexpr int64_t kBestFloats = (int64_t)1 << 28;  // tile maxima at a time: 1 G
 constexpr int64_t kBestRows = 8192;                // rows that have room for any piece
 constexpr int64_t kListRows = 32768;               // rows times splits of k_lp_select
 constexpr int kMostSplits = 64;
+constexpr int kTopLds = 80 * 1024;
 constexpr int64_t kMostRows = (int64_t)1 << 22;    // rows at a time: a workgroup each
 
 // A tile's key: its largest logit, then the lower tile.  0 is below all keys.
@@ -60,21 +61,56 @@ __device__ __forceinline__ double dot64(const SoftmaxArgs& a, const double* h, i
 // ---------------------------------------------------------------------------
 // lse, entropy and the label's log probability of a row, LANES threads each
 // ---------------------------------------------------------------------------
+// Over the LANES threads of a row, in the same order always; a workgroup's four waves meet
+// in s, and all of its threads call.
+template <int LANES, typename T>
+__device__ __forceinline__ T row_add(T v, double* s) {
+#pragma unroll
+    for (int off = 1; off < (LANES < 64 ? LANES : 64); off <<= 1) v += __shfl_xor(v, off);
+    if constexpr (LANES > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = (double)v;
+        __syncthreads();
+        v = (T)s[0] + (T)s[1] + (T)s[2] + (T)s[3];
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float row_max(float v, double* s) {
+#pragma unroll
+    for (int off = 1; off < (LANES < 64 ? LANES : 64); off <<= 1) v = fmaxf(v, __shfl_xor(v, off));
+    if constexpr (LANES > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = (double)v;
+        __syncthreads();
+        v = fmaxf(fmaxf((float)s[0], (float)s[1]), fmaxf((float)s[2], (float)s[3]));
+    }
+    return v;
+}
+
 template <typename E, bool CODES, int LANES>
 __global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, const float4* __restrict__ part,
                                                     int slots, int64_t pad, int64_t rows,
                                                     int64_t first) {
+    __shared__ double s_join[4];
     const int lane = threadIdx.x % LANES;
     const int64_t i = (first + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
     if (i >= rows) return;
-    Stats s{kLeast, 0.f, 0.f};
+    // the top of all slots first, then their sums from it: one exponential a slot, none of
+    // which waits for another
+    float top = kLeast;
+#pragma unroll 4
+    for (int k = lane; k < slots; k += LANES) top = fmaxf(top, part[(int64_t)k * pad + i].x);
+    top = row_max<LANES>(top, s_join);
+    float sum = 0.f, first_ = 0.f;
+#pragma unroll 4
     for (int k = lane; k < slots; k += LANES) {
         const float4 p = part[(int64_t)k * pad + i];
-        s = join(s, {p.x, p.y, p.z});
+        const Stats s = raise({p.x, p.y, p.z}, top);
+        sum += s.sum;
+        first_ += s.first;
     }
-#pragma unroll
-    for (int off = 1; off < LANES; off <<= 1)
-        s = join(s, {__shfl_xor(s.top, off), __shfl_xor(s.sum, off), __shfl_xor(s.first, off)});
+    const Stats s{top, row_add<LANES>(sum, s_join), row_add<LANES>(first_, s_join)};
     const float logs = logf(s.sum);
     const float lse = s.sum == 0.f ? -INFINITY : s.top + logs;
     float entropy = s.sum == 0.f ? 0.f : logs - 0.69314718055994531f * (s.first / s.sum);
@@ -106,8 +142,7 @@ __global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, const float4*
                     dot = fma((double)u.z, (double)v.z, dot);
                     dot = fma((double)u.w, (double)v.w, dot);
                 }
-#pragma unroll
-                for (int off = 1; off < LANES; off <<= 1) dot += __shfl_xor(dot, off);
+                dot = row_add<LANES>(dot, s_join);
                 logp = (float)(dot + (double)b - (double)lse);
                 logp = logp > 0.f ? 0.f : logp;  // as above
             }
@@ -123,11 +158,14 @@ __global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, const float4*
 // ---------------------------------------------------------------------------
 // The best tiles of each row
 // ---------------------------------------------------------------------------
-// A workgroup takes RW rows and a split of the tiles, in rounds of four tiles a thread.
-// What is above a row's threshold goes to its list in LDS, whose order does not
-// matter; a list that the next round could overfill is cut to its best `keep`, the
-// last of which is the new threshold.  Tiles come in rising order from round to round, so
-// that an equal one of a later round is not better.
+// A workgroup takes RW rows and a split of the tiles.  What is above a row's bar goes to
+// its list in LDS, whose order does not matter.  The bar: each slot of the pass over the
+// logits has left its largest logit, of another tile each, so that the best `keep` of all
+// tiles are at or above the keep-th largest of those (of some threads' largest of them).
+// A list that overflows all the same is built again in rounds of four tiles a thread: one that
+// the next round could overfill is cut to its best `keep`, the last of which is the new
+// bar.  Tiles come in rising order from round to round, so that an equal one of a later
+// round is not better.
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectKeys = 10496;
 template <int RW>
@@ -174,44 +212,89 @@ __global__ __launch_bounds__(kSelectThreads) void k_lp_select(const float* __res
                                                               int64_t ld, int64_t rows,
                                                               int64_t tiles, int64_t tile0,
                                                               int64_t per, int keep,
-                                                              u64* __restrict__ lists) {
+                                                              const float4* __restrict__ part,
+                                                              int slots, u64* __restrict__ lists) {
     using S = Select<RW>;
     extern __shared__ __align__(16) uint8_t lds[];
     u64* keys = reinterpret_cast<u64*>(lds);  // [RW][kRoom]
     __shared__ int count[RW];
     __shared__ uint32_t least[RW];
+    __shared__ bool over;
     const int r = threadIdx.x % RW, sub = threadIdx.x / RW;
     const int64_t row = (int64_t)blockIdx.x * RW + r;
     const bool in = row < rows;
-    if (threadIdx.x < RW) count[threadIdx.x] = 0, least[threadIdx.x] = 0;
-    __syncthreads();
+    // a tile whose classes are all out has kFloor
+    if (threadIdx.x < RW) count[threadIdx.x] = 0, least[threadIdx.x] = ordered(kLeast);
+    if (threadIdx.x == 0) over = false;
     const int64_t t0 = (int64_t)blockIdx.y * per;
     const int64_t t1 = t0 + per < tiles ? t0 + per : tiles;
-    auto load = [&](int64_t at, float* v) {
+    constexpr int kDeep = 8;
+    auto load = [&](int64_t at, float* v, int n) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kDeep; ++k) {
+            if (k >= n) break;
             const int64_t t = at + sub + k * S::kSubs;
             v[k] = in && t < t1 ? best[t * ld + row] : NAN;
         }
     };
-    float now[4], next[4];
-    load(t0, now);
-    for (int64_t at = t0; at < t1; at += S::kRound) {
-        load(at + S::kRound, next);
-        const uint32_t bar = least[r];
-        bool full = false;
+    float now[kDeep], next[kDeep];
+    load(t0, now, kDeep);
+    if (keep <= S::kSubs) {
+        float v = -INFINITY;
+        if (in)
+#pragma unroll 4
+            for (int k = sub; k < slots; k += S::kSubs) v = fmaxf(v, part[k * ld + row].w);
+        uint32_t* of_row = reinterpret_cast<uint32_t*>(lds);  // [sub][row]
+        const uint32_t own = v > kLeast ? ordered(v) : 0;
+        of_row[threadIdx.x] = own;
+        __syncthreads();
+        int rank = 0;
+#pragma unroll 8
+        for (int k = 0; k < S::kSubs; ++k) {
+            const uint32_t o = of_row[k * RW + r];
+            rank += o > own || (o == own && k < sub) ? 1 : 0;
+        }
+        if (rank == keep - 1 && own != 0) least[r] = own - 1;
+    }
+    __syncthreads();
+    const uint32_t bar = least[r];
+    for (int64_t at = t0; at < t1; at += kDeep * S::kSubs) {
+        load(at + kDeep * S::kSubs, next, kDeep);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kDeep; ++k) {
             const uint32_t o = ordered(now[k]);
             if (now[k] == now[k] && o > bar) {
                 const int slot = atomicAdd(&count[r], 1);
-                keys[r * S::kRoom + slot] =
-                    tile_key(o, (uint32_t)(tile0 + at + sub + k * S::kSubs));
-                full |= slot >= S::kRoom - S::kRound - 1;
+                if (slot < S::kRoom)
+                    keys[r * S::kRoom + slot] =
+                        tile_key(o, (uint32_t)(tile0 + at + sub + k * S::kSubs));
+                else
+                    over = true;
             }
             now[k] = next[k];
         }
-        if (__syncthreads_or(full)) cut_lists<RW>(keys, count, least, keep);
+    }
+    __syncthreads();
+    if (over) {
+        __syncthreads();
+        if (threadIdx.x < RW) count[threadIdx.x] = 0;
+        __syncthreads();
+        for (int64_t at = t0; at < t1; at += S::kRound) {
+            load(at, now, 4);
+            const uint32_t above = least[r];
+            bool full = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t o = ordered(now[k]);
+                if (now[k] == now[k] && o > above) {
+                    const int slot = atomicAdd(&count[r], 1);
+                    keys[r * S::kRoom + slot] =
+                        tile_key(o, (uint32_t)(tile0 + at + sub + k * S::kSubs));
+                    full |= slot >= S::kRoom - S::kRound - 1;
+                }
+            }
+            if (__syncthreads_or(full)) cut_lists<RW>(keys, count, least, keep);
+        }
     }
     cut_lists<RW>(keys, count, least, keep);
     for (int j = threadIdx.x; j < RW * keep; j += kSelectThreads) {
@@ -223,16 +306,30 @@ __global__ __launch_bounds__(kSelectThreads) void k_lp_select(const float* __res
     }
 }
 
-// The best `keep` of n keys in LDS, in order, to `out` (LDS too).
-__device__ __forceinline__ void best_keys(const u64* keys, int n, int keep, u64* out) {
-    for (int e = threadIdx.x; e < keep; e += kTopThreads) out[e] = 0;
+// The best `keep` of the n keys of `splits` lists in LDS to `out` (LDS too), in order; 0
+// behind the last.  A key below the last of a full list is not one of them.  `left` (LDS)
+// has room for n.
+template <int THREADS>
+__device__ __forceinline__ void best_keys(const u64* keys, int n, int keep, u64* left, u64* out) {
+    __shared__ u64 s_bar;
+    __shared__ int s_count;
+    if (threadIdx.x == 0) s_bar = 0, s_count = 0;
+    for (int e = threadIdx.x; e < keep; e += THREADS) out[e] = 0;
     __syncthreads();
-    for (int e = threadIdx.x; e < n; e += kTopThreads) {
-        const u64 own = keys[e];
+    for (int e = keep - 1 + keep * threadIdx.x; e < n; e += keep * THREADS)
+        if (keys[e] != 0) atomicMax(&s_bar, keys[e]);
+    __syncthreads();
+    const u64 bar = s_bar;
+    for (int e = threadIdx.x; e < n; e += THREADS)
+        if (keys[e] != 0 && keys[e] >= bar) left[atomicAdd(&s_count, 1)] = keys[e];
+    __syncthreads();
+    const int m = s_count;
+    for (int e = threadIdx.x; e < m; e += THREADS) {
+        const u64 own = left[e];
         int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) rank += keys[j] > own ? 1 : 0;
-        if (own != 0 && rank < keep) out[rank] = own;
+#pragma unroll 8
+        for (int j = 0; j < m; ++j) rank += left[j] > own ? 1 : 0;
+        if (rank < keep) out[rank] = own;
     }
     __syncthreads();
 }
@@ -244,93 +341,100 @@ __global__ __launch_bounds__(kTopThreads) void k_lp_merge(const u64* __restrict_
                                                           int keep, bool first,
                                                           u64* __restrict__ running) {
     __shared__ u64 s_keys[(kMostSplits + 1) * kMostKeep], s_out[kMostKeep];
+    extern __shared__ __align__(16) uint8_t lds[];
     const int64_t row = blockIdx.x;
     const int n = splits * keep;
     for (int e = threadIdx.x; e < n; e += kTopThreads) s_keys[e] = lists[row * n + e];
     if (!first)
         for (int e = threadIdx.x; e < keep; e += kTopThreads) s_keys[n + e] = running[row * keep + e];
     __syncthreads();
-    best_keys(s_keys, first ? n : n + keep, keep, s_out);
+    best_keys<kTopThreads>(s_keys, first ? n : n + keep, keep, reinterpret_cast<u64*>(lds), s_out);
     for (int e = threadIdx.x; e < keep; e += kTopThreads) running[row * keep + e] = s_out[e];
 }
 
 // The best classes of a row among those of its best tiles of G.
-template <typename E, bool CODES, int G>
-__global__ __launch_bounds__(kTopThreads) void k_lp_top(SoftmaxArgs a, const u64* __restrict__ lists,
-                                                        int splits, int keep) {
-    constexpr int kLanes = 8, kAtOnce = kTopThreads / kLanes;
+template <typename E, bool CODES, int G, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_lp_top(SoftmaxArgs a, const u64* __restrict__ lists,
+                                                    int splits, int keep) {
+    constexpr int kLanes = 8, kAtOnce = THREADS / kLanes;
     extern __shared__ __align__(16) uint8_t lds[];
-    const int n = splits * keep;
-    u64* s_keys = reinterpret_cast<u64*>(lds);
-    u64* s_best = s_keys + n;
-    double* s_h = reinterpret_cast<double*>(s_best + keep);
-    double* s_x = s_h + a.dim;
+    __shared__ double s_bar;
+    __shared__ int s_count;
+    const int n = splits * keep, m = keep * G;
+    double* s_h = reinterpret_cast<double*>(lds);             // the row
+    u64* s_best = reinterpret_cast<u64*>(s_h + a.dim);        // its best tiles
+    double* s_most = reinterpret_cast<double*>(s_best + keep);  // the largest logit of each
+    double* s_x = s_most + keep;                              // their classes' logits
+    int* s_left = reinterpret_cast<int*>(s_x + m);            // those that may be wanted
+    u64* s_keys = reinterpret_cast<u64*>(s_x);                // before: the lists, twice
     const int64_t row = blockIdx.x;
     const float lse = a.lse[row];
     int32_t* ids = a.ids + row * a.top;
     float* logp = a.top_logp + row * a.top;
     if (!(lse > -INFINITY && lse < INFINITY)) {  // no class, or no number
-        for (int k = threadIdx.x; k < a.top; k += kTopThreads) {
+        for (int k = threadIdx.x; k < a.top; k += THREADS) {
             ids[k] = -1;
             logp[k] = lse == -INFINITY ? -INFINITY : NAN;
         }
         return;
     }
-    for (int e = threadIdx.x; e < n; e += kTopThreads) s_keys[e] = lists[row * n + e];
+    for (int e = threadIdx.x; e < n; e += THREADS) s_keys[e] = lists[row * n + e];
     const E* h = static_cast<const E*>(a.h) + row * a.ld_h;
-    for (int d = 4 * threadIdx.x; d < a.dim; d += 4 * kTopThreads) {
+    for (int d = 4 * threadIdx.x; d < a.dim; d += 4 * THREADS) {
         const float4 v = load_cols(h, d, a.dim, a.vec_h);
         s_h[d] = v.x, s_h[d + 1] = v.y, s_h[d + 2] = v.z, s_h[d + 3] = v.w;
     }
+    if (threadIdx.x == 0) s_bar = -INFINITY, s_count = 0;
     __syncthreads();
-    best_keys(s_keys, n, keep, s_best);
-    const int lane = threadIdx.x % kLanes, m = keep * G;
+    best_keys<THREADS>(s_keys, n, keep, s_keys + n, s_best);
+    auto class_of = [&](int e) { return key_tile(s_best[e / G]) * G + e % G; };
+    const int lane = threadIdx.x % kLanes;
     for (int e = threadIdx.x / kLanes; e < m; e += kAtOnce) {
-        const u64 key = s_best[e / G];
-        const int64_t cls = key_tile(key) * G + e % G;
+        const int64_t cls = class_of(e);
         double x = -INFINITY;
-        if (key != 0 && cls < a.classes) {
+        if (s_best[e / G] != 0 && cls < a.classes) {
             const float b = a.bias == nullptr ? 0.f : a.bias[cls];
             if (!(b < kLeast)) x = dot64<E, CODES, kLanes>(a, s_h, cls, lane) + (double)b;
         }
         if (lane == 0) s_x[e] = x;
     }
     __syncthreads();
-    if (threadIdx.x >= 64) return;
-    // a wave takes the best `top` times: each lane knows the best of its elements
-    auto better = [&](double x, int64_t c, double y, int64_t d) { return x > y || (x == y && c < d); };
-    auto of = [&](int e) { return key_tile(s_best[e / G]) * G + e % G; };
-    double x = -INFINITY;
-    int64_t cls = 0x7FFFFFFFFFFFFFFF;
-    int at = -1;
-    auto scan = [&] {
-        x = -INFINITY, cls = 0x7FFFFFFFFFFFFFFF, at = -1;
-        for (int e = threadIdx.x; e < m; e += 64) {
-            const double y = s_x[e];
-            if (y > -INFINITY && better(y, of(e), x, cls)) x = y, cls = of(e), at = e;
+    // at least `top` classes are at or above the top-th largest of the tiles' largest
+    if (threadIdx.x < keep) {
+        double v = -INFINITY;
+#pragma unroll 8
+        for (int e = 0; e < G; ++e) v = fmax(v, s_x[threadIdx.x * G + e]);
+        s_most[threadIdx.x] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < keep) {
+        const double own = s_most[threadIdx.x];
+        int rank = 0;
+        for (int k = 0; k < keep; ++k)
+            rank += s_most[k] > own || (s_most[k] == own && k < (int)threadIdx.x) ? 1 : 0;
+        if (rank == a.top - 1) s_bar = own;
+    }
+    __syncthreads();
+    const double bar = s_bar;
+    for (int e = threadIdx.x; e < m; e += THREADS)
+        if (s_x[e] > -INFINITY && s_x[e] >= bar) s_left[atomicAdd(&s_count, 1)] = e;
+    __syncthreads();
+    const int c = s_count;
+    for (int k = threadIdx.x; k < c; k += THREADS) {
+        const double x = s_x[s_left[k]];
+        const int64_t cls = class_of(s_left[k]);
+        int rank = 0;
+        for (int j = 0; j < c && rank < a.top; ++j) {
+            const double y = s_x[s_left[j]];
+            rank += y > x || (y == x && class_of(s_left[j]) < cls) ? 1 : 0;
         }
-    };
-    scan();
-    for (int k = 0; k < a.top; ++k) {
-        double bx = x;
-        int64_t bc = cls;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const double y = __shfl_xor(bx, off);
-            const int64_t d = __shfl_xor((long long)bc, off);
-            if (better(y, d, bx, bc)) bx = y, bc = d;
-        }
-        const bool none = bx == -INFINITY;
-        if (threadIdx.x == 0) {
-            const float l = (float)(bx - (double)lse);
-            ids[k] = none ? -1 : (int32_t)bc;
-            logp[k] = none ? -INFINITY : l > 0.f ? 0.f : l;
-        }
-        if (!none && bc == cls) {
-            s_x[at] = -INFINITY;
-            scan();
+        if (rank < a.top) {
+            const float l = (float)(x - (double)lse);
+            ids[rank] = (int32_t)cls;
+            logp[rank] = l > 0.f ? 0.f : l;
         }
     }
+    for (int k = c + threadIdx.x; k < a.top; k += THREADS) ids[k] = -1, logp[k] = -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -352,18 +456,21 @@ int select_splits(int64_t rows, int64_t tiles, int rw) {
 
 template <int RW>
 hipError_t select(const float* best, int64_t ld, int64_t rows, int64_t tiles, int64_t tile0,
-                  int splits, int keep, u64* lists, hipStream_t s) {
+                  int splits, int keep, const float4* part, int64_t slots, u64* lists, hipStream_t s) {
     SM_TRY(allow_lds<&k_lp_select<RW>>(kSelectKeys * 8));
     k_lp_select<RW><<<dim3((uint32_t)div_up(rows, RW), (uint32_t)splits), kSelectThreads,
                       kSelectKeys * 8, s>>>(best, ld, rows, tiles, tile0, div_up(tiles, splits),
-                                            keep, lists);
+                                            keep, part, (int)slots, lists);
     return hipGetLastError();
 }
 
 template <typename E, bool CODES, int G>
 hipError_t finish(const SoftmaxArgs& a, const AnswerPlan& p, const float4* part, int64_t slots,
                   int64_t pad, int64_t rows, int splits, const u64* lists, hipStream_t s) {
-    if (rows < 16 * kCus)
+    if (rows < kCus)
+        k_lp_rows<E, CODES, 256><<<dim3((uint32_t)rows), kBlock, 0, s>>>(a, part, (int)slots, pad,
+                                                                        rows, 0);
+    else if (rows < 16 * kCus)
         k_lp_rows<E, CODES, 64><<<dim3((uint32_t)div_up(rows, 4)), kBlock, 0, s>>>(
             a, part, (int)slots, pad, rows, 0);
     else
@@ -372,8 +479,17 @@ hipError_t finish(const SoftmaxArgs& a, const AnswerPlan& p, const float4* part,
         }));
     SM_TRY(hipGetLastError());
     if (a.top == 0) return hipSuccess;
-    const int lds = 8 * (splits * p.keep + p.keep + a.dim + p.keep * G);
-    k_lp_top<E, CODES, G><<<dim3((uint32_t)rows), kTopThreads, lds, s>>>(a, lists, splits, p.keep);
+    const int lists_ = 2 * splits * p.keep, logits = p.keep * G + (p.keep * G + 1) / 2;
+    const int lds = 8 * (a.dim + 2 * p.keep + (lists_ > logits ? lists_ : logits));
+    if (rows < kCus) {
+        constexpr auto* kKernel = &k_lp_top<E, CODES, G, 1024>;
+        if (lds > 64 * 1024) SM_TRY(allow_lds<kKernel>(kTopLds));
+        kKernel<<<dim3((uint32_t)rows), 1024, lds, s>>>(a, lists, splits, p.keep);
+    } else {
+        constexpr auto* kKernel = &k_lp_top<E, CODES, G, kTopThreads>;
+        if (lds > 64 * 1024) SM_TRY(allow_lds<kKernel>(kTopLds));
+        kKernel<<<dim3((uint32_t)rows), kTopThreads, lds, s>>>(a, lists, splits, p.keep);
+    }
     return hipGetLastError();
 }
 
@@ -440,9 +556,9 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             slots += more;
             if (a.top == 0) continue;
             splits = select_splits(pad, tiles, 16);
-            SM_TRY(select<16>(best, pad, a.n, tiles, t0, splits, p.keep, lists, s));
+            SM_TRY(select<16>(best, pad, a.n, tiles, t0, splits, p.keep, part, slots, lists, s));
             if (!pieces) continue;
-            k_lp_merge<<<dim3((uint32_t)a.n), kTopThreads, 0, s>>>(lists, splits, p.keep, t0 == 0,
+            k_lp_merge<<<dim3((uint32_t)a.n), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(lists, splits, p.keep, t0 == 0,
                                                                    running);
             SM_TRY(hipGetLastError());
         }
@@ -480,9 +596,9 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             SM_TRY((lse_pass<E, true>(sm, l, true, &slots, s)));
             if (a.top == 0) continue;
             splits = select_splits(pad, tiles, 32);
-            SM_TRY(select<32>(best, pad, rows, tiles, t0, splits, p.keep, lists, s));
+            SM_TRY(select<32>(best, pad, rows, tiles, t0, splits, p.keep, part, slots, lists, s));
             if (!pieces) continue;
-            k_lp_merge<<<dim3((uint32_t)rows), kTopThreads, 0, s>>>(lists, splits, p.keep, t0 == 0,
+            k_lp_merge<<<dim3((uint32_t)rows), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(lists, splits, p.keep, t0 == 0,
                                                                     running);
             SM_TRY(hipGetLastError());
         }

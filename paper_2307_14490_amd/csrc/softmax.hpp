@@ -428,7 +428,7 @@ struct PassArgs {
     // split and wave along Y: [slot][part_rows]...
     int64_t part_first, part_rows;
     float2* lse_part;      // loss: maximum and sum
-    float4* stat_part;     // answers: maximum, sum and first moment
+    float4* stat_part;     // answers: top, sum and first moment, and the largest logit
     float* best;           // answers: each tile's largest logit [y tile][best_ld], or null
     int64_t best_ld;
     float* part;           // gradient: [dp], or null: to `out`
@@ -685,7 +685,7 @@ void k_sm_lse(PassArgs a) {
     const int rec_bytes = record_bytes(nfrag, Kind<E>::kParts, a.forms);
     const XTiles<XB> xt = x_tiles_of<XB>(a, at.x_block, xg, rec_bytes);
     Operand<E> x[XB][2 * ND];
-    float xmul[XB], top[XB], sum[XB], first[XB];
+    float xmul[XB], top[XB], sum[XB], first[XB], most[XB];
 #pragma unroll
     for (int b = 0; b < XB; ++b) {
         if constexpr (STAGED) {
@@ -697,6 +697,7 @@ void k_sm_lse(PassArgs a) {
         top[b] = ANSWER ? kLeast : -INFINITY;
         sum[b] = 0.f;
         first[b] = 0.f;
+        most[b] = kFloor;
     }
     // DIRECT: no headers; there is no bias then, only the end of the classes
     const int y_bytes = DIRECT ? 2 * ND * 1024 : rec_bytes;
@@ -746,6 +747,7 @@ void k_sm_lse(PassArgs a) {
                         if (half == 0 && xt.in[b])
                             a.best[yt * a.best_ld + xt.t[b] * 32 + lane] = of_tile;
                     }
+                    most[b] = fmaxf(most[b], m);
                     if (__ballot(m > top[b] + kRiseAnswer) != 0) {
                         const Stats s = raise({top[b], sum[b], first[b]}, fmaxf(m, top[b]));
                         top[b] = s.top, sum[b] = s.sum, first[b] = s.first;
@@ -785,14 +787,16 @@ void k_sm_lse(PassArgs a) {
             // the halves hold different classes of the same row
             Stats s = join({top[b], sum[b], first[b]},
                            {__shfl_xor(top[b], 32), __shfl_xor(sum[b], 32), __shfl_xor(first[b], 32)});
+            float largest = fmaxf(most[b], __shfl_xor(most[b], 32));
             if (half == 0 && xt.in[b]) {
                 float4* out = a.stat_part + ((int64_t)at.split * yw + yg) * a.part_rows +
                               xt.t[b] * 32 + lane;
                 if (!a.first) {
                     const float4 p = *out;
                     s = join(s, {p.x, p.y, p.z});
+                    largest = fmaxf(largest, p.w);
                 }
-                *out = make_float4(s.top, s.sum, s.first, 0.f);
+                *out = make_float4(s.top, s.sum, s.first, largest);
             }
         }
         return;
@@ -1088,7 +1092,8 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
             for (int off = 16; off < 64; off <<= 1)
                 s = join(s, {__shfl_xor(s.top, off), __shfl_xor(s.sum, off),
                              __shfl_xor(s.first, off)});
-            if (lane < 16) s_part[wave][16 * b + lane] = make_float4(s.top, s.sum, s.first, 0.f);
+            // the top of few rows is the maximum
+            if (lane < 16) s_part[wave][16 * b + lane] = make_float4(s.top, s.sum, s.first, s.top);
         } else {
 #pragma unroll
             for (int off = 16; off < 64; off <<= 1) {
@@ -1108,7 +1113,7 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
             const Part q = s_part[k][threadIdx.x];
             if constexpr (ANSWER) {
                 const Stats s = join({r.x, r.y, r.z}, {q.x, q.y, q.z});
-                r = make_float4(s.top, s.sum, s.first, 0.f);
+                r = make_float4(s.top, s.sum, s.first, s.top);
             } else {
                 const float m = fmaxf(r.x, q.x);
                 r.y = r.y * exp_below(r.x, m) + q.y * exp_below(q.x, m);

@@ -350,6 +350,30 @@ def test_equal_logits_give_the_lowest_classes(n, dtype):
     assert a.ids[0].tolist() == list(range(20))
 
 
+@pytest.mark.parametrize("top", [1, 20, 64])
+@pytest.mark.parametrize("n", [3, 40, 70])
+def test_more_tiles_above_the_bar_than_a_list_holds(n, top):
+    """Rows of zeros whose logits are the bias alone: all equal, rising, falling, and
+    nearly all classes out."""
+    classes, dim = 60_000, 8
+    op = P.LogProbs(n, classes, dim, dtype="bf16", top=top)
+    h = torch.zeros(n, dim, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(classes, dim, device="cuda").to(torch.bfloat16)
+    up = torch.arange(classes, device="cuda", dtype=torch.float32) * 2.0 ** -12
+    few = torch.full((classes,), -math.inf, device="cuda")
+    few[59_000:59_000 + 3 * top:3] = up[:top]
+    for name, b, ids in (("equal", torch.zeros_like(up), torch.arange(top)),
+                         ("rising", up, classes - 1 - torch.arange(top)),
+                         ("falling", up.flip(0), torch.arange(top)),
+                         ("few in", few, 59_000 + 3 * torch.arange(top).flip(0))):
+        say(f"{name}, {n} rows, best {top}")
+        a = op.log_probs(h, w, bias=b)
+        assert (a.ids.cpu() == ids.to(torch.int32)).all()
+        want = torch.log_softmax(b.double(), 0)[ids.cuda()]
+        assert (a.top_logp - want).abs().max().item() <= 1e-5
+        op.check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "q8"])
 @pytest.mark.parametrize("n", [6, 75])
 @pytest.mark.parametrize("lowest", [-math.inf, -3.4e38, -1e29])
