@@ -12,6 +12,8 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple
 
+import numpy as np
+
 from . import head as _head
 from .binding import (HUGE_DTYPE_Q8, HUGE_ERR_INVALID_ARG, HugeError, HugeGradTensor,
                       HugeLogProbsConfig, _arg, _dptr, _ok)
@@ -267,28 +269,36 @@ class LogProbs(_Status):
 # --------------------------------------------------------------------------- #
 # Norms of gradients
 # --------------------------------------------------------------------------- #
+_TABLE = [("d_grad", "u8"), ("n", "i8"), ("dtype", "i4"), ("fill", "i4")]  # HugeGradTensor
+
+
 def _grads(grads, what):
     """The list, its device and its table for the C calls."""
     import torch
+    types = {torch.float32: _DTYPES["f32"], torch.bfloat16: _DTYPES["bf16"]}
     grads = list(grads)
     if not grads:
         raise ValueError(f"{what}: no gradients")
-    table = (HugeGradTensor * len(grads))()
-    for k, (t, g) in enumerate(zip(table, grads)):
+    for k, g in enumerate(grads):
         if not (isinstance(g, torch.Tensor) and g.is_cuda and g.is_contiguous()
-                and g.dtype in (torch.float32, torch.bfloat16)):
+                and g.dtype in types):
             _arg(g, ("float32", "bfloat16"), f"{what}[{k}]")
-        if g.device != grads[0].device:
-            raise ValueError(f"{what}[{k}]: on {g.device}, expected {grads[0].device}")
-        t.d_grad, t.n, t.dtype = g.data_ptr(), g.numel(), _dtype_code(g, what)
-    return grads, grads[0].device, table
+    device = grads[0].device
+    if len({g.get_device() for g in grads}) > 1:
+        k = next(k for k, g in enumerate(grads) if g.device != device)
+        raise ValueError(f"{what}[{k}]: on {grads[k].device}, expected {device}")
+    table = np.empty(len(grads), _TABLE)
+    table["d_grad"] = [g.data_ptr() for g in grads]
+    table["n"] = [g.numel() for g in grads]
+    table["dtype"] = [types[g.dtype] for g in grads]
+    return grads, device, table.ctypes.data_as(ctypes.POINTER(HugeGradTensor)), table
 
 
 def grad_norm(grads, stream=None):
     """The 2-norm over all elements of a list of contiguous float32 or bfloat16 GPU tensors
     (one float32 element), by huge_grad_norm."""
     import torch
-    grads, device, table = _grads(grads, "grad_norm")
+    grads, device, table, _keep = _grads(grads, "grad_norm")
     L = _head.load()
     with _on(device, stream, grads) as st:
         norm = torch.empty(1, dtype=torch.float32, device=device)
@@ -304,7 +314,7 @@ def clip_grads(grads, max_norm, stream=None):
     huge_clip_grads, and returns the norm before.  They stay as they are where it is
     not finite.  The tensors must share no memory."""
     import torch
-    grads, device, table = _grads(grads, "clip_grads")
+    grads, device, table, _keep = _grads(grads, "clip_grads")
     if not float(max_norm) > 0:
         raise ValueError(f"clip_grads: max_norm {max_norm}")
     _head._apart(grads, "clip_grads: gradients")

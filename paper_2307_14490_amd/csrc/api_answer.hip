@@ -18,6 +18,11 @@ bool matrix_ok(const void* p, int64_t ld, int32_t dim, size_t size) {
     return p != nullptr && on(p, size) && ld >= dim;
 }
 
+// Whether rows start on a number of bytes, that many at a time being whole rows.
+bool starts_on(const void* p, int64_t ld, size_t size, size_t bytes) {
+    return p == nullptr || (on(p, bytes) && ld * size % bytes == 0);
+}
+
 // Codes and scales of rows in 8 bits.
 bool bytes_ok(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
               int32_t dim) {
@@ -71,7 +76,8 @@ SoftmaxArgs answer_call(const huge_log_probs_config* c, const void* h, int64_t l
 // A launch's tensors and what goes on with each full one.
 template <typename Tensor, typename Launch>
 huge_status clip_launches(int32_t count, Tensor tensor, Launch launch) {
-    ClipArgs a{};
+    ClipArgs a;
+    a.count = 0, a.chunks = 0;
     auto go = [&] {
         if (a.count == 0) return hipSuccess;
         const hipError_t e = launch(a);
@@ -83,10 +89,8 @@ huge_status clip_launches(int32_t count, Tensor tensor, Launch launch) {
         if (g.n == 0) continue;
         const int64_t more = (g.n + kClipChunk - 1) / kClipChunk;
         if (a.count == kClipTensors || (int64_t)a.chunks + more > kMaxRows) HEAD_TRY(go());
-        ClipTensor t{};
-        t.g = g.d_grad, t.n = g.n, t.first = a.chunks, t.dtype = (int16_t)g.dtype;
-        t.vec = on(g.d_grad, 16);
-        a.t[a.count++] = t;
+        a.t[a.count] = {g.d_grad, 2 * g.n + (g.dtype == HUGE_DTYPE_BF16 ? 1 : 0)};
+        a.first[a.count++] = a.chunks;
         a.chunks += (uint32_t)more;
     }
     HEAD_TRY(go());
@@ -115,14 +119,21 @@ huge_status norm_factor(int32_t count, Tensor tensor, double scale, double max_n
                         void* ws, hipStream_t s) {
     float* factor = static_cast<float*>(ws);
     double* part = reinterpret_cast<double*>(static_cast<uint8_t*>(ws) + kFactorBytes);
-    int parts = 0;
+    int parts = 0, left = 0;
+    for (int32_t k = 0; k < count; ++k) left += tensor(k).n > 0;
+    bool done = false;
     const huge_status st = clip_launches(count, tensor, [&](const ClipArgs& a) {
+        left -= a.count;
+        if (parts == 0 && left == 0 && a.chunks <= kClipSmall) {
+            done = true;
+            return launch_norm_small(a, scale, max_norm, d_norm, factor, s);
+        }
         int more = 0;
         const hipError_t e = launch_squares(a, part + parts, &more, s);
         parts += more;
         return e;
     });
-    if (st != HUGE_OK) return st;
+    if (st != HUGE_OK || done) return st;
     HEAD_TRY(launch_norm_factor(part, parts, scale, max_norm, d_norm, factor, s));
     return HUGE_OK;
 }
@@ -157,6 +168,10 @@ huge_status huge_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual,
     a.vec = dim % 4 == 0 && fours(d_x, ld_x, dtype) && on(d_gamma, 16) &&
             (!d_residual || (fours(d_residual, ld_residual, dtype) && fours(d_total, ld_total, dtype))) &&
             (d_y ? fours(d_y, ld_y, dtype) : on(d_codes, 4) && ld_codes % 4 == 0);
+    a.eights = dtype == HUGE_DTYPE_BF16 && dim % 8 == 0 && on(d_gamma, 16) &&
+               starts_on(d_x, ld_x, e, 16) && starts_on(d_residual, ld_residual, e, 16) &&
+               starts_on(d_total, ld_total, e, 16) && starts_on(d_y, ld_y, e, 16) &&
+               starts_on(d_codes, ld_codes, 1, 8);
     HEAD_TRY(launch_rms(a, static_cast<hipStream_t>(stream)));
     return HUGE_OK;
 }
@@ -192,6 +207,9 @@ huge_status huge_rms_norm_backward(const void* d_dy, int64_t ld_dy, const void* 
     a.vec = dim % 4 == 0 && fours(d_total, ld_total, dtype) && fours(d_dy, ld_dy, dtype) &&
             (!d_dtotal || fours(d_dtotal, ld_dtotal, dtype)) &&
             (!d_dx || fours(d_dx, ld_dx, dtype)) && on(d_gamma, 16);
+    a.eights = dtype == HUGE_DTYPE_BF16 && dim % 8 == 0 && on(d_gamma, 16) &&
+               starts_on(d_total, ld_total, e, 16) && starts_on(d_dy, ld_dy, e, 16) &&
+               starts_on(d_dtotal, ld_dtotal, e, 16) && starts_on(d_dx, ld_dx, e, 16);
     HEAD_TRY(launch_rms_backward(a, d_dgamma, static_cast<hipStream_t>(stream)));
     return HUGE_OK;
 }
@@ -208,6 +226,8 @@ huge_status huge_quantise_rows(const void* d_x, int64_t ld_x, int64_t n, int32_t
     a.x = d_x, a.ld_x = ld_x, a.codes = d_codes, a.ld_codes = ld_codes, a.scales = d_scales;
     a.ld_scales = ld_scales, a.n = n, a.dim = dim, a.dtype = dtype;
     a.vec = dim % 4 == 0 && fours(d_x, ld_x, dtype) && on(d_codes, 4) && ld_codes % 4 == 0;
+    a.eights = dim % 8 == 0 && starts_on(d_x, ld_x, elem(dtype), 16) &&
+               starts_on(d_codes, ld_codes, 1, 8);
     HEAD_TRY(launch_to_bytes(a, static_cast<hipStream_t>(stream)));
     return HUGE_OK;
 }
@@ -225,6 +245,8 @@ huge_status huge_dequantise_rows(const uint8_t* d_codes, int64_t ld_codes, const
     a.scales = const_cast<uint8_t*>(d_scales), a.ld_scales = ld_scales;
     a.n = n, a.dim = dim, a.dtype = dtype;
     a.vec = dim % 4 == 0 && fours(d_y, ld_y, dtype) && on(d_codes, 4) && ld_codes % 4 == 0;
+    a.eights = dim % 8 == 0 && starts_on(d_y, ld_y, elem(dtype), 16) &&
+               starts_on(d_codes, ld_codes, 1, 8);
     HEAD_TRY(launch_from_bytes(a, static_cast<hipStream_t>(stream)));
     return HUGE_OK;
 }

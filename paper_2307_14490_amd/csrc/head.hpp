@@ -52,6 +52,7 @@ struct RmsArgs {
     float* rstd;
     float* partial;    // backward pass: [workgroups][dim], or null
     bool vec;          // four elements at a time
+    bool eights;       // eight: 16 bytes of bf16 rows, 8 of codes
 };
 hipError_t launch_rms(const RmsArgs& a, hipStream_t s);
 hipError_t launch_rms_backward(const RmsArgs& a, float* dgamma, hipStream_t s);
@@ -68,25 +69,29 @@ __device__ __forceinline__ float byte_scale(uint32_t b) {
 // ---------------------------------------------------------------------------
 // Norm over many tensors (k_clip.hip)
 // ---------------------------------------------------------------------------
-constexpr int kClipTensors = 64;       // tensors of a launch
+constexpr int kClipTensors = 150;      // tensors of a launch: 3000 bytes of arguments
 constexpr int kClipChunk = 16384;      // elements of a workgroup at a time
 constexpr uint32_t kClipBlocks = 2048; // workgroups of a launch, at most
+constexpr uint32_t kClipSmall = 4;     // chunks that one workgroup takes, up to the factor
 
 struct ClipTensor {
     void* g;
-    int64_t n;
-    uint32_t first;   // its first chunk among the launch's
-    int16_t dtype;
-    bool vec;         // 16 bytes at a time
+    int64_t n_bf16;   // elements, times two, plus one for bf16
 };
 struct ClipArgs {
     ClipTensor t[kClipTensors];
+    uint32_t first[kClipTensors];  // a tensor's first chunk among the launch's
     int32_t count;
     uint32_t chunks;
 };
+// The sums of squares of a launch's tensors: *parts entries of `part`.
 hipError_t launch_squares(const ClipArgs& a, double* part, int* parts, hipStream_t s);
+// The norm of `scale` times the elements behind `parts` entries, and the factor for them.
 hipError_t launch_norm_factor(const double* part, int parts, double scale, double max_norm,
                               float* norm, float* factor, hipStream_t s);
+// Both at once, of up to kClipSmall chunks.
+hipError_t launch_norm_small(const ClipArgs& a, double scale, double max_norm, float* norm,
+                             float* factor, hipStream_t s);
 hipError_t launch_scale(const ClipArgs& a, const float* factor, hipStream_t s);
 
 // ---------------------------------------------------------------------------

@@ -88,32 +88,38 @@ __device__ __forceinline__ float row_max(float v, double* s) {
     return v;
 }
 
+// What the pass over the logits leaves: `slots` entries of each row.
+struct Parts {
+    const float4* p;
+    int64_t of_slot, of_row;  // strides
+    int32_t slots;
+    __device__ __forceinline__ float4 at(int64_t row, int64_t slot) const {
+        return p[slot * of_slot + row * of_row];
+    }
+};
+
+// Row i, by LANES threads.  s_join: of a workgroup of four waves where LANES is all of it.
 template <typename E, bool CODES, int LANES>
-__global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, const float4* __restrict__ part,
-                                                    int slots, int64_t pad, int64_t rows,
-                                                    int64_t first) {
-    __shared__ double s_join[4];
-    const int lane = threadIdx.x % LANES;
-    const int64_t i = (first + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
-    if (i >= rows) return;
+__device__ __forceinline__ void answer_row(const SoftmaxArgs& a, const Parts& part, int64_t i,
+                                           int lane, double* s_join) {
     // the top of all slots first, then their sums from it: one exponential a slot, none of
     // which waits for another
     float top = kLeast;
-#pragma unroll 4
-    for (int k = lane; k < slots; k += LANES) top = fmaxf(top, part[(int64_t)k * pad + i].x);
+#pragma unroll 8
+    for (int k = lane; k < part.slots; k += LANES) top = fmaxf(top, part.at(i, k).x);
     top = row_max<LANES>(top, s_join);
-    float sum = 0.f, first_ = 0.f;
-#pragma unroll 4
-    for (int k = lane; k < slots; k += LANES) {
-        const float4 p = part[(int64_t)k * pad + i];
+    float sum = 0.f, first = 0.f;
+#pragma unroll 8
+    for (int k = lane; k < part.slots; k += LANES) {
+        const float4 p = part.at(i, k);
         const Stats s = raise({p.x, p.y, p.z}, top);
         sum += s.sum;
-        first_ += s.first;
+        first += s.first;
     }
-    const Stats s{top, row_add<LANES>(sum, s_join), row_add<LANES>(first_, s_join)};
-    const float logs = logf(s.sum);
-    const float lse = s.sum == 0.f ? -INFINITY : s.top + logs;
-    float entropy = s.sum == 0.f ? 0.f : logs - 0.69314718055994531f * (s.first / s.sum);
+    sum = row_add<LANES>(sum, s_join), first = row_add<LANES>(first, s_join);
+    const float logs = logf(sum);
+    const float lse = sum == 0.f ? -INFINITY : top + logs;
+    float entropy = sum == 0.f ? 0.f : logs - 0.69314718055994531f * (first / sum);
     entropy = entropy < 0.f ? 0.f : entropy;  // rounding alone takes it below 0
     float logp = 0.f;
     if (a.labels != nullptr) {
@@ -153,6 +159,14 @@ __global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, const float4*
         if (a.entropy != nullptr) a.entropy[i] = entropy;
         if (a.logp != nullptr) a.logp[i] = logp;
     }
+}
+
+template <typename E, bool CODES, int LANES>
+__global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, Parts part, int64_t rows,
+                                                    int64_t first) {
+    __shared__ double s_join[4];
+    const int64_t i = (first + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
+    if (i < rows) answer_row<E, CODES, LANES>(a, part, i, threadIdx.x % LANES, s_join);
 }
 
 // ---------------------------------------------------------------------------
@@ -207,14 +221,20 @@ __device__ __forceinline__ void cut_lists(u64* keys, int* count, uint32_t* least
     __syncthreads();
 }
 
-template <int RW>
-__global__ __launch_bounds__(kSelectThreads) void k_lp_select(const float* __restrict__ best,
+// The last row of workgroups of a call's last search forms the rows' own results beside it.
+template <typename E, bool CODES, int RW>
+__global__ __launch_bounds__(kSelectThreads) void k_lp_select(SoftmaxArgs a,
+                                                              const float* __restrict__ best,
                                                               int64_t ld, int64_t rows,
                                                               int64_t tiles, int64_t tile0,
-                                                              int64_t per, int keep,
-                                                              const float4* __restrict__ part,
-                                                              int slots, u64* __restrict__ lists) {
+                                                              int64_t per, int splits, int keep,
+                                                              Parts part, u64* __restrict__ lists) {
     using S = Select<RW>;
+    if ((int)blockIdx.y == splits) {
+        const int64_t i = (int64_t)blockIdx.x * RW + threadIdx.x / S::kSubs;
+        if (i < rows) answer_row<E, CODES, S::kSubs>(a, part, i, threadIdx.x % S::kSubs, nullptr);
+        return;
+    }
     extern __shared__ __align__(16) uint8_t lds[];
     u64* keys = reinterpret_cast<u64*>(lds);  // [RW][kRoom]
     __shared__ int count[RW];
@@ -242,8 +262,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_lp_select(const float* __res
     if (keep <= S::kSubs) {
         float v = -INFINITY;
         if (in)
-#pragma unroll 4
-            for (int k = sub; k < slots; k += S::kSubs) v = fmaxf(v, part[k * ld + row].w);
+#pragma unroll 8
+            for (int k = sub; k < part.slots; k += S::kSubs) v = fmaxf(v, part.at(row, k).w);
         uint32_t* of_row = reinterpret_cast<uint32_t*>(lds);  // [sub][row]
         const uint32_t own = v > kLeast ? ordered(v) : 0;
         of_row[threadIdx.x] = own;
@@ -301,7 +321,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_lp_select(const float* __res
         const int k = j / keep;
         const int64_t out = (int64_t)blockIdx.x * RW + k;
         if (out < rows)
-            lists[(out * gridDim.y + blockIdx.y) * keep + j % keep] =
+            lists[(out * splits + blockIdx.y) * keep + j % keep] =
                 j % keep < count[k] ? keys[k * S::kRoom + j % keep] : 0;
     }
 }
@@ -454,31 +474,36 @@ int select_splits(int64_t rows, int64_t tiles, int rw) {
     return (int)(s < 1 ? 1 : s);
 }
 
-template <int RW>
-hipError_t select(const float* best, int64_t ld, int64_t rows, int64_t tiles, int64_t tile0,
-                  int splits, int keep, const float4* part, int64_t slots, u64* lists, hipStream_t s) {
-    SM_TRY(allow_lds<&k_lp_select<RW>>(kSelectKeys * 8));
-    k_lp_select<RW><<<dim3((uint32_t)div_up(rows, RW), (uint32_t)splits), kSelectThreads,
-                      kSelectKeys * 8, s>>>(best, ld, rows, tiles, tile0, div_up(tiles, splits),
-                                            keep, part, (int)slots, lists);
+// last: with the rows' own results.
+template <typename E, bool CODES, int RW>
+hipError_t select(const SoftmaxArgs& a, const float* best, int64_t ld, int64_t rows, int64_t tiles,
+                  int64_t tile0, int splits, int keep, const Parts& part, u64* lists, bool last,
+                  hipStream_t s) {
+    constexpr auto* kKernel = &k_lp_select<E, CODES, RW>;
+    SM_TRY(allow_lds<kKernel>(kSelectKeys * 8));
+    const dim3 grid((uint32_t)div_up(rows, RW), (uint32_t)(splits + (last ? 1 : 0)));
+    kKernel<<<grid, kSelectThreads, kSelectKeys * 8, s>>>(a, best, ld, rows, tiles, tile0,
+                                                          div_up(tiles, splits), splits, keep, part,
+                                                          lists);
     return hipGetLastError();
 }
 
+// What is left behind the passes: the rows' own results where nothing is to be found, or
+// the best classes.
 template <typename E, bool CODES, int G>
-hipError_t finish(const SoftmaxArgs& a, const AnswerPlan& p, const float4* part, int64_t slots,
-                  int64_t pad, int64_t rows, int splits, const u64* lists, hipStream_t s) {
-    if (rows < kCus)
-        k_lp_rows<E, CODES, 256><<<dim3((uint32_t)rows), kBlock, 0, s>>>(a, part, (int)slots, pad,
-                                                                        rows, 0);
-    else if (rows < 16 * kCus)
-        k_lp_rows<E, CODES, 64><<<dim3((uint32_t)div_up(rows, 4)), kBlock, 0, s>>>(
-            a, part, (int)slots, pad, rows, 0);
-    else
-        SM_TRY(in_launches(div_up(rows, 16), [&](dim3 grid, int64_t first) {
-            k_lp_rows<E, CODES, 16><<<grid, kBlock, 0, s>>>(a, part, (int)slots, pad, rows, first);
-        }));
-    SM_TRY(hipGetLastError());
-    if (a.top == 0) return hipSuccess;
+hipError_t finish(const SoftmaxArgs& a, const AnswerPlan& p, const Parts& part, int64_t rows,
+                  int splits, const u64* lists, hipStream_t s) {
+    if (a.top == 0) {
+        if (rows < kCus)
+            k_lp_rows<E, CODES, 256><<<dim3((uint32_t)rows), kBlock, 0, s>>>(a, part, rows, 0);
+        else if (rows < 16 * kCus)
+            k_lp_rows<E, CODES, 64><<<dim3((uint32_t)div_up(rows, 4)), kBlock, 0, s>>>(a, part, rows, 0);
+        else
+            SM_TRY(in_launches(div_up(rows, 16), [&](dim3 grid, int64_t first) {
+                k_lp_rows<E, CODES, 16><<<grid, kBlock, 0, s>>>(a, part, rows, first);
+            }));
+        return hipGetLastError();
+    }
     const int lists_ = 2 * splits * p.keep, logits = p.keep * G + (p.keep * G + 1) / 2;
     const int lds = 8 * (a.dim + 2 * p.keep + (lists_ > logits ? lists_ : logits));
     if (rows < kCus) {
@@ -543,27 +568,39 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
         if constexpr (!CODES) f.vec = a.vec && a.vec_h;
         const int64_t pad = 16 * p.few;
         const bool pieces = piece < all;
-        int64_t slots = 0;
+        int64_t slots = 0, all_slots = 0;
+        for (int64_t t0 = 0; t0 < all; t0 += piece) {
+            const int64_t c0 = t0 * 16, left = a.classes - c0;
+            const int64_t count = left < piece * 16 ? left : piece * 16;
+            all_slots += p.few == 1 ? few_grid<1>(count) : p.few == 2 ? few_grid<2>(count)
+                                                                      : few_grid<4>(count);
+        }
         int splits = 1;
         for (int64_t t0 = 0; t0 < all; t0 += piece) {
             const int64_t tiles = all - t0 < piece ? all - t0 : piece, c0 = t0 * 16;
             const int64_t count = a.classes - c0 < tiles * 16 ? a.classes - c0 : tiles * 16;
             const SoftmaxArgs q = classes_from<E, CODES>(f, c0, count);
             int64_t more = 0;
-            SM_TRY((p.few == 1   ? few_pass<E, 1, true, CODES>(q, part + slots * pad, &more, s, best)
-                    : p.few == 2 ? few_pass<E, 2, true, CODES>(q, part + slots * pad, &more, s, best)
-                                 : few_pass<E, 4, true, CODES>(q, part + slots * pad, &more, s, best)));
+            auto pass = [&](auto nb) {
+                return few_pass<E, decltype(nb)::value, true, CODES>(q, part, &more, s, best,
+                                                                     all_slots, slots);
+            };
+            SM_TRY(p.few == 1   ? pass(std::integral_constant<int, 1>{})
+                   : p.few == 2 ? pass(std::integral_constant<int, 2>{})
+                                : pass(std::integral_constant<int, 4>{}));
             slots += more;
             if (a.top == 0) continue;
             splits = select_splits(pad, tiles, 16);
-            SM_TRY(select<16>(best, pad, a.n, tiles, t0, splits, p.keep, part, slots, lists, s));
+            const Parts now{part, 1, all_slots, (int32_t)slots};
+            SM_TRY((select<E, CODES, 16>(a, best, pad, a.n, tiles, t0, splits, p.keep, now, lists,
+                                         t0 + tiles == all, s)));
             if (!pieces) continue;
-            k_lp_merge<<<dim3((uint32_t)a.n), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(lists, splits, p.keep, t0 == 0,
-                                                                   running);
+            k_lp_merge<<<dim3((uint32_t)a.n), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(
+                lists, splits, p.keep, t0 == 0, running);
             SM_TRY(hipGetLastError());
         }
-        return finish<E, CODES, 16>(a, p, part, slots, pad, a.n, pieces ? 1 : splits,
-                                    pieces ? running : lists, s);
+        return finish<E, CODES, 16>(a, p, Parts{part, 1, all_slots, (int32_t)all_slots}, a.n,
+                                    pieces ? 1 : splits, pieces ? running : lists, s);
     }
     // bf16 classes without a bias are used as they lie, as in the loss
     const bool direct = !CODES && sizeof(E) == 2 && a.bias == nullptr && a.vec16 &&
@@ -572,7 +609,10 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
     SoftmaxPlan sm = p.sm;
     sm.piece = p.piece;
     const int64_t rec = record_bytes(sm.dp / 16, sm.parts, 1);
-    if (direct) SM_TRY((pack<E, true, CODES>(sm, a, 0, 0, 1, s)));  // the rows
+    // ... and so are bf16 rows of whole operands, which a wave reads once
+    const bool x_direct = sizeof(E) == 2 && p.sm.chunks == 1 && a.dim == p.sm.dp &&
+                          sixteen(a.h, a.ld_h, kNh);
+    if (direct && !x_direct) SM_TRY((pack<E, true, CODES>(sm, a, 0, 0, 1, s)));  // the rows
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows;
         const SoftmaxArgs q = rows_from<E>(a, r0);
@@ -580,6 +620,7 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
         int splits = 1;
         PassArgs l{};
         l.x = a.ws + p.sm.h + r0 / kSmTile * rec, l.forms = 1, l.stat_part = part;
+        if (x_direct) l.x_direct = static_cast<const bf16_t*>(q.h), l.x_ld = a.ld_h, l.x_count = rows;
         l.x_tiles = div_up(rows, kSmTile);
         const int64_t pad = l.x_tiles * kSmTile;
         l.best = best, l.best_ld = pad;
@@ -587,7 +628,7 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             const int64_t tiles = all - t0 < piece ? all - t0 : piece, c0 = t0 * kSmTile;
             const int64_t count = a.classes - c0 < tiles * kSmTile ? a.classes - c0 : tiles * kSmTile;
             if (!direct && (pieces || r0 == 0))
-                SM_TRY((pack<E, true, CODES>(sm, a, c0, count, 1, s)));
+                SM_TRY((pack<E, true, CODES>(sm, a, c0, count, 1, s, !x_direct)));
             if (direct)
                 l.y_rows = static_cast<const bf16_t*>(a.w) + c0 * a.ld_w, l.ld = a.ld_w, l.classes = count;
             else
@@ -596,14 +637,16 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             SM_TRY((lse_pass<E, true>(sm, l, true, &slots, s)));
             if (a.top == 0) continue;
             splits = select_splits(pad, tiles, 32);
-            SM_TRY(select<32>(best, pad, rows, tiles, t0, splits, p.keep, part, slots, lists, s));
+            SM_TRY((select<E, CODES, 32>(q, best, pad, rows, tiles, t0, splits, p.keep,
+                                         Parts{part, pad, 1, (int32_t)slots}, lists,
+                                         t0 + tiles == all, s)));
             if (!pieces) continue;
             k_lp_merge<<<dim3((uint32_t)rows), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(lists, splits, p.keep, t0 == 0,
                                                                     running);
             SM_TRY(hipGetLastError());
         }
-        SM_TRY((finish<E, CODES, 32>(q, p, part, slots, pad, rows, pieces ? 1 : splits,
-                                     pieces ? running : lists, s)));
+        SM_TRY((finish<E, CODES, 32>(q, p, Parts{part, pad, 1, (int32_t)slots}, rows,
+                                     pieces ? 1 : splits, pieces ? running : lists, s)));
     }
     return hipSuccess;
 }

@@ -27,40 +27,92 @@ __device__ __forceinline__ int scale_exponent(uint32_t big) {
     return e < kByteLeast ? kByteLeast : e;
 }
 
-// The largest over eight lanes, aligned, all of which are active (as xor_add).
-__device__ __forceinline__ uint32_t max_of_eight(uint32_t v) {
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// W elements of a row: four, or eight of bf16 rows that are whole aligned eights (16 bytes).
+template <int W>
+struct Cells {
+    float v[W];
+};
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+template <int W, bool WHOLE, typename E>
+__device__ __forceinline__ Cells<W> load_cells(const E* row, int c, int D) {
+    Cells<W> r;
+    if constexpr (W == 4) {
+        const Few f = load_few<WHOLE>(row, c, D);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[e] = f.v[e];
+    } else if constexpr (sizeof(E) == 4) {
+        const float4 p = load_chunk(row, 2 * c), q = load_chunk(row, 2 * c + 1);
+        r = {{p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w}};
+    } else {
+        const u16x8 q = *reinterpret_cast<const u16x8*>(row + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = __uint_as_float((uint32_t)q[e] << 16);
+    }
+    return r;
+}
+
+template <int W, bool WHOLE, typename E>
+__device__ __forceinline__ void store_cells(E* row, int c, int D, const Cells<W>& r) {
+    if constexpr (W == 4) {
+        store_few<WHOLE>(row, c, D, Few{{r.v[0], r.v[1], r.v[2], r.v[3]}});
+    } else if constexpr (sizeof(E) == 4) {
+        store_chunk(row, 2 * c, make_float4(r.v[0], r.v[1], r.v[2], r.v[3]));
+        store_chunk(row, 2 * c + 1, make_float4(r.v[4], r.v[5], r.v[6], r.v[7]));
+    } else {
+        const f32x8 q = {r.v[0], r.v[1], r.v[2], r.v[3], r.v[4], r.v[5], r.v[6], r.v[7]};
+        *reinterpret_cast<bf16x8*>(row + 8 * c) = __builtin_convertvector(q, bf16x8);
+    }
+}
+
+// The largest over the lanes that hold a block of 32 columns, W each: aligned, and all of
+// them active (as xor_add).
+template <int W>
+__device__ __forceinline__ uint32_t max_of_block(uint32_t v) {
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));
+    if constexpr (W == 4)
+        v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));
     return v;
 }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
-// Stores chunk c of a row in 8 bits and, from the first of eight chunks, its scale.
-// Eight lanes with adjacent chunks call together; f is 0 past the row's end.
-template <bool WHOLE>
+// Stores cells c of a row in 8 bits and, from the first of a block, its scale.  The
+// lanes of a block call together; r is 0 past the row's end.
+template <int W, bool WHOLE>
 __device__ __forceinline__ void store_bytes(uint8_t* codes, uint8_t* scales, int c, int D,
-                                            const Few& f) {
+                                            const Cells<W>& r) {
     uint32_t big = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) big = max(big, abs_bits(f.v[e]));
-    const int x = scale_exponent(max_of_eight(big));
-    if (4 * c >= D) return;
+    for (int e = 0; e < W; ++e) big = max(big, abs_bits(r.v[e]));
+    const int x = scale_exponent(max_of_block<W>(big));
+    if (W * c >= D) return;
     const float mul = __uint_as_float((uint32_t)(127 - (x == kNone ? 0 : x)) << 23);
-    uint32_t q = 0x7F7F7F7Fu;  // NaN
-    if (x != kNone) {
-        q = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f.v[0] * mul, f.v[1] * mul, 0, false);
-        q = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f.v[2] * mul, f.v[3] * mul, (int)q, true);
+    uint32_t q[W / 4];
+#pragma unroll
+    for (int k = 0; k < W / 4; ++k) {
+        q[k] = 0x7F7F7F7Fu;  // NaN
+        if (x != kNone) {
+            const float* v = r.v + 4 * k;
+            q[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] * mul, v[1] * mul, 0, false);
+            q[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * mul, v[3] * mul, (int)q[k], true);
+        }
     }
-    if constexpr (WHOLE) {
-        *reinterpret_cast<uint32_t*>(codes + 4 * c) = q;
+    if constexpr (W == 8) {
+        *reinterpret_cast<u32x2*>(codes + 8 * c) = u32x2{q[0], q[1]};
+    } else if constexpr (WHOLE) {
+        *reinterpret_cast<uint32_t*>(codes + 4 * c) = q[0];
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (4 * c + e < D) codes[4 * c + e] = (uint8_t)(q >> (8 * e));
+            if (4 * c + e < D) codes[4 * c + e] = (uint8_t)(q[0] >> (8 * e));
     }
-    if (c % 8 == 0) scales[c / 8] = (uint8_t)(x + 127);
+    constexpr int kCells = kByteBlock / W;
+    if (c % kCells == 0) scales[c / kCells] = (uint8_t)(x + 127);
 }
 
 template <typename E>
@@ -69,24 +121,24 @@ __device__ __forceinline__ float rounded(float v) {
     else return __uint_as_float(float_to_bf16_bits(v) << 16);
 }
 
-template <typename E, int TPR, int NV, bool WHOLE, bool BYTES>
+template <typename E, int W, int TPR, int NV, bool WHOLE, bool BYTES>
 __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
     __shared__ float s_sum[8];
     int turn = 0;
     constexpr int kRows = kBlock / TPR;
-    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + 3) / 4;
+    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + W - 1) / W;
     const E* x = static_cast<const E*>(a.x);
     const E* res = static_cast<const E*>(a.res);
     E* total = static_cast<E*>(a.total);
     const float inv = 1.0f / (float)D;
     for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
          r += (int64_t)gridDim.x * kRows) {
-        Few f[NV], o[NV];
+        Cells<W> f[NV], o[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
-            f[i] = c < chunks ? load_few<WHOLE>(x + r * a.ld_x, c, D) : Few{};
-            if (res != nullptr) o[i] = c < chunks ? load_few<WHOLE>(res + r * a.ld_res, c, D) : Few{};
+            f[i] = c < chunks ? load_cells<W, WHOLE>(x + r * a.ld_x, c, D) : Cells<W>{};
+            if (res != nullptr) o[i] = c < chunks ? load_cells<W, WHOLE>(res + r * a.ld_res, c, D) : Cells<W>{};
         }
         float sq = 0.f;
 #pragma unroll
@@ -94,64 +146,64 @@ __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
             const int c = t + TPR * i;
             if (res != nullptr) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[i].v[e] = rounded<E>(f[i].v[e] + o[i].v[e]);
-                if (c < chunks) store_few<WHOLE>(total + r * a.ld_total, c, D, f[i]);
+                for (int e = 0; e < W; ++e) f[i].v[e] = rounded<E>(f[i].v[e] + o[i].v[e]);
+                if (c < chunks) store_cells<W, WHOLE>(total + r * a.ld_total, c, D, f[i]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sq = fmaf(f[i].v[e], f[i].v[e], sq);
+            for (int e = 0; e < W; ++e) sq = fmaf(f[i].v[e], f[i].v[e], sq);
         }
         const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s_sum, turn) * inv + a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
-            const Few g = c < chunks ? load_few<WHOLE>(a.gamma, c, D) : Few{};
+            const Cells<W> g = c < chunks ? load_cells<W, WHOLE>(a.gamma, c, D) : Cells<W>{};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f[i].v[e] = f[i].v[e] * rstd * g.v[e];
+            for (int e = 0; e < W; ++e) f[i].v[e] = f[i].v[e] * rstd * g.v[e];
             if constexpr (BYTES)
-                store_bytes<WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f[i]);
+                store_bytes<W, WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f[i]);
             else if (c < chunks)
-                store_few<WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f[i]);
+                store_cells<W, WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f[i]);
         }
         if (t == 0 && a.rstd != nullptr) a.rstd[r] = rstd;
     }
 }
 
-template <typename E, int TPR, int NV, bool WHOLE>
+template <typename E, int W, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_rms_backward(RmsArgs a) {
     __shared__ float s_sum[8];
     int turn = 0;
     constexpr int kRows = kBlock / TPR;
     constexpr int kHeld = TPR < 64 ? TPR : 64;  // lanes of a wave that hold different columns
-    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + 3) / 4;
+    const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + W - 1) / W;
     const E* x = static_cast<const E*>(a.x);
     const E* dy = static_cast<const E*>(a.dy);
     const E* res = static_cast<const E*>(a.res);
     E* dx = static_cast<E*>(a.y);
     const float inv = 1.0f / (float)D;
-    Few g[NV], dg[NV];
+    Cells<W> g[NV], dg[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = t + TPR * i;
-        g[i] = c < chunks ? load_few<WHOLE>(a.gamma, c, D) : Few{};
-        dg[i] = Few{};
+        g[i] = c < chunks ? load_cells<W, WHOLE>(a.gamma, c, D) : Cells<W>{};
+        dg[i] = Cells<W>{};
     }
     for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
          r += (int64_t)gridDim.x * kRows) {
         const float rstd = a.rstd[r];
-        Few z[NV], d[NV], o[NV];
+        Cells<W> z[NV], d[NV], o[NV];
         float along = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
             const bool in = c < chunks;
-            z[i] = in ? load_few<WHOLE>(x + r * a.ld_x, c, D) : Few{};
-            d[i] = in ? load_few<WHOLE>(dy + r * a.ld_dy, c, D) : Few{};
-            o[i] = in && res != nullptr ? load_few<WHOLE>(res + r * a.ld_res, c, D) : Few{};
+            z[i] = in ? load_cells<W, WHOLE>(x + r * a.ld_x, c, D) : Cells<W>{};
+            d[i] = in ? load_cells<W, WHOLE>(dy + r * a.ld_dy, c, D) : Cells<W>{};
+            o[i] = in && res != nullptr ? load_cells<W, WHOLE>(res + r * a.ld_res, c, D) : Cells<W>{};
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < W; ++e) {
                 z[i].v[e] *= rstd;
                 dg[i].v[e] = fmaf(d[i].v[e], z[i].v[e], dg[i].v[e]);
                 d[i].v[e] *= g[i].v[e];
@@ -165,30 +217,30 @@ __global__ __launch_bounds__(kBlock) void k_rms_backward(RmsArgs a) {
             const int c = t + TPR * i;
             if (c >= chunks) continue;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < W; ++e)
                 d[i].v[e] = fmaf(rstd, d[i].v[e] - z[i].v[e] * along, o[i].v[e]);
-            store_few<WHOLE>(dx + r * a.ld_y, c, D, d[i]);
+            store_cells<W, WHOLE>(dx + r * a.ld_y, c, D, d[i]);
         }
     }
     if (a.partial == nullptr) return;
     // the groups of a wave, then the waves
-    __shared__ float s_part[TPR <= 64 ? 4 * kHeld * NV * 4 : 1];
+    __shared__ float s_part[TPR <= 64 ? 4 * kHeld * NV * W : 1];
     float* out = a.partial + (int64_t)blockIdx.x * D;
     if constexpr (TPR <= 64) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < W; ++e) {
                 float v = dg[i].v[e];
 #pragma unroll
                 for (int off = TPR; off < 64; off <<= 1) v += __shfl_xor(v, off);
-                if (lane < kHeld) s_part[((wave * NV + i) * 4 + e) * kHeld + lane] = v;
+                if (lane < kHeld) s_part[((wave * NV + i) * W + e) * kHeld + lane] = v;
             }
         __syncthreads();
         for (int j = threadIdx.x; j < D; j += kBlock) {
-            const int c = j / 4, at = ((c / TPR) * 4 + j % 4) * kHeld + c % TPR;
-            constexpr int kWave = NV * 4 * kHeld;
+            const int c = j / W, at = ((c / TPR) * W + j % W) * kHeld + c % TPR;
+            constexpr int kWave = NV * W * kHeld;
             out[j] = (s_part[at] + s_part[kWave + at]) +
                      (s_part[2 * kWave + at] + s_part[3 * kWave + at]);
         }
@@ -198,8 +250,8 @@ __global__ __launch_bounds__(kBlock) void k_rms_backward(RmsArgs a) {
             const int c = t + TPR * i;
             if (c >= chunks) continue;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (inside<WHOLE>(c, e, D)) out[c * 4 + e] = dg[i].v[e];
+            for (int e = 0; e < W; ++e)
+                if (W * c + e < D) out[c * W + e] = dg[i].v[e];
         }
     }
 }
@@ -225,68 +277,76 @@ __global__ __launch_bounds__(kBlock) void k_rms_reduce(const float* __restrict__
     }
 }
 
-// Rows into 8 bits: eight threads a block of 32 columns, blocks in the order of rows.
-template <typename E, bool WHOLE>
+// Rows into 8 bits: a thread takes W columns, in the order of rows' blocks of 32.
+template <typename E, int W, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_to_bytes(RmsArgs a) {
+    constexpr int kCells = kByteBlock / W;
     const int D = a.dim, blocks = (D + kByteBlock - 1) / kByteBlock;
     const int64_t all = a.n * blocks;
-    for (int64_t b = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / 8; b < all;
-         b += (int64_t)gridDim.x * kBlock / 8) {
+    for (int64_t b = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kCells; b < all;
+         b += (int64_t)gridDim.x * kBlock / kCells) {
         const int64_t r = b / blocks;
-        const int c = (int)(b % blocks) * 8 + (threadIdx.x & 7);
-        const Few f = 4 * c < D
-                          ? load_few<WHOLE>(static_cast<const E*>(a.x) + r * a.ld_x, c, D) : Few{};
-        store_bytes<WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f);
+        const int c = (int)(b % blocks) * kCells + threadIdx.x % kCells;
+        const Cells<W> f =
+            W * c < D ? load_cells<W, WHOLE>(static_cast<const E*>(a.x) + r * a.ld_x, c, D) : Cells<W>{};
+        store_bytes<W, WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f);
     }
 }
 
-// ... and back: a thread takes four columns.
-template <typename E, bool WHOLE>
+// ... and back: a thread takes W columns.
+template <typename E, int W, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_from_bytes(RmsArgs a) {
-    const int D = a.dim, chunks = (D + 3) / 4;
+    constexpr int kCells = kByteBlock / W;
+    const int D = a.dim, chunks = (D + W - 1) / W;
     const int64_t all = a.n * chunks;
     for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < all;
          i += (int64_t)gridDim.x * kBlock) {
         const int64_t r = i / chunks;
         const int c = (int)(i % chunks);
         const uint8_t* row = a.codes + r * a.ld_codes;
-        uint32_t q = 0;
-        if constexpr (WHOLE) {
-            q = reinterpret_cast<const uint32_t*>(row)[c];
+        uint32_t q[W / 4] = {};
+        if constexpr (W == 8) {
+            const u32x2 v = reinterpret_cast<const u32x2*>(row)[c];
+            q[0] = v.x, q[1] = v.y;
+        } else if constexpr (WHOLE) {
+            q[0] = reinterpret_cast<const uint32_t*>(row)[c];
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (4 * c + e < D) q |= (uint32_t)row[4 * c + e] << (8 * e);
+                if (4 * c + e < D) q[0] |= (uint32_t)row[4 * c + e] << (8 * e);
         }
-        const float mul = byte_scale(a.scales[r * a.ld_scales + c / 8]);
-        const Few f = {{__builtin_amdgcn_cvt_f32_fp8((int)q, 0) * mul,
-                        __builtin_amdgcn_cvt_f32_fp8((int)q, 1) * mul,
-                        __builtin_amdgcn_cvt_f32_fp8((int)q, 2) * mul,
-                        __builtin_amdgcn_cvt_f32_fp8((int)q, 3) * mul}};
-        store_few<WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f);
+        const float mul = byte_scale(a.scales[r * a.ld_scales + c / kCells]);
+        Cells<W> f;
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k) {
+            f.v[4 * k] = __builtin_amdgcn_cvt_f32_fp8((int)q[k], 0) * mul;
+            f.v[4 * k + 1] = __builtin_amdgcn_cvt_f32_fp8((int)q[k], 1) * mul;
+            f.v[4 * k + 2] = __builtin_amdgcn_cvt_f32_fp8((int)q[k], 2) * mul;
+            f.v[4 * k + 3] = __builtin_amdgcn_cvt_f32_fp8((int)q[k], 3) * mul;
+        }
+        store_cells<W, WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f);
     }
 }
 
-template <typename E, int TPR, int NV, bool WHOLE>
+template <typename E, int W, int TPR, int NV, bool WHOLE>
 void rms_one(const RmsArgs& a, bool backward, hipStream_t s) {
     const int64_t rows = kBlock / TPR, need = (a.n + rows - 1) / rows;
     const dim3 grid((uint32_t)(need < 65536 ? need : 65536));
     if (backward)
-        k_rms_backward<E, TPR, NV, WHOLE>
+        k_rms_backward<E, W, TPR, NV, WHOLE>
             <<<dim3((uint32_t)norm_blocks(a.n, a.dim)), kBlock, 0, s>>>(a);
     else if (a.codes != nullptr)
-        k_rms<E, TPR, NV, WHOLE, true><<<grid, kBlock, 0, s>>>(a);
+        k_rms<E, W, TPR, NV, WHOLE, true><<<grid, kBlock, 0, s>>>(a);
     else
-        k_rms<E, TPR, NV, WHOLE, false><<<grid, kBlock, 0, s>>>(a);
+        k_rms<E, W, TPR, NV, WHOLE, false><<<grid, kBlock, 0, s>>>(a);
 }
 
-template <typename E>
-hipError_t rms_dispatch(const RmsArgs& a, bool backward, hipStream_t s) {
-    const NormShape p = norm_shape((a.dim + 3) / 4);
+template <typename E, int W, bool WHOLE>
+hipError_t rms_shape(const RmsArgs& a, bool backward, hipStream_t s) {
+    const NormShape p = norm_shape((a.dim + W - 1) / W);
 #define HUGE_RMS_CASE(T, N)                           \
     case (T) * 64 + (N):                              \
-        if (a.vec) rms_one<E, T, N, true>(a, backward, s); \
-        else rms_one<E, T, N, false>(a, backward, s); \
+        rms_one<E, W, T, N, WHOLE>(a, backward, s);   \
         return hipGetLastError();
     switch (p.tpr * 64 + p.nv) {
         HUGE_RMS_CASE(8, 1)
@@ -297,24 +357,36 @@ hipError_t rms_dispatch(const RmsArgs& a, bool backward, hipStream_t s) {
         HUGE_RMS_CASE(64, 4)
         HUGE_RMS_CASE(256, 2)
         HUGE_RMS_CASE(256, 4)
-        HUGE_RMS_CASE(256, 8)
+    }
+    if constexpr (W == 4) {
+        switch (p.tpr * 64 + p.nv) { HUGE_RMS_CASE(256, 8) }
     }
 #undef HUGE_RMS_CASE
     return hipErrorInvalidValue;
 }
 
 template <typename E>
+hipError_t rms_dispatch(const RmsArgs& a, bool backward, hipStream_t s) {
+    if constexpr (sizeof(E) == 2)
+        if (a.eights) return rms_shape<E, 8, true>(a, backward, s);
+    return a.vec ? rms_shape<E, 4, true>(a, backward, s) : rms_shape<E, 4, false>(a, backward, s);
+}
+
+template <typename E>
 hipError_t bytes_dispatch(const RmsArgs& a, bool back, hipStream_t s) {
-    const int64_t work = back ? a.n * ((a.dim + 3) / 4)
-                              : a.n * ((a.dim + kByteBlock - 1) / kByteBlock) * 8;
+    const int w = a.eights ? 8 : 4;
+    const int64_t work = back ? a.n * ((a.dim + w - 1) / w)
+                              : a.n * ((a.dim + kByteBlock - 1) / kByteBlock) * (kByteBlock / w);
     const int64_t need = (work + kBlock - 1) / kBlock;
     const dim3 grid((uint32_t)(need < 65536 ? need : 65536));
     if (back) {
-        if (a.vec) k_from_bytes<E, true><<<grid, kBlock, 0, s>>>(a);
-        else k_from_bytes<E, false><<<grid, kBlock, 0, s>>>(a);
+        if (a.eights) k_from_bytes<E, 8, true><<<grid, kBlock, 0, s>>>(a);
+        else if (a.vec) k_from_bytes<E, 4, true><<<grid, kBlock, 0, s>>>(a);
+        else k_from_bytes<E, 4, false><<<grid, kBlock, 0, s>>>(a);
     } else {
-        if (a.vec) k_to_bytes<E, true><<<grid, kBlock, 0, s>>>(a);
-        else k_to_bytes<E, false><<<grid, kBlock, 0, s>>>(a);
+        if (a.eights) k_to_bytes<E, 8, true><<<grid, kBlock, 0, s>>>(a);
+        else if (a.vec) k_to_bytes<E, 4, true><<<grid, kBlock, 0, s>>>(a);
+        else k_to_bytes<E, 4, false><<<grid, kBlock, 0, s>>>(a);
     }
     return hipGetLastError();
 }

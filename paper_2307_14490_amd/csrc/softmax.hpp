@@ -421,6 +421,8 @@ struct PassArgs {
     int32_t stage;         // Y tiles of an LDS buffer
     int32_t nfrag, kd;
     int32_t forms;
+    const bf16_t* x_direct;  // answers: the rows unpacked, instead of x
+    int64_t x_ld, x_count;
     const bf16_t* y_rows;  // loss: the classes unpacked, instead of y
     int64_t ld, classes;
     bool first;            // the first piece of the classes: partial results are written
@@ -685,18 +687,36 @@ void k_sm_lse(PassArgs a) {
     const int rec_bytes = record_bytes(nfrag, Kind<E>::kParts, a.forms);
     const XTiles<XB> xt = x_tiles_of<XB>(a, at.x_block, xg, rec_bytes);
     Operand<E> x[XB][2 * ND];
-    float xmul[XB], top[XB], sum[XB], first[XB], most[XB];
+    // the first moment in a few running sums, so that each takes one addition in so many
+    constexpr int kSums = Kind<E>::kScaled ? 2 : 4;
+    float xmul[XB], top[XB], sum[XB], first[XB][kSums], most[XB];
 #pragma unroll
     for (int b = 0; b < XB; ++b) {
         if constexpr (STAGED) {
+            bool packed = true;
+            if constexpr (ANSWER && !Kind<E>::kScaled) {
+                packed = a.x_direct == nullptr;
+                if (!packed) {
+                    // whole operands: 16 bytes of the lane's row each
+                    const int64_t row = xt.t[b] * 32 + (lane & 31);
+                    const bf16_t* from = a.x_direct + (row < a.x_count ? row : a.x_count - 1) * a.x_ld;
 #pragma unroll
-            for (int k = 0; k < 2 * ND; ++k)
-                x[b][k] = load_operand<E>(xt.rec[b] + kHeader, k, 2 * ND, lane);
+                    for (int k = 0; k < 2 * ND; ++k)
+                        x[b][k].p[0] = *reinterpret_cast<const typename Kind<E>::Vec*>(
+                            from + 16 * k + 8 * half);
+                }
+            }
+            if (packed) {
+#pragma unroll
+                for (int k = 0; k < 2 * ND; ++k)
+                    x[b][k] = load_operand<E>(xt.rec[b] + kHeader, k, 2 * ND, lane);
+            }
         }
         xmul[b] = Kind<E>::kScaled ? field(xt.rec[b], kMul)[lane & 31] : 1.f;
         top[b] = ANSWER ? kLeast : -INFINITY;
         sum[b] = 0.f;
-        first[b] = 0.f;
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) first[b][k] = 0.f;
         most[b] = kFloor;
     }
     // DIRECT: no headers; there is no bias then, only the end of the classes
@@ -749,23 +769,29 @@ void k_sm_lse(PassArgs a) {
                     }
                     most[b] = fmaxf(most[b], m);
                     if (__ballot(m > top[b] + kRiseAnswer) != 0) {
-                        const Stats s = raise({top[b], sum[b], first[b]}, fmaxf(m, top[b]));
-                        top[b] = s.top, sum[b] = s.sum, first[b] = s.first;
+                        const float up = fmaxf(m, top[b]), d = (top[b] - up) * kLog2e;
+                        const float f = exp2f(d);
+                        first[b][0] = fmaf(d, sum[b], first[b][0]);
+#pragma unroll
+                        for (int k = 0; k < kSums; ++k) first[b][k] *= f;
+                        sum[b] *= f;
+                        top[b] = up;
                     }
                     const float sub = -top[b] * kLog2e;
                     // in two halves, so that few of the logarithms are held at a time
 #pragma unroll
                     for (int j = 0; j < 16; j += 8) {
-                        float s[4], f[4];
+                        float s[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float u = fmaf(c[b][j + i], kLog2e, sub);
                             const float v = fmaf(c[b][j + 4 + i], kLog2e, sub);
                             const float e = __builtin_amdgcn_exp2f(u), g = __builtin_amdgcn_exp2f(v);
-                            s[i] = e + g, f[i] = fmaf(u, e, v * g);
+                            s[i] = e + g;
+                            float& of_sum = first[b][i % kSums];
+                            of_sum = fmaf(v, g, fmaf(u, e, of_sum));
                         }
                         sum[b] += (s[0] + s[1]) + (s[2] + s[3]);
-                        first[b] += (f[0] + f[1]) + (f[2] + f[3]);
                     }
                 } else {
                     if (__ballot(m > top[b] + kRise) != 0) {
@@ -785,8 +811,10 @@ void k_sm_lse(PassArgs a) {
 #pragma unroll
         for (int b = 0; b < XB; ++b) {
             // the halves hold different classes of the same row
-            Stats s = join({top[b], sum[b], first[b]},
-                           {__shfl_xor(top[b], 32), __shfl_xor(sum[b], 32), __shfl_xor(first[b], 32)});
+            float of_lane = first[b][0] + first[b][1];
+            if constexpr (kSums == 4) of_lane += first[b][2] + first[b][3];
+            Stats s = join({top[b], sum[b], of_lane},
+                           {__shfl_xor(top[b], 32), __shfl_xor(sum[b], 32), __shfl_xor(of_lane, 32)});
             float largest = fmaxf(most[b], __shfl_xor(most[b], 32));
             if (half == 0 && xt.in[b]) {
                 float4* out = a.stat_part + ((int64_t)at.split * yw + yg) * a.part_rows +
@@ -975,7 +1003,8 @@ struct FewTable<bf16_t, BYTES, true> {
 template <typename E, int NB, int BYTES, bool ANSWER, bool CODES>
 __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
                                                                void* __restrict__ parts,
-                                                               int64_t pad,
+                                                               int64_t pad, int64_t slots,
+                                                               int64_t slot0,
                                                                float* __restrict__ best) {
     constexpr int kWaves = few_waves(NB);
     using F = Few<E>;
@@ -1120,7 +1149,8 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
                 r.x = m;
             }
         }
-        part[blockIdx.x * pad + threadIdx.x] = r;
+            // of answers a row's entries are adjacent, which few threads then join
+        part[ANSWER ? threadIdx.x * slots + slot0 + blockIdx.x : blockIdx.x * pad + threadIdx.x] = r;
     }
 }
 
@@ -1690,12 +1720,13 @@ bool fours(const void* m, int64_t ld, size_t elem) {
 // Packs a piece of the classes, and before the first the rows.
 template <typename E, bool ANSWER = false, bool CODES = false>
 hipError_t pack(const SoftmaxPlan& p, const SoftmaxArgs& a, int64_t c0, int64_t count, int forms,
-                hipStream_t s) {
+                hipStream_t s, bool rows = true) {
     PackArgs w{}, h{};
     w.m = a.w, w.ld = a.ld_w, w.first = c0, w.count = count, w.tiles = div_up(count, kSmTile);
     w.out = a.ws + p.w, w.classes = true, w.vec = fours(a.w, a.ld_w, CODES ? 1 : sizeof(E));
     w.scales = a.w_scales, w.ld_scales = a.ld_scales;
-    h.m = a.h, h.ld = a.ld_h, h.count = a.n, h.tiles = c0 == 0 ? p.rows_pad / kSmTile : 0;
+    h.m = a.h, h.ld = a.ld_h, h.count = a.n;
+    h.tiles = c0 == 0 && rows ? p.rows_pad / kSmTile : 0;
     h.out = a.ws + p.h, h.vec = fours(a.h, a.ld_h, sizeof(E));
     return in_launches(w.tiles + h.tiles, [&](dim3 grid, int64_t first) {
         k_sm_pack<E, ANSWER, CODES><<<grid, kBlock, 0, s>>>(a, w, h, p.dp / 16, forms, first);
@@ -1711,17 +1742,24 @@ int few_blocks(int64_t n, int32_t dim) {
     return 0;
 }
 
+// Workgroups of it: each leaves an entry per row.
+template <int NB>
+int64_t few_grid(int64_t classes) {
+    const int64_t need = div_up(div_up(classes, 16), few_waves(NB));
+    return need < 2048 ? need : 2048;
+}
+
+// of answers: the entries of a row are all_slots, these from slot0 on.
 template <typename E, int NB, bool ANSWER = false, bool CODES = false>
 hipError_t few_pass(const SoftmaxArgs& a, void* part, int64_t* slots, hipStream_t s,
-                    float* best = nullptr) {
+                    float* best = nullptr, int64_t all_slots = 0, int64_t slot0 = 0) {
     constexpr int kWaves = few_waves(NB);
-    const int64_t tiles = div_up(a.classes, 16), need = div_up(tiles, kWaves);
-    const int64_t blocks = need < 2048 ? need : 2048;
+    const int64_t tiles = div_up(a.classes, 16), blocks = few_grid<NB>(a.classes);
     const int lds = few_operands<E, CODES>(a.dim) * NB * 1024;
     auto go = [&](auto bytes) {
         constexpr auto* kKernel = &k_sm_few<E, NB, decltype(bytes)::value, ANSWER, CODES>;
         if (lds > 60 * 1024) SM_TRY(allow_lds<kKernel>(kFewLds<E>));
-        kKernel<<<dim3((uint32_t)blocks), kWaves * 64, lds, s>>>(a, tiles, part, 16 * NB, best);
+        kKernel<<<dim3((uint32_t)blocks), kWaves * 64, lds, s>>>(a, tiles, part, 16 * NB, all_slots, slot0, best);
         return hipGetLastError();
     };
     *slots = blocks;

@@ -333,7 +333,10 @@ class AdamW(_Status):
             self._state_at.append(at)
             at += -(-L.huge_adamw_state_bytes(p.numel(), self.kind) // 256) * 256
         self.states = torch.zeros(at + 256, dtype=torch.uint8, device=self.device)
-        self._own += [self.states, *self.params]
+        # of clipped steps
+        self._norm_ws = torch.empty(L.huge_grad_norm_workspace_bytes(count), dtype=torch.uint8,
+                                    device=self.device)
+        self._own += [self.states, self._norm_ws, *self.params]
         self._skip = (-self.states.data_ptr()) % 256
         for k, p in enumerate(self.params):
             t = self._tensors[k]
@@ -404,11 +407,10 @@ class AdamW(_Status):
         import torch
         L, count = load(), len(self.params)
         norm = torch.empty(1, dtype=torch.float32, device=self.device)
-        bytes_ = L.huge_grad_norm_workspace_bytes(count)
-        ws = torch.empty(bytes_, dtype=torch.uint8, device=self.device)
+        ws = self._norm_ws
         _ok(L.huge_adamw_step_clipped(ctypes.byref(self.cfg), self._tensors, count, max_norm,
-                                      norm.data_ptr(), self._status_ptr, ws.data_ptr(), bytes_,
-                                      st), "huge_adamw_step_clipped")
+                                      norm.data_ptr(), self._status_ptr, ws.data_ptr(),
+                                      ws.numel(), st), "huge_adamw_step_clipped")
         return norm
 
     def _pointers(self, ts):
