@@ -273,25 +273,30 @@ _TABLE = [("d_grad", "u8"), ("n", "i8"), ("dtype", "i4"), ("fill", "i4")]  # Hug
 
 
 def _grads(grads, what):
-    """The list, its device and its table for the C calls."""
+    """The list, its device, its table for the C calls and what holds that.  A property of
+    all tensors at a time: lists may be hundreds long, and each look costs host time."""
     import torch
-    types = {torch.float32: _DTYPES["f32"], torch.bfloat16: _DTYPES["bf16"]}
     grads = list(grads)
     if not grads:
         raise ValueError(f"{what}: no gradients")
-    for k, g in enumerate(grads):
-        if not (isinstance(g, torch.Tensor) and g.is_cuda and g.is_contiguous()
-                and g.dtype in types):
-            _arg(g, ("float32", "bfloat16"), f"{what}[{k}]")
-    device = grads[0].device
-    if len({g.get_device() for g in grads}) > 1:
-        k = next(k for k, g in enumerate(grads) if g.device != device)
-        raise ValueError(f"{what}[{k}]: on {grads[k].device}, expected {device}")
-    table = np.empty(len(grads), _TABLE)
-    table["d_grad"] = [g.data_ptr() for g in grads]
-    table["n"] = [g.numel() for g in grads]
-    table["dtype"] = [types[g.dtype] for g in grads]
-    return grads, device, table.ctypes.data_as(ctypes.POINTER(HugeGradTensor)), table
+    codes = {torch.float32: _DTYPES["f32"], torch.bfloat16: _DTYPES["bf16"]}
+    if all(issubclass(c, torch.Tensor) for c in {type(g) for g in grads}):
+        types = [g.dtype for g in grads]
+        devices = {g.get_device() for g in grads}
+        if codes.keys() >= set(types) and min(devices) >= 0 and \
+                all([g.is_contiguous() for g in grads]):
+            device = grads[0].device
+            if len(devices) > 1:
+                k = next(k for k, g in enumerate(grads) if g.device != device)
+                raise ValueError(f"{what}[{k}]: on {grads[k].device}, expected {device}")
+            table = np.empty(len(grads), _TABLE)
+            table["d_grad"] = [g.data_ptr() for g in grads]
+            table["n"] = [g.numel() for g in grads]
+            table["dtype"] = [codes[t] for t in types]
+            return grads, device, table.ctypes.data_as(ctypes.POINTER(HugeGradTensor)), table
+    for k, g in enumerate(grads):  # one of them is refused
+        _arg(g, ("float32", "bfloat16"), f"{what}[{k}]")
+    raise TypeError(f"{what}: expected GPU tensors")
 
 
 def grad_norm(grads, stream=None):

@@ -254,12 +254,13 @@ huge_status huge_dequantise_rows(const uint8_t* d_codes, int64_t ld_codes, const
 size_t huge_log_probs_workspace_bytes(const huge_log_probs_config* cfg) {
     if (!answer_ok(cfg)) return 0;
     const bool codes = cfg->table_dtype == HUGE_DTYPE_Q8;
-    const int64_t few = cfg->max_rows < 64 ? cfg->max_rows : 64;
     size_t most = 0;
     auto at_least = [&](size_t bytes) { most = bytes > most ? bytes : most; };
     // few rows are laid out otherwise
-    for (int64_t n : {few < 16 ? few : (int64_t)16, few < 32 ? few : (int64_t)32, few, cfg->max_rows})
+    for (int64_t few : {16, 32, 48, 64, 0}) {
+        const int64_t n = few == 0 || few > cfg->max_rows ? cfg->max_rows : few;
         at_least(answer_plan(cfg->num_classes, n, cfg->dim, cfg->dtype, codes, cfg->top).total);
+    }
     if (cfg->grad)
         at_least(softmax_plan(cfg->num_classes, cfg->max_rows, cfg->dim, cfg->dtype, true).total);
     return most;

@@ -189,6 +189,7 @@ constexpr int kMostTop = 64;
 struct AnswerPlan {
     SoftmaxPlan sm;
     int32_t few;                             // blocks of 16 rows, or 0: more than few
+    bool thirds;                             // few fp32 rows in three bf16 parts
     int32_t group;                           // classes of a tile
     int32_t keep;                            // tiles that are looked at
     int64_t piece, rows;

@@ -20,6 +20,7 @@ typedef unsigned long long u64;
 constexpr int kSlack = 4;
 constexpr int kTopThreads = 256;
 constexpr int64_t kBestFloats = (int64_t)1 << 28;  // tile maxima at a time: 1 GiB
+constexpr int kThirdsFrom = 3;                     // blocks of 16 fp32 rows that go in thirds
 constexpr int64_t kBestRows = 8192;                // rows that have room for any piece
 constexpr int64_t kListRows = 32768;               // rows times splits of k_lp_select
 constexpr int kMostSplits = 64;
@@ -572,8 +573,8 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
         for (int64_t t0 = 0; t0 < all; t0 += piece) {
             const int64_t c0 = t0 * 16, left = a.classes - c0;
             const int64_t count = left < piece * 16 ? left : piece * 16;
-            all_slots += p.few == 1 ? few_grid<1>(count) : p.few == 2 ? few_grid<2>(count)
-                                                                      : few_grid<4>(count);
+            // above 16 rows all workgroups are alike
+            all_slots += p.few == 1 ? few_grid<1>(count) : few_grid<4>(count);
         }
         int splits = 1;
         for (int64_t t0 = 0; t0 < all; t0 += piece) {
@@ -582,11 +583,16 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             const SoftmaxArgs q = classes_from<E, CODES>(f, c0, count);
             int64_t more = 0;
             auto pass = [&](auto nb) {
-                return few_pass<E, decltype(nb)::value, true, CODES>(q, part, &more, s, best,
-                                                                     all_slots, slots);
+                constexpr int NB = decltype(nb)::value;
+                if constexpr (sizeof(E) == 4 && NB >= kThirdsFrom)
+                    if (p.thirds)
+                        return few_pass<E, NB, true, false, true>(q, part, &more, s, best,
+                                                                  all_slots, slots);
+                return few_pass<E, NB, true, CODES>(q, part, &more, s, best, all_slots, slots);
             };
             SM_TRY(p.few == 1   ? pass(std::integral_constant<int, 1>{})
                    : p.few == 2 ? pass(std::integral_constant<int, 2>{})
+                   : p.few == 3 ? pass(std::integral_constant<int, 3>{})
                                 : pass(std::integral_constant<int, 4>{}));
             slots += more;
             if (a.top == 0) continue;
@@ -658,8 +664,14 @@ AnswerPlan answer_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype, b
     AnswerPlan p{};
     const bool bf16 = dtype == kDtypeBf16;
     p.sm = softmax_plan(classes, n, dim, dtype, false);
-    p.few = codes ? few_blocks<bf16_t, true>(n, dim)
-                  : bf16 ? few_blocks<bf16_t>(n, dim) : few_blocks<float>(n, dim);
+    const int64_t blocks = div_up(n, 16);
+    if (blocks <= 4) {
+        p.thirds = !bf16 && blocks >= kThirdsFrom &&
+                   few_kb<float, false, true>(dim) * blocks * 1024 <= kFewLds<float>;
+        const int64_t kb = p.thirds ? 0 : codes ? few_kb<bf16_t, true>(dim)
+                           : bf16 ? few_kb<bf16_t, false>(dim) : few_kb<float, false>(dim);
+        if (kb * blocks * 1024 <= (bf16 ? kFewLds<bf16_t> : kFewLds<float>)) p.few = (int32_t)blocks;
+    }
     p.group = p.few != 0 ? 16 : kSmTile;
     const int64_t all = div_up(classes, p.group);
     const int64_t pad = p.few != 0 ? 16 * p.few : p.sm.rows_pad;

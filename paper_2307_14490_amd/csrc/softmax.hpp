@@ -895,10 +895,16 @@ struct Few<float> {
     }
 };
 
-// Operands of a row; of codes whole pairs.
-template <typename E, bool CODES>
+// Operands of a row; of codes and of thirds whole pairs.
+template <typename E, bool CODES, bool THIRDS = false>
 __host__ __device__ constexpr int few_operands(int dim) {
-    return CODES ? 2 * ((dim + 63) / 64) : (dim + Few<E>::kCols - 1) / Few<E>::kCols;
+    return CODES ? 2 * ((dim + 63) / 64)
+                 : THIRDS ? 2 * ((dim + 31) / 32) : (dim + Few<E>::kCols - 1) / Few<E>::kCols;
+}
+// KB of LDS for a block of 16 rows.
+template <typename E, bool CODES, bool THIRDS = false>
+__host__ __device__ constexpr int few_kb(int dim) {
+    return THIRDS ? 3 * ((dim + 31) / 32) : few_operands<E, CODES>(dim);
 }
 
 // 16 bytes of a row at a column, 0 past its end, read BYTES at a time.
@@ -999,8 +1005,27 @@ struct FewTable<bf16_t, BYTES, true> {
     }
 };
 
-// NB blocks of 16 rows.  Of a table in 8 bits the operands come in pairs.
-template <typename E, int NB, int BYTES, bool ANSWER, bool CODES>
+// An fp32 number as the sum of three bf16 ones, each the nearest to what the ones before
+// leave: within 2^-27 of it.  Of the nine products of two such sums the six above 2^-27 are
+// formed, the smallest first, which is an fp32 product but for its rounding, at six bf16
+// products in place of eight fp32 ones of twice the time each.
+struct Thirds {
+    bf16x8 p[3];
+};
+__device__ __forceinline__ Thirds thirds(f32x4 a, f32x4 b) {
+    f32x8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    Thirds r;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        r.p[k] = __builtin_convertvector(v, bf16x8);
+        v -= __builtin_convertvector(r.p[k], f32x8);
+    }
+    return r;
+}
+
+// NB blocks of 16 rows.  Of a table in 8 bits the operands come in pairs.  THIRDS: so do
+// those of fp32 rows, each pair of 16 columns as one of 32 in three parts.
+template <typename E, int NB, int BYTES, bool ANSWER, bool CODES, bool THIRDS>
 __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
                                                                void* __restrict__ parts,
                                                                int64_t pad, int64_t slots,
@@ -1016,12 +1041,26 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
     __shared__ Part s_part[kWaves][NB * 16];
     Vec* sh = reinterpret_cast<Vec*>(lds);  // [operand][block of rows][lane]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
-    const int ops = few_operands<E, CODES>(a.dim);
+    const int ops = few_operands<E, CODES, THIRDS>(a.dim);
     // h's alignment is its own where the table is in 8 bits
     constexpr int kBytesH = CODES ? 2 : BYTES;
-    for (int j = threadIdx.x; j < ops * NB * 64; j += kWaves * 64) {
+    bf16x8* sh3 = reinterpret_cast<bf16x8*>(lds);  // [pair][part][block of rows][lane]
+    for (int j = threadIdx.x; j < (THIRDS ? ops / 2 : ops) * NB * 64; j += kWaves * 64) {
         const int l = j & 63, b = (j >> 6) % NB, k = (j >> 6) / NB;
         const int64_t row = 16 * b + (l & 15);
+        if constexpr (THIRDS) {
+            f32x4 v[2] = {};
+            if (row < a.n) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    v[e] = load_few_cols<E, kBytesH>(static_cast<const E*>(a.h) + row * a.ld_h,
+                                                     Table::column(2 * k + e, l >> 4), a.dim);
+            }
+            const Thirds r = thirds(v[0], v[1]);
+#pragma unroll
+            for (int part = 0; part < 3; ++part) sh3[((k * 3 + part) * NB + b) * 64 + l] = r.p[part];
+            continue;
+        }
         sh[j] = row < a.n ? load_few_cols<E, kBytesH>(static_cast<const E*>(a.h) + row * a.ld_h,
                                                     Table::column(k, l >> 4), a.dim)
                           : Vec{};
@@ -1059,6 +1098,28 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
                 term[i] = k >= a.classes ? -INFINITY : a.bias == nullptr ? 0.f : a.bias[k];
             }
         }
+        if constexpr (THIRDS) {
+#pragma unroll
+            for (int i = 0; i < kFewGroup; i += 2)
+                if (g * kFewGroup + i < ops) {
+                    const Thirds w = thirds(now.operand(i), now.operand(i + 1));
+                    const int pair = (g * kFewGroup + i) / 2;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        bf16x8 h[3];
+#pragma unroll
+                        for (int part = 0; part < 3; ++part)
+                            h[part] = sh3[((pair * 3 + part) * NB + b) * 64 + lane];
+                        using B = Few<bf16_t>;
+                        c[b] = B::mfma(w.p[2], h[0], c[b]);
+                        c[b] = B::mfma(w.p[0], h[2], c[b]);
+                        c[b] = B::mfma(w.p[1], h[1], c[b]);
+                        c[b] = B::mfma(w.p[1], h[0], c[b]);
+                        c[b] = B::mfma(w.p[0], h[1], c[b]);
+                        c[b] = B::mfma(w.p[0], h[0], c[b]);
+                    }
+                }
+        } else
 #pragma unroll
         for (int i = 0; i < kFewGroup; ++i)
             if (g * kFewGroup + i < ops) {
@@ -1750,14 +1811,14 @@ int64_t few_grid(int64_t classes) {
 }
 
 // of answers: the entries of a row are all_slots, these from slot0 on.
-template <typename E, int NB, bool ANSWER = false, bool CODES = false>
+template <typename E, int NB, bool ANSWER = false, bool CODES = false, bool THIRDS = false>
 hipError_t few_pass(const SoftmaxArgs& a, void* part, int64_t* slots, hipStream_t s,
                     float* best = nullptr, int64_t all_slots = 0, int64_t slot0 = 0) {
     constexpr int kWaves = few_waves(NB);
     const int64_t tiles = div_up(a.classes, 16), blocks = few_grid<NB>(a.classes);
-    const int lds = few_operands<E, CODES>(a.dim) * NB * 1024;
+    const int lds = few_kb<E, CODES, THIRDS>(a.dim) * NB * 1024;
     auto go = [&](auto bytes) {
-        constexpr auto* kKernel = &k_sm_few<E, NB, decltype(bytes)::value, ANSWER, CODES>;
+        constexpr auto* kKernel = &k_sm_few<E, NB, decltype(bytes)::value, ANSWER, CODES, THIRDS>;
         if (lds > 60 * 1024) SM_TRY(allow_lds<kKernel>(kFewLds<E>));
         kKernel<<<dim3((uint32_t)blocks), kWaves * 64, lds, s>>>(a, tiles, part, 16 * NB, all_slots, slot0, best);
         return hipGetLastError();
