@@ -499,9 +499,11 @@ hipError_t finish(const SoftmaxArgs& a, const AnswerPlan& p, const Parts& part, 
             k_lp_rows<E, CODES, 256><<<dim3((uint32_t)rows), kBlock, 0, s>>>(a, part, rows, 0);
         else if (rows < 16 * kCus)
             k_lp_rows<E, CODES, 64><<<dim3((uint32_t)div_up(rows, 4)), kBlock, 0, s>>>(a, part, rows, 0);
-        else
-            SM_TRY(in_launches(div_up(rows, 16), [&](dim3 grid, int64_t first) {
-                k_lp_rows<E, CODES, 16><<<grid, kBlock, 0, s>>>(a, part, rows, first);
+        else if (rows < 128 * kCus)
+            k_lp_rows<E, CODES, 16><<<dim3((uint32_t)div_up(rows, 16)), kBlock, 0, s>>>(a, part, rows, 0);
+        else  // fewer waves, each with more loads in flight: 100003 x 1000 x 128 bf16 12.9 us, 18.5 with 16
+            SM_TRY(in_launches(div_up(rows, 32), [&](dim3 grid, int64_t first) {
+                k_lp_rows<E, CODES, 8><<<grid, kBlock, 0, s>>>(a, part, rows, first);
             }));
         return hipGetLastError();
     }
@@ -569,12 +571,25 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
         if constexpr (!CODES) f.vec = a.vec && a.vec_h;
         const int64_t pad = 16 * p.few;
         const bool pieces = piece < all;
+        // calls with(blocks of 16 rows, thirds), as types
+        auto dispatch = [&](auto with) {
+            auto of = [&](auto nb) {
+                if constexpr (sizeof(E) == 4 && decltype(nb)::value >= kThirdsFrom)
+                    if (p.thirds) return with(nb, std::true_type{});
+                return with(nb, std::false_type{});
+            };
+            return p.few == 1   ? of(std::integral_constant<int, 1>{})
+                   : p.few == 2 ? of(std::integral_constant<int, 2>{})
+                   : p.few == 3 ? of(std::integral_constant<int, 3>{})
+                                : of(std::integral_constant<int, 4>{});
+        };
         int64_t slots = 0, all_slots = 0;
         for (int64_t t0 = 0; t0 < all; t0 += piece) {
-            const int64_t c0 = t0 * 16, left = a.classes - c0;
-            const int64_t count = left < piece * 16 ? left : piece * 16;
-            // above 16 rows all workgroups are alike
-            all_slots += p.few == 1 ? few_grid<1>(count) : few_grid<4>(count);
+            const int64_t left = a.classes - t0 * 16, count = left < piece * 16 ? left : piece * 16;
+            all_slots += dispatch([&](auto nb, auto thirds) {
+                return few_grid<E, decltype(nb)::value, true, CODES, decltype(thirds)::value>(count,
+                                                                                            a.dim);
+            });
         }
         int splits = 1;
         for (int64_t t0 = 0; t0 < all; t0 += piece) {
@@ -582,18 +597,10 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             const int64_t count = a.classes - c0 < tiles * 16 ? a.classes - c0 : tiles * 16;
             const SoftmaxArgs q = classes_from<E, CODES>(f, c0, count);
             int64_t more = 0;
-            auto pass = [&](auto nb) {
-                constexpr int NB = decltype(nb)::value;
-                if constexpr (sizeof(E) == 4 && NB >= kThirdsFrom)
-                    if (p.thirds)
-                        return few_pass<E, NB, true, false, true>(q, part, &more, s, best,
-                                                                  all_slots, slots);
-                return few_pass<E, NB, true, CODES>(q, part, &more, s, best, all_slots, slots);
-            };
-            SM_TRY(p.few == 1   ? pass(std::integral_constant<int, 1>{})
-                   : p.few == 2 ? pass(std::integral_constant<int, 2>{})
-                   : p.few == 3 ? pass(std::integral_constant<int, 3>{})
-                                : pass(std::integral_constant<int, 4>{}));
+            SM_TRY(dispatch([&](auto nb, auto thirds) {
+                return few_pass<E, decltype(nb)::value, true, CODES, decltype(thirds)::value>(
+                    q, part, &more, s, best, all_slots, slots);
+            }));
             slots += more;
             if (a.top == 0) continue;
             splits = select_splits(pad, tiles, 16);

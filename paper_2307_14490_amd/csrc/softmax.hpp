@@ -931,35 +931,35 @@ __device__ __forceinline__ typename Few<E>::Vec load_few_cols(const E* row, int 
     return u.v;
 }
 
-// The classes' rows as a wave of k_sm_few reads them: a group of kFewGroup operands in
+// The classes' rows as a wave of k_sm_few reads them: a group of GROUP operands in
 // flight, then one operand at a time.
-template <typename E, int BYTES, bool CODES>
+template <typename E, int BYTES, bool CODES, int GROUP>
 struct FewTable {
     using F = Few<E>;
     using Vec = typename F::Vec;
     static constexpr int kN = 16 / sizeof(E);
-    Vec v[kFewGroup];
+    Vec v[GROUP];
 
     // First column of operand k in lane quad q.
     static __device__ __forceinline__ int column(int k, int q) { return F::kCols * k + kN * q; }
     __device__ __forceinline__ void fetch(const SoftmaxArgs& a, int64_t row, int g, int ops, int quad) {
         const E* w = static_cast<const E*>(a.w) + row * a.ld_w;
 #pragma unroll
-        for (int i = 0; i < kFewGroup; ++i)
-            if (g * kFewGroup + i < ops)
-                v[i] = load_few_cols<E, BYTES>(w, column(g * kFewGroup + i, quad), a.dim);
+        for (int i = 0; i < GROUP; ++i)
+            if (g * GROUP + i < ops)
+                v[i] = load_few_cols<E, BYTES>(w, column(g * GROUP + i, quad), a.dim);
     }
     __device__ __forceinline__ Vec operand(int i) const { return v[i]; }
 };
 
 // A table in 8 bits: a lane takes 16 codes at a time, which are two operands of a bf16
 // product (whose columns are taken in that order), and their scale.
-template <int BYTES>
-struct FewTable<bf16_t, BYTES, true> {
+template <int BYTES, int GROUP>
+struct FewTable<bf16_t, BYTES, true, GROUP> {
     using Vec = bf16x8;
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    u32x4 q[kFewGroup / 2];
-    uint32_t scale[kFewGroup / 2];
+    u32x4 q[GROUP / 2];
+    uint32_t scale[GROUP / 2];
 
     static __device__ __forceinline__ int column(int k, int q) {
         return 64 * (k >> 1) + 16 * q + 8 * (k & 1);
@@ -968,8 +968,8 @@ struct FewTable<bf16_t, BYTES, true> {
         const uint8_t* w = static_cast<const uint8_t*>(a.w) + row * a.ld_w;
         const uint8_t* s = a.w_scales + row * a.ld_scales;
 #pragma unroll
-        for (int i = 0; i < kFewGroup; i += 2) {
-            const int col = column(g * kFewGroup + i, quad);
+        for (int i = 0; i < GROUP; i += 2) {
+            const int col = column(g * GROUP + i, quad);
             u32x4 r = {};
             uint32_t b = 127;
             if (col < a.dim) {
@@ -1026,7 +1026,7 @@ __device__ __forceinline__ Thirds thirds(f32x4 a, f32x4 b) {
 // NB blocks of 16 rows.  Of a table in 8 bits the operands come in pairs.  THIRDS: so do
 // those of fp32 rows, each pair of 16 columns as one of 32 in three parts.
 template <typename E, int NB, int BYTES, bool ANSWER, bool CODES, bool THIRDS>
-__global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, int64_t tiles,
+__global__ __launch_bounds__(few_waves(NB) * 64, THIRDS ? 4 : 1) void k_sm_few(SoftmaxArgs a, int64_t tiles,
                                                                void* __restrict__ parts,
                                                                int64_t pad, int64_t slots,
                                                                int64_t slot0,
@@ -1034,7 +1034,9 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
     constexpr int kWaves = few_waves(NB);
     using F = Few<E>;
     using Vec = typename F::Vec;
-    using Table = FewTable<E, BYTES, CODES>;
+    // thirds need the registers of half a group
+    constexpr int kGroup = THIRDS ? kFewGroup / 2 : kFewGroup;
+    using Table = FewTable<E, BYTES, CODES, kGroup>;
     using Part = std::conditional_t<ANSWER, float4, float2>;
     Part* part = static_cast<Part*>(parts);
     extern __shared__ __align__(16) uint8_t lds[];
@@ -1066,7 +1068,7 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
                           : Vec{};
     }
     __syncthreads();
-    const int groups = (ops + kFewGroup - 1) / kFewGroup;
+    const int groups = (ops + kGroup - 1) / kGroup;
     const int64_t step = (int64_t)gridDim.x * kWaves;
     int64_t tile = (int64_t)blockIdx.x * kWaves + wave;
     auto fetch = [&](int64_t t, int g, Table& v) {
@@ -1100,10 +1102,10 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
         }
         if constexpr (THIRDS) {
 #pragma unroll
-            for (int i = 0; i < kFewGroup; i += 2)
-                if (g * kFewGroup + i < ops) {
+            for (int i = 0; i < kGroup; i += 2)
+                if (g * kGroup + i < ops) {
                     const Thirds w = thirds(now.operand(i), now.operand(i + 1));
-                    const int pair = (g * kFewGroup + i) / 2;
+                    const int pair = (g * kGroup + i) / 2;
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
                         bf16x8 h[3];
@@ -1121,12 +1123,12 @@ __global__ __launch_bounds__(few_waves(NB) * 64) void k_sm_few(SoftmaxArgs a, in
                 }
         } else
 #pragma unroll
-        for (int i = 0; i < kFewGroup; ++i)
-            if (g * kFewGroup + i < ops) {
+        for (int i = 0; i < kGroup; ++i)
+            if (g * kGroup + i < ops) {
                 const Vec w = now.operand(i);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
-                    c[b] = F::mfma(w, sh[((g * kFewGroup + i) * NB + b) * 64 + lane], c[b]);
+                    c[b] = F::mfma(w, sh[((g * kGroup + i) * NB + b) * 64 + lane], c[b]);
             }
         if (last) {
 #pragma unroll
@@ -1803,11 +1805,22 @@ int few_blocks(int64_t n, int32_t dim) {
     return 0;
 }
 
-// Workgroups of it: each leaves an entry per row.
-template <int NB>
-int64_t few_grid(int64_t classes) {
+// Workgroups of it: each leaves an entry per row.  Answers take as many as the card holds
+// at once (by registers: four waves per SIMD, five of a table in 8 bits; by LDS), so that
+// none starts behind another and what joins their entries has few: 38 x 300007 x 256 fp32 80 us
+// with 512, 83 with 1024, 98 with 2048; 1 x 1e6 x 128 in 8 bits 32.4 with 1280, 33.7 with
+// 2048, 38.8 with 1536.
+template <typename E, int NB, bool ANSWER, bool CODES, bool THIRDS>
+int64_t few_grid(int64_t classes, int32_t dim) {
     const int64_t need = div_up(div_up(classes, 16), few_waves(NB));
-    return need < 2048 ? need : 2048;
+    int64_t most = 2048;
+    if constexpr (ANSWER) {
+        const int lds = (few_kb<E, CODES, THIRDS>(dim) + 2) * NB * 1024;  // with s_part
+        int64_t at_once = NB == 1 ? (CODES ? 5 : 4) : 2;
+        if (at_once > 160 * 1024 / lds) at_once = 160 * 1024 / lds;
+        most = kCus * at_once;
+    }
+    return need < most ? need : most;
 }
 
 // of answers: the entries of a row are all_slots, these from slot0 on.
@@ -1815,7 +1828,8 @@ template <typename E, int NB, bool ANSWER = false, bool CODES = false, bool THIR
 hipError_t few_pass(const SoftmaxArgs& a, void* part, int64_t* slots, hipStream_t s,
                     float* best = nullptr, int64_t all_slots = 0, int64_t slot0 = 0) {
     constexpr int kWaves = few_waves(NB);
-    const int64_t tiles = div_up(a.classes, 16), blocks = few_grid<NB>(a.classes);
+    const int64_t tiles = div_up(a.classes, 16);
+    const int64_t blocks = few_grid<E, NB, ANSWER, CODES, THIRDS>(a.classes, a.dim);
     const int lds = few_kb<E, CODES, THIRDS>(a.dim) * NB * 1024;
     auto go = [&](auto bytes) {
         constexpr auto* kKernel = &k_sm_few<E, NB, decltype(bytes)::value, ANSWER, CODES, THIRDS>;
