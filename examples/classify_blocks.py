@@ -78,23 +78,26 @@ def train_exact(workload, epochs, batch, log, lr=1e-2, states="f32"):
     return rows
 
 
-def classify(rows, block, classes, log, steps=200):
-    """Test accuracy of a softmax head on the rows of half of the nodes."""
+def classify(rows, block, classes, log, steps=200, norm="layer", max_norm=None):
+    """Test accuracy of a softmax head on the rows of half of the nodes: how often the
+    most likely block is the node's."""
     import torch
 
     import paper_2307_14490_amd as P
     label = torch.from_numpy(block.astype(np.int32)).cuda()
     half = torch.randperm(len(block), generator=torch.Generator().manual_seed(1)).cuda()
     train, test = half[: len(block) // 2], half[len(block) // 2:]
-    head = P.SoftmaxHead(classes, rows.shape[1], train.numel(), lr=1e-2)
+    head = P.SoftmaxHead(classes, rows.shape[1], len(block), lr=1e-2, norm=norm,
+                         max_norm=max_norm, top=1)
     x, y = rows[train].contiguous(), label[train]
     for step in range(steps):
         loss, _ = head.step(x, y, want_dx=False)
     log(f"classifier: loss {loss.item():.4f} a node after {steps} steps")
     head.check()
-    z, _, _ = P.layer_norm(rows[test].contiguous(), head.gamma, head.beta, head.eps)
-    found = (z @ head.w.t() + head.bias).argmax(1)
-    return (found == label[test]).float().mean().item()
+    answers = head.answers(rows[test].contiguous(), label[test])
+    log(f"classifier: log probability {answers.logp.mean().item():.4f} of a node's block, entropy "
+        f"{answers.entropy.mean().item():.4f}")
+    return (answers.ids[:, 0] == label[test]).float().mean().item()
 
 
 def main(argv=None, log=print):
@@ -104,6 +107,10 @@ def main(argv=None, log=print):
     ap.add_argument("--batch", type=int, default=8192)
     ap.add_argument("--states", choices=("f32", "q8"), default="f32",
                     help="moments of AdamW in 32 or in 8 bits")
+    ap.add_argument("--norm", choices=("layer", "rms"), default="layer",
+                    help="the classifier's norm")
+    ap.add_argument("--clip", type=float, default=None,
+                    help="largest norm of the classifier's gradients")
     a = ap.parse_args(argv)
     from synth import make_workload
     workload = make_workload("tiny", 0)
@@ -111,7 +118,8 @@ def main(argv=None, log=print):
         rows = train_exact(workload, a.epochs, a.batch, log, states=a.states)
     else:
         rows = train_sampled(workload, a.epochs, log)
-    accuracy = classify(rows, blocks_of(workload), workload.cfg.blocks, log)
+    accuracy = classify(rows, blocks_of(workload), workload.cfg.blocks, log, norm=a.norm,
+                        max_norm=a.clip)
     log(f"{a.objective}: {100 * accuracy:.1f}% of the other half's blocks found "
         f"({100 / workload.cfg.blocks:.0f}% by chance)")
     return accuracy

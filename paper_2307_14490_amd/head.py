@@ -455,59 +455,130 @@ class AdamW(_Status):
 # A head that trains
 # --------------------------------------------------------------------------- #
 class SoftmaxHead:
-    """Layer norm, a linear layer and the softmax loss over num_classes classes on
-    rows of embeddings, trained by AdamW: the downstream classifier of Sec. 4.2,
-    or the exact softmax over all nodes that negative sampling stands in for.
+    """A norm, a linear layer and the softmax loss over num_classes classes on rows of
+    embeddings, trained by AdamW: the downstream classifier of Sec. 4.2, or the exact
+    softmax over all nodes that negative sampling stands in for.
+
+    norm: "layer", or "rms" (no beta).  max_norm: steps clip the gradients of all
+    parameters together to that norm, and norm_before holds what it was.  top: with a
+    number the head also answers (that many of the most likely classes) and trains by
+    log probabilities.
 
     step(x, labels) trains the head on rows x (n x dim) and returns the mean loss
-    (device) and the gradient of x, for a caller that trains the rows too.  Steps and
-    losses on different streams wait for each other; what a call returns is ready
-    on its own stream."""
+    (device) and the gradient of x, for a caller that trains the rows too.  Steps,
+    losses and answers on different streams wait for each other; what a call returns is
+    ready on its own stream."""
 
     def __init__(self, num_classes, dim, max_rows, dtype="f32", lr=1e-3, weight_decay=0.01,
-                 states="f32", eps=1e-5, seed=0, device="cuda"):
+                 states="f32", eps=1e-5, seed=0, device="cuda", norm="layer", max_norm=None,
+                 top=None):
         import torch
+        if norm not in ("layer", "rms"):
+            raise ValueError(f"SoftmaxHead: norm {norm!r}")
+        if max_norm is not None and not float(max_norm) > 0:
+            raise ValueError(f"SoftmaxHead: max_norm {max_norm}")
+        self.norm, self.max_norm, self.norm_before = norm, max_norm, None
         self.op = SoftmaxLoss(max_rows, num_classes, dim, dtype=dtype, device=device)
         dev = self.op.device
+        self.answering = None
+        if top is not None:
+            from .answer import LogProbs
+            self.answering = LogProbs(max_rows, num_classes, dim, dtype=dtype, top=top, grad=True,
+                                      device=device)
         g = torch.Generator(device=dev).manual_seed(int(seed))
         self.eps = float(eps)
         self.gamma = torch.ones(dim, device=dev)
-        self.beta = torch.zeros(dim, device=dev)
+        self.beta = torch.zeros(dim, device=dev) if norm == "layer" else None
         w = torch.randn((num_classes, dim), device=dev, generator=g) * dim ** -0.5
         self.w = w.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
         self.bias = torch.zeros(num_classes, device=dev)
-        self.opt = AdamW([self.gamma, self.beta, self.w, self.bias], lr=lr,
+        of_norm = [self.gamma, self.beta] if norm == "layer" else [self.gamma]
+        self.opt = AdamW([*of_norm, self.w, self.bias], lr=lr,
                          weight_decay=weight_decay, states=states)
         self.total = torch.zeros(1, dtype=torch.float64, device=dev)
         self.op._own.append(self.total)
 
     def _ordered(self, stream):
-        # before the first kernel: layer norm, which waits for nothing, reads parameters
+        # before the first kernel: the norm, which waits for nothing, reads parameters
         self.op._ordered(stream)
+        if self.answering is not None:
+            self.answering._ordered(stream)
         self.opt._ordered(stream)
+
+    def _normed(self, x, stream):
+        """The normalised rows, and what the backward pass needs of them."""
+        if self.norm == "layer":
+            y, *kept = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
+        else:
+            from .answer import rms_norm
+            y, _, *kept = rms_norm(x, self.gamma, eps=self.eps, stream=stream)
+        return y, kept
+
+    def _update(self, x, kept, dy, dw, db, lr, want_dx, stream):
+        """The step behind the gradients of the linear layer; dx, or None."""
+        if self.norm == "layer":
+            dx, *of_norm = layer_norm_backward(dy, x, self.gamma, *kept, want_dx=want_dx,
+                                               stream=stream)
+        else:
+            from .answer import rms_norm_backward
+            dx, *of_norm = rms_norm_backward(dy, x, self.gamma, *kept, want_dx=want_dx,
+                                             stream=stream)
+        self.norm_before = self.opt.step([*of_norm, dw, db], lr=lr, max_norm=self.max_norm,
+                                         stream=stream)
+        return dx
 
     def loss(self, x, labels, weights=None, stream=None):
         """Loss per row, forward only."""
         self._ordered(stream)
-        y, _, _ = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
+        y, _ = self._normed(x, stream)
         return self.op.loss(y, self.w, labels, self.bias, weights, stream=stream)[0]
 
     def step(self, x, labels, weights=None, lr=None, want_dx=True, stream=None):
         """One training step on the mean over the rows of their losses."""
         scale = 1.0 / max(1, x.shape[0])
         self._ordered(stream)
-        y, mean, rstd = layer_norm(x, self.gamma, self.beta, self.eps, stream=stream)
+        y, kept = self._normed(x, stream)
         _, lse = self.op.loss(y, self.w, labels, self.bias, weights, total=self.total,
                               stream=stream)
         dy, dw, db = self.op.grad(y, self.w, labels, lse, self.bias, weights, scale=scale,
                                   stream=stream)
-        dx, dgamma, dbeta = layer_norm_backward(dy, x, self.gamma, mean, rstd, want_dx=want_dx,
-                                                stream=stream)
-        self.opt.step([dgamma, dbeta, dw, db], lr=lr, stream=stream)
+        dx = self._update(x, kept, dy, dw, db, lr, want_dx, stream)
         with _on(self.op.device, stream, ()):
             return self.total * scale, dx
+
+    def _answering(self, what):
+        if self.answering is None:
+            raise ValueError(f"SoftmaxHead.{what}: the head was made without top")
+        return self.answering
+
+    def answers(self, x, labels=None, stream=None):
+        """Log probabilities of the labels, entropies and the most likely classes (Answers)."""
+        op = self._answering("answers")
+        self._ordered(stream)
+        y, _ = self._normed(x, stream)
+        return op.log_probs(y, self.w, labels, self.bias, stream=stream)
+
+    def policy_step(self, x, labels, advantages, entropy_weight=0.0, lr=None, want_dx=True,
+                    stream=None):
+        """One training step that raises the mean over the rows of advantage logp +
+        entropy_weight entropy (advantages: float32 of either sign).  Returns the rows'
+        Answers before the step and the gradient of x of that mean's negative."""
+        import torch
+        op = self._answering("policy_step")
+        n = x.shape[0]
+        _vector(advantages, n, torch.float32, "SoftmaxHead.policy_step advantages", x.device)
+        self._ordered(stream)
+        y, kept = self._normed(x, stream)
+        a = op.log_probs(y, self.w, labels, self.bias, stream=stream)
+        with _on(self.op.device, stream, (advantages,)):
+            dlogp = advantages * (-1.0 / max(1, n))
+            dentropy = torch.full((n,), -float(entropy_weight) / max(1, n), device=self.op.device)
+        dy, dw, db = op.grad(y, self.w, a, labels, dlogp, dentropy, self.bias, stream=stream)
+        return a, self._update(x, kept, dy, dw, db, lr, want_dx, stream)
 
     def check(self):
         """Raise the first device-side error since the last check."""
         self.op.check()
+        if self.answering is not None:
+            self.answering.check()
         self.opt.check()
