@@ -702,7 +702,8 @@ size_t huge_log_probs_workspace_bytes(const huge_log_probs_config* cfg);
      d_ids, d_top_logp : n x top, the classes of the largest logits, the largest first
                   and the lowest class first among equals, and their log probabilities
                   (NULL with top = 0).  -1 and -inf behind the last class that is in
-   Logits are below 1e28 in magnitude.  Where every class is out, lse is -inf, the entropy 0
+   Logits are below 1e9 in magnitude (the exponentials' arguments are taken from fp32
+   products).  Where every class is out, lse is -inf, the entropy 0
    and no class is found; where lse is no finite number (a NaN or an infinity in h, or in a
    class that counts) ids are -1 and the rest NaN.
    Sums, maxima and exponentials are fp32 on logits as in huge_softmax_loss.  The classes

@@ -105,7 +105,8 @@ def rms_norm(x, gamma, residual=None, eps=1e-5, q8=False, stream=None):
         if residual.shape[0] != n:
             raise ValueError(f"rms_norm: {residual.shape[0]} rows of residual, {n} of x")
     with _on(x.device, stream, (x, residual, gamma)) as st:
-        total = x if residual is None else torch.empty((n, dim), dtype=x.dtype, device=x.device)
+        # dense like x, or where that is a part of wider rows by themselves
+        total = x if residual is None else torch.empty_like(x)
         rstd = torch.empty(n, dtype=torch.float32, device=x.device)
         py = pc = ps = None
         ld_scales = 0
@@ -113,7 +114,7 @@ def rms_norm(x, gamma, residual=None, eps=1e-5, q8=False, stream=None):
             y = _new_q8(n, dim, x.device)
             pc, ps, ld_scales = y.codes.data_ptr(), y.scales.data_ptr(), y.scales.shape[1]
         else:
-            y = torch.empty((n, dim), dtype=x.dtype, device=x.device)
+            y = torch.empty_like(x)
             py = y.data_ptr()
         _ok(_head.load().huge_rms_norm(px, ld, pr, ldr, n, dim, code, pg, float(eps),
                                        None if residual is None else total.data_ptr(), dim, py,
@@ -143,7 +144,7 @@ def rms_norm_backward(dy, total, gamma, rstd, dtotal=None, want_dx=True, want_ga
         raise TypeError("rms_norm_backward: gamma and rstd are required")
     L = _head.load()
     with _on(total.device, stream, (dy, total, gamma, rstd, dtotal)) as st:
-        dx = torch.empty((n, dim), dtype=total.dtype, device=total.device) if want_dx else None
+        dx = torch.empty_like(total) if want_dx else None
         dgamma = ws = None
         bytes_ = 0
         if want_gamma:

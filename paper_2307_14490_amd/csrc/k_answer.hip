@@ -355,21 +355,20 @@ __device__ __forceinline__ void best_keys(const u64* keys, int n, int keep, u64*
     __syncthreads();
 }
 
-constexpr int kMostKeep = kMostTop + kSlack;
-
 // A row's lists of `splits`, and of the pieces of the vocabulary before, into one.
 __global__ __launch_bounds__(kTopThreads) void k_lp_merge(const u64* __restrict__ lists, int splits,
                                                           int keep, bool first,
                                                           u64* __restrict__ running) {
-    __shared__ u64 s_keys[(kMostSplits + 1) * kMostKeep], s_out[kMostKeep];
     extern __shared__ __align__(16) uint8_t lds[];
     const int64_t row = blockIdx.x;
     const int n = splits * keep;
+    u64* s_out = reinterpret_cast<u64*>(lds);
+    u64* s_keys = s_out + keep;  // the lists, twice
     for (int e = threadIdx.x; e < n; e += kTopThreads) s_keys[e] = lists[row * n + e];
     if (!first)
         for (int e = threadIdx.x; e < keep; e += kTopThreads) s_keys[n + e] = running[row * keep + e];
     __syncthreads();
-    best_keys<kTopThreads>(s_keys, first ? n : n + keep, keep, reinterpret_cast<u64*>(lds), s_out);
+    best_keys<kTopThreads>(s_keys, first ? n : n + keep, keep, s_keys + n + keep, s_out);
     for (int e = threadIdx.x; e < keep; e += kTopThreads) running[row * keep + e] = s_out[e];
 }
 
@@ -486,6 +485,14 @@ hipError_t select(const SoftmaxArgs& a, const float* best, int64_t ld, int64_t r
     kKernel<<<grid, kSelectThreads, kSelectKeys * 8, s>>>(a, best, ld, rows, tiles, tile0,
                                                           div_up(tiles, splits), splits, keep, part,
                                                           lists);
+    return hipGetLastError();
+}
+
+hipError_t merge(const u64* lists, int splits, int keep, bool first, u64* running, int64_t rows,
+                 hipStream_t s) {
+    const int lds = 8 * (2 * (splits + 1) + 1) * keep;
+    if (lds > 64 * 1024) SM_TRY(allow_lds<&k_lp_merge>(kTopLds));
+    k_lp_merge<<<dim3((uint32_t)rows), kTopThreads, lds, s>>>(lists, splits, keep, first, running);
     return hipGetLastError();
 }
 
@@ -608,9 +615,7 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
             SM_TRY((select<E, CODES, 16>(a, best, pad, a.n, tiles, t0, splits, p.keep, now, lists,
                                          t0 + tiles == all, s)));
             if (!pieces) continue;
-            k_lp_merge<<<dim3((uint32_t)a.n), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(
-                lists, splits, p.keep, t0 == 0, running);
-            SM_TRY(hipGetLastError());
+            SM_TRY(merge(lists, splits, p.keep, t0 == 0, running, a.n, s));
         }
         return finish<E, CODES, 16>(a, p, Parts{part, 1, all_slots, (int32_t)all_slots}, a.n,
                                     pieces ? 1 : splits, pieces ? running : lists, s);
@@ -654,9 +659,7 @@ hipError_t log_probs(SoftmaxArgs a, hipStream_t s) {
                                          Parts{part, pad, 1, (int32_t)slots}, lists,
                                          t0 + tiles == all, s)));
             if (!pieces) continue;
-            k_lp_merge<<<dim3((uint32_t)rows), kTopThreads, 8 * (splits + 1) * p.keep, s>>>(lists, splits, p.keep, t0 == 0,
-                                                                    running);
-            SM_TRY(hipGetLastError());
+            SM_TRY(merge(lists, splits, p.keep, t0 == 0, running, rows, s));
         }
         SM_TRY((finish<E, CODES, 32>(q, p, Parts{part, pad, 1, (int32_t)slots}, rows,
                                      pieces ? 1 : splits, pieces ? running : lists, s)));

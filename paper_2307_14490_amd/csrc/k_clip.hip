@@ -129,7 +129,10 @@ __device__ __forceinline__ double block_sum(double v, double* s) {
 __global__ __launch_bounds__(kBlock) void k_squares(ClipArgs a, double* __restrict__ part) {
     __shared__ double s[kBlock / 64];
     double v = 0.0;
-    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) v += squares<kBlock>(chunk_of(a, c));
+    // from the last chunk on: the step that follows starts at the first, whose elements are then
+    // the last that were read (129e6 fp32 elements and AdamW's step: 704 -> 694 us)
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x)
+        v += squares<kBlock>(chunk_of(a, a.chunks - 1 - c));
     v = block_sum<kBlock>(v, s);
     if (threadIdx.x == 0) part[blockIdx.x] = v;
 }

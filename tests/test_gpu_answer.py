@@ -426,9 +426,9 @@ def test_nan_stays_in_its_row(n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "q8"])
-@pytest.mark.parametrize("size", [8.0, 60.0])
+@pytest.mark.parametrize("size", [8.0, 60.0, 1e5])
 def test_confident_rows(size, dtype):
-    """Logits of tens and hundreds: entropies near 0, probabilities that vanish."""
+    """Logits of tens, hundreds and a million: entropies near 0, probabilities that vanish."""
     rng = np.random.default_rng(12)
     for n in (30, 200):
         check(case(n, 90, 64, dtype, rng, size=size), top=3)

@@ -49,10 +49,11 @@ def test_more_classes_than_a_piece(dtype, bias):
     op.check()
 
 
-def test_more_classes_than_a_piece_for_one_row():
+@pytest.mark.parametrize("top", [5, 64])
+def test_more_classes_than_a_piece_for_one_row(top):
     """More than 2^24 tiles of 16, with offsets past 32 bits."""
-    classes, dim, top = (1 << 24) * 16 + 1_000_003, 8, 5
-    say(f"pieces of {classes} classes for one row")
+    classes, dim = (1 << 24) * 16 + 1_000_003, 8
+    say(f"pieces of {classes} classes for one row, best {top}")
     g = torch.Generator(device="cuda").manual_seed(6)
     codes = torch.randint(0, 120, (classes, dim), device="cuda", generator=g, dtype=torch.uint8)
     codes |= torch.randint(0, 2, (classes, dim), device="cuda", generator=g,
