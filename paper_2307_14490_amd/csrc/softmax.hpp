@@ -660,7 +660,7 @@ constexpr float kRiseAnswer = 2.f;
 
 // The same from another top at or above.
 __device__ __forceinline__ Stats raise(Stats s, float top) {
-    const float d = (s.top - top) * kLog2e, f = exp2f(d);
+    const float d = (s.top - top) * kLog2e, f = __builtin_amdgcn_exp2f(d);
     return {top, s.sum * f, f * fmaf(d, s.sum, s.first)};
 }
 __device__ __forceinline__ Stats join(Stats a, Stats b) {
@@ -770,7 +770,7 @@ void k_sm_lse(PassArgs a) {
                     most[b] = fmaxf(most[b], m);
                     if (__ballot(m > top[b] + kRiseAnswer) != 0) {
                         const float up = fmaxf(m, top[b]), d = (top[b] - up) * kLog2e;
-                        const float f = exp2f(d);
+                        const float f = __builtin_amdgcn_exp2f(d);
                         first[b][0] = fmaf(d, sum[b], first[b][0]);
 #pragma unroll
                         for (int k = 0; k < kSums; ++k) first[b][k] *= f;
@@ -1005,6 +1005,16 @@ struct FewTable<bf16_t, BYTES, true, GROUP> {
     }
 };
 
+// The largest over the four lanes that are 16 apart (as xor_add).
+__device__ __forceinline__ float quads_max(float v) {
+    const int a = __float_as_int(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    v = fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+    const int b = __float_as_int(v);
+    const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return fmaxf(__int_as_float(q[0]), __int_as_float(q[1]));
+}
+
 // An fp32 number as the sum of three bf16 ones, each the nearest to what the ones before
 // leave: within 2^-27 of it.  Of the nine products of two such sums the six above 2^-27 are
 // formed, the smallest first, which is an fp32 product but for its rounding, at six bf16
@@ -1141,12 +1151,13 @@ __global__ __launch_bounds__(few_waves(NB) * 64, THIRDS ? 4 : 1) void k_sm_few(S
                         m = fmaxf(m, x[i]);
                     }
                     if (best != nullptr) {
-                        float t = fmaxf(m, __shfl_xor(m, 16));
-                        t = fmaxf(t, __shfl_xor(t, 32));
+                        const float t = quads_max(m);
                         if (lane < 16) best[tile * pad + 16 * b + lane] = t;
                     }
-                    const Stats s = raise({top[b], sum[b], first[b]}, fmaxf(m, top[b]));
-                    top[b] = s.top, sum[b] = s.sum, first[b] = s.first;
+                    if (__ballot(m > top[b]) != 0) {
+                        const Stats s = raise({top[b], sum[b], first[b]}, fmaxf(m, top[b]));
+                        top[b] = s.top, sum[b] = s.sum, first[b] = s.first;
+                    }
                     const float sub = -top[b] * kLog2e;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
