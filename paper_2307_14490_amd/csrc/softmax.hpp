@@ -733,11 +733,10 @@ void k_sm_lse(PassArgs a) {
             f32x16 c[XB], term = {};
             if constexpr (!DIRECT) {
                 term = row_values(rec, kTerm, half);
-            } else if (yt * 32 + 32 > a.classes) {
+            } else if (!ANSWER && yt * 32 + 32 > a.classes) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (yt * 32 + tile_row(i, half) >= a.classes)
-                        term[i] = ANSWER ? kFloor : -INFINITY;
+                    if (yt * 32 + tile_row(i, half) >= a.classes) term[i] = -INFINITY;
             }
 #pragma unroll
             for (int b = 0; b < XB; ++b) c[b] = Kind<E>::kScaled ? f32x16{} : term;
@@ -750,6 +749,17 @@ void k_sm_lse(PassArgs a) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         c[b][i] = fmaf(c[b][i] * ymul[i], xmul[b], term[i]);
+            }
+            // behind the products: their sum then starts from a constant 0, which costs nothing,
+            // and not from 16 registers that are filled for every tile
+            if constexpr (ANSWER && DIRECT) {
+                if (yt * 32 + 32 > a.classes) {
+#pragma unroll
+                    for (int b = 0; b < XB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (yt * 32 + tile_row(i, half) >= a.classes) c[b][i] = kFloor;
+                }
             }
             // `top` is where the sums' exponentials start from, and is raised only when a
             // logit is far above it: sums of a few hundred e^kRise are no trouble
