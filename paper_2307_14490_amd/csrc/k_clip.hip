@@ -69,30 +69,32 @@ __device__ __forceinline__ Chunk chunk_of(const ClipArgs& a, uint32_t chunk) {
 
 // Calls body(pointer) for a thread's 16-byte pieces of a chunk, and one(pointer) for the
 // elements before the first and behind the last aligned one.
-template <typename E, int THREADS, typename Body, typename One>
+// kBlock threads share a chunk.
+template <typename E, typename Body, typename One>
 __device__ __forceinline__ void each(E* p, int64_t left, Body body, One one) {
     constexpr int W = kWide<E>;
+    const int tid = threadIdx.x % kBlock;
     const int n = (int)(left < kClipChunk ? left : kClipChunk);
     const int off = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(E));
     const int skip = off == 0 ? 0 : W - off < n ? W - off : n;
     const int wide = (n - skip) / W;
     if (wide == kClipChunk / W) {
 #pragma unroll 8
-        for (int k = 0; k < kClipChunk / W; k += THREADS) body(p + skip + (k + (int)threadIdx.x) * W);
+        for (int k = 0; k < kClipChunk / W; k += kBlock) body(p + skip + (k + tid) * W);
     } else {
 #pragma unroll 4
-        for (int k = threadIdx.x; k < wide; k += THREADS) body(p + skip + k * W);
+        for (int k = tid; k < wide; k += kBlock) body(p + skip + k * W);
     }
-    if ((int)threadIdx.x < skip) one(p + threadIdx.x);
+    if (tid < skip) one(p + tid);
     const int end = skip + wide * W;
-    if ((int)threadIdx.x < n - end) one(p + end + threadIdx.x);
+    if (tid < n - end) one(p + end + tid);
 }
 
 // Sum of the squares of a thread's elements of a chunk.
-template <typename E, int THREADS>
+template <typename E>
 __device__ __forceinline__ double squares(E* p, int64_t left) {
     double s[2] = {0.0, 0.0};
-    each<E, THREADS>(
+    each<E>(
         p, left,
         [&](const E* at) {
             const Sixteen<E> q = load_sixteen(at);
@@ -108,10 +110,9 @@ __device__ __forceinline__ double squares(E* p, int64_t left) {
         });
     return s[0] + s[1];
 }
-template <int THREADS>
 __device__ __forceinline__ double squares(const Chunk& c) {
-    return c.bf16 ? squares<bf16_t, THREADS>(static_cast<bf16_t*>(c.p), c.left)
-                  : squares<float, THREADS>(static_cast<float*>(c.p), c.left);
+    return c.bf16 ? squares(static_cast<bf16_t*>(c.p), c.left)
+                  : squares(static_cast<float*>(c.p), c.left);
 }
 
 // Sum over a workgroup, in thread 0.
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(kBlock) void k_squares(ClipArgs a, double* __restri
     // from the last chunk on: the step that follows starts at the first, whose elements are then
     // the last that were read (129e6 fp32 elements and AdamW's step: 704 -> 694 us)
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x)
-        v += squares<kBlock>(chunk_of(a, a.chunks - 1 - c));
+        v += squares(chunk_of(a, a.chunks - 1 - c));
     v = block_sum<kBlock>(v, s);
     if (threadIdx.x == 0) part[blockIdx.x] = v;
 }
@@ -158,21 +159,22 @@ __global__ __launch_bounds__(1024) void k_norm_factor(const double* __restrict__
     if (threadIdx.x == 0) write_factor(v, scale, max_norm, norm, factor);
 }
 
-// A few chunks: by one workgroup, in one launch.  394 elements of four tensors before
-// AdamW's step: 3 us in place of 3 and 2.
+// A few chunks: by one workgroup at once, in one launch.
 __global__ __launch_bounds__(1024) void k_norm_small(ClipArgs a, double scale, double max_norm,
                                                      float* __restrict__ norm,
                                                      float* __restrict__ factor) {
     __shared__ double s[16];
     double v = 0.0;
-    for (uint32_t c = 0; c < a.chunks; ++c) v += squares<1024>(chunk_of(a, c));
+    static_assert(kClipSmall * kBlock <= 1024, "a chunk has kBlock threads");
+    const uint32_t c = threadIdx.x / kBlock;
+    if (c < a.chunks) v = squares(chunk_of(a, c));
     v = block_sum<1024>(v, s);
     if (threadIdx.x == 0) write_factor(v, scale, max_norm, norm, factor);
 }
 
 template <typename E>
 __device__ __forceinline__ void scale_chunk(E* p, int64_t left, float f) {
-    each<E, kBlock>(
+    each<E>(
         p, left,
         [&](E* at) {
             const Sixteen<E> q = load_sixteen(at);

@@ -256,23 +256,23 @@ __global__ __launch_bounds__(kBlock) void k_rms_backward(RmsArgs a) {
     }
 }
 
-// Column sums of `partial`: a workgroup takes 16 columns, 16 threads each.
+// Column sums of `partial`: a workgroup takes 8 columns, 32 threads each.
 __global__ __launch_bounds__(kBlock) void k_rms_reduce(const float* __restrict__ partial,
                                                        int blocks, int dim,
                                                        float* __restrict__ dgamma) {
-    __shared__ float s[16][17];
-    const int col = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
+    __shared__ float s[32][9];
+    const int col = blockIdx.x * 8 + (threadIdx.x & 7), lane = threadIdx.x >> 3;
     float v = 0.f;
     if (col < dim) {
 #pragma unroll 8
-        for (int b = lane; b < blocks; b += 16) v += partial[(int64_t)b * dim + col];
+        for (int b = lane; b < blocks; b += 32) v += partial[(int64_t)b * dim + col];
     }
-    s[lane][threadIdx.x & 15] = v;
+    s[lane][threadIdx.x & 7] = v;
     __syncthreads();
     if (lane == 0 && col < dim) {
         float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) sum += s[k][threadIdx.x & 15];
+        for (int k = 0; k < 32; ++k) sum += s[k][threadIdx.x & 7];
         dgamma[col] = sum;
     }
 }
@@ -405,7 +405,7 @@ hipError_t launch_rms_backward(const RmsArgs& a, float* dgamma, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     if (dgamma == nullptr) return hipSuccess;
-    k_rms_reduce<<<dim3((uint32_t)((a.dim + 15) / 16)), kBlock, 0, s>>>(
+    k_rms_reduce<<<dim3((uint32_t)((a.dim + 7) / 8)), kBlock, 0, s>>>(
         a.partial, norm_blocks(a.n, a.dim), a.dim, dgamma);
     return hipGetLastError();
 }
