@@ -281,19 +281,20 @@ def _grads(grads, what):
     if not grads:
         raise ValueError(f"{what}: no gradients")
     codes = {torch.float32: _DTYPES["f32"], torch.bfloat16: _DTYPES["bf16"]}
-    if all(issubclass(c, torch.Tensor) for c in {type(g) for g in grads}):
-        types = [g.dtype for g in grads]
-        devices = {g.get_device() for g in grads}
-        if codes.keys() >= set(types) and min(devices) >= 0 and \
-                all([g.is_contiguous() for g in grads]):
+    T = torch.Tensor
+    if all(issubclass(c, T) for c in set(map(type, grads))):
+        types = list(map(T.dtype.__get__, grads))
+        kinds, devices = set(types), set(map(T.get_device, grads))
+        if codes.keys() >= kinds and min(devices) >= 0 and all(map(T.is_contiguous, grads)):
             device = grads[0].device
             if len(devices) > 1:
                 k = next(k for k, g in enumerate(grads) if g.device != device)
                 raise ValueError(f"{what}[{k}]: on {grads[k].device}, expected {device}")
             table = np.empty(len(grads), _TABLE)
-            table["d_grad"] = [g.data_ptr() for g in grads]
-            table["n"] = [g.numel() for g in grads]
-            table["dtype"] = [codes[t] for t in types]
+            table["d_grad"] = list(map(T.data_ptr, grads))
+            table["n"] = list(map(T.numel, grads))
+            table["dtype"] = (codes[types[0]] if len(kinds) == 1
+                              else list(map(codes.__getitem__, types)))
             return grads, device, table.ctypes.data_as(ctypes.POINTER(HugeGradTensor)), table
     for k, g in enumerate(grads):  # one of them is refused
         _arg(g, ("float32", "bfloat16"), f"{what}[{k}]")
