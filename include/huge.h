@@ -627,7 +627,7 @@ huge_status huge_adamw_set_state(const huge_adamw_tensor* h_tensors, int32_t cou
      d_gamma            : dim floats
      d_y                : rows of `dtype`, which may be the array of d_x if there
                           is no residual; or NULL, and y in 8 bits to
-     d_codes, d_scales  : as huge_quantise_rows writes them from the y in 32 bits
+     d_codes, d_scales  : as huge_quantise_rows says, those of a y in fp64
      d_rstd             : n floats, or NULL
    eps > 0.  Squares are summed in fp32: a row whose sum of them passes 3.4e38 has
    rstd 0. */
@@ -730,7 +730,11 @@ huge_status huge_log_probs(const huge_log_probs_config* cfg, const void* d_h, in
      d_dentropy       : n floats, or NULL (zeros)
      d_dh, d_dw, d_dbias : as in huge_softmax_grad
    A row whose weights are 0, or which has no class, has no gradient, whatever its h
-   holds.  Roundings, time and the status are those of huge_softmax_grad. */
+   holds.  Time and the status are those of huge_softmax_grad, and so are the roundings of
+   fp32 rows.  With bf16 rows each g_ij is rounded to fp16 under a scale per row of the
+   result that follows its largest element, 2^-11 of it (or 2^-39 of that largest), and the
+   rows that it multiplies are exact there (within 2^-40 of the largest of 32 rows): what is
+   left is the rounding of the result, 1.7e-3 of the norm of dh and dw. */
 huge_status huge_log_probs_grad(const huge_log_probs_config* cfg, const void* d_h, int64_t ld_h,
                                 int64_t n, const void* d_w, int64_t ld_w, const float* d_bias,
                                 const int32_t* d_labels, const float* d_lse, const float* d_entropy,

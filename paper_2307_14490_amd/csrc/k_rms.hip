@@ -11,6 +11,8 @@
 // everything, gives the smallest power under which no code is above 448.  A code
 // times a power of two is a bf16 number, so that what reads such rows widens them
 // without another rounding.
+#include <type_traits>
+
 #include "rows.hpp"
 
 namespace huge {
@@ -81,38 +83,81 @@ __device__ __forceinline__ uint32_t max_of_block(uint32_t v) {
     return v;
 }
 
-// Stores cells c of a row in 8 bits and, from the first of a block, its scale.  The
-// lanes of a block call together; r is 0 past the row's end.
-template <int W, bool WHOLE>
-__device__ __forceinline__ void store_bytes(uint8_t* codes, uint8_t* scales, int c, int D,
-                                            const Cells<W>& r) {
+// W cells in 8 bits, and the exponent of their block's scale.  The lanes of a block call
+// together; r is 0 past the row's end.
+template <int W>
+struct Bytes {
+    uint32_t q[W / 4];
+    int x;
+};
+template <int W>
+__device__ __forceinline__ void codes_of(const Cells<W>& r, float mul, uint32_t* q) {
+#pragma unroll
+    for (int k = 0; k < W / 4; ++k) {
+        const float* v = r.v + 4 * k;
+        q[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] * mul, v[1] * mul, 0, false);
+        q[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * mul, v[3] * mul, (int)q[k], true);
+    }
+}
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+template <int W>
+__device__ __forceinline__ uint32_t largest_of_block(const Cells<W>& r) {
     uint32_t big = 0;
 #pragma unroll
     for (int e = 0; e < W; ++e) big = max(big, abs_bits(r.v[e]));
-    const int x = scale_exponent(max_of_block<W>(big));
-    if (W * c >= D) return;
-    const float mul = __uint_as_float((uint32_t)(127 - (x == kNone ? 0 : x)) << 23);
-    uint32_t q[W / 4];
+    return max_of_block<W>(big);
+}
+template <int W>
+__device__ __forceinline__ Bytes<W> encode(const Cells<W>& r) {
+    Bytes<W> o;
+    o.x = scale_exponent(largest_of_block<W>(r));
+    codes_of<W>(r, power(o.x == kNone ? 0 : -o.x), o.q);
+    if (o.x == kNone) {
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k) o.q[k] = 0x7F7F7F7Fu;  // NaN
+    }
+    return o;
+}
+
+// The same of numbers that are known within `near` of themselves, and whether another code or
+// scale is that near.
+template <int W>
+__device__ __forceinline__ Bytes<W> encode_near(const Cells<W>& r, float near, bool& doubt) {
+    const uint32_t big = largest_of_block<W>(r);
+    Bytes<W> o;
+    o.x = scale_exponent(big);
+    const float most = __uint_as_float(big);
+    doubt |= scale_exponent(__float_as_uint(most * (1.f - near))) !=
+             scale_exponent(__float_as_uint(most * (1.f + near)));
+    uint32_t low[W / 4];
+    const float mul = power(o.x == kNone ? 0 : -o.x);
+    codes_of<W>(r, mul * (1.f + near), o.q);
+    codes_of<W>(r, mul * (1.f - near), low);
 #pragma unroll
     for (int k = 0; k < W / 4; ++k) {
-        q[k] = 0x7F7F7F7Fu;  // NaN
-        if (x != kNone) {
-            const float* v = r.v + 4 * k;
-            q[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] * mul, v[1] * mul, 0, false);
-            q[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * mul, v[3] * mul, (int)q[k], true);
-        }
+        doubt |= o.x != kNone && o.q[k] != low[k];
+        if (o.x == kNone) o.q[k] = 0x7F7F7F7Fu;  // NaN
     }
+    return o;
+}
+
+// Stores them and, from the first cells of a block, its scale.
+template <int W, bool WHOLE>
+__device__ __forceinline__ void store_bytes(uint8_t* codes, uint8_t* scales, int c, int D,
+                                            const Bytes<W>& o) {
+    if (W * c >= D) return;
     if constexpr (W == 8) {
-        *reinterpret_cast<u32x2*>(codes + 8 * c) = u32x2{q[0], q[1]};
+        *reinterpret_cast<u32x2*>(codes + 8 * c) = u32x2{o.q[0], o.q[1]};
     } else if constexpr (WHOLE) {
-        *reinterpret_cast<uint32_t*>(codes + 4 * c) = q[0];
+        *reinterpret_cast<uint32_t*>(codes + 4 * c) = o.q[0];
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (4 * c + e < D) codes[4 * c + e] = (uint8_t)(q[0] >> (8 * e));
+            if (4 * c + e < D) codes[4 * c + e] = (uint8_t)(o.q[0] >> (8 * e));
     }
     constexpr int kCells = kByteBlock / W;
-    if (c % kCells == 0) scales[c / kCells] = (uint8_t)(x + 127);
+    if (c % kCells == 0) scales[c / kCells] = (uint8_t)(o.x + 127);
 }
 
 template <typename E>
@@ -121,9 +166,46 @@ __device__ __forceinline__ float rounded(float v) {
     else return __uint_as_float(float_to_bf16_bits(v) << 16);
 }
 
+// The float next to v, towards zero where v is none, with its last bit set: rounded from
+// there to the few bits of a code, a number is rounded as if it were rounded once.
+__device__ __forceinline__ float to_odd(double v) {
+    const float f = (float)v;
+    const double back = (double)f;
+    uint32_t b = __float_as_uint(f);
+    if (back != v && b << 1 < 0xFF000000u) b = (b - (fabs(back) > fabs(v) ? 1u : 0u)) | 1u;
+    return __uint_as_float(b);
+}
+
+// Sum over a row's threads in fp64, as row_sum; between two calls all of a workgroup's threads
+// meet elsewhere.
+template <int TPR>
+__device__ __forceinline__ double row_sum64(double v, double* s) {
+#pragma unroll
+    for (int off = 1; off < (TPR < 64 ? TPR : 64); off <<= 1) v += __shfl_xor(v, off);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = (s[0] + s[1]) + (s[2] + s[3]);
+    }
+    return v;
+}
+
+// BYTES: a code that is next to where it changes would change with the last bits of fp32.
+// Where one of a wave's is that near, its rows are formed in fp64 once more, so that all codes
+// are those of the formula.  How near: n squares in sequence and over lanes are summed within
+// n + 3 roundings with the mean and eps, rstd is within half of that and two, y within
+// two more, and the test itself takes two.
+template <int W, int TPR, int NV>
+constexpr float near_of() {
+    int levels = TPR > 64 ? 3 : 0;
+    for (int k = 1; k < TPR && k < 64; k <<= 1) ++levels;
+    return (0.5f * (NV * W + levels) + 8.f) * 0x1p-24f;
+}
+
 template <typename E, int W, int TPR, int NV, bool WHOLE, bool BYTES>
 __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
     __shared__ float s_sum[8];
+    __shared__ double s_sum64[BYTES ? 4 : 1];
     int turn = 0;
     constexpr int kRows = kBlock / TPR;
     const int t = threadIdx.x % TPR, D = a.dim, chunks = (D + W - 1) / W;
@@ -153,18 +235,59 @@ __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
             for (int e = 0; e < W; ++e) sq = fmaf(f[i].v[e], f[i].v[e], sq);
         }
         const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s_sum, turn) * inv + a.eps);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = t + TPR * i;
-            const Cells<W> g = c < chunks ? load_cells<W, WHOLE>(a.gamma, c, D) : Cells<W>{};
-#pragma unroll
-            for (int e = 0; e < W; ++e) f[i].v[e] = f[i].v[e] * rstd * g.v[e];
-            if constexpr (BYTES)
-                store_bytes<W, WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f[i]);
-            else if (c < chunks)
-                store_cells<W, WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f[i]);
-        }
         if (t == 0 && a.rstd != nullptr) a.rstd[r] = rstd;
+        if constexpr (!BYTES) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = t + TPR * i;
+                if (c >= chunks) continue;
+                const Cells<W> g = load_cells<W, WHOLE>(a.gamma, c, D);
+#pragma unroll
+                for (int e = 0; e < W; ++e) f[i].v[e] = f[i].v[e] * rstd * g.v[e];
+                store_cells<W, WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f[i]);
+            }
+        } else {
+            uint8_t* codes = a.codes + r * a.ld_codes;
+            uint8_t* scales = a.scales + r * a.ld_scales;
+            Bytes<W> q[NV];
+            constexpr float kNear = near_of<W, TPR, NV>();
+            bool doubt = false;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = t + TPR * i;
+                const Cells<W> g = c < chunks ? load_cells<W, WHOLE>(a.gamma, c, D) : Cells<W>{};
+                Cells<W> y;
+#pragma unroll
+                for (int e = 0; e < W; ++e) y.v[e] = f[i].v[e] * rstd * g.v[e];
+                q[i] = encode_near<W>(y, kNear, doubt);
+            }
+            bool again;
+            if constexpr (TPR > 64) again = __syncthreads_or(doubt);
+            else again = __ballot(doubt) != 0;
+            if (again) {
+                double sq64 = 0.0;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        sq64 = fma((double)f[i].v[e], (double)f[i].v[e], sq64);
+                const double rstd64 =
+                    1.0 / sqrt(row_sum64<TPR>(sq64, s_sum64) / (double)D + (double)a.eps);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = t + TPR * i;
+                    const Cells<W> g = c < chunks ? load_cells<W, WHOLE>(a.gamma, c, D) : Cells<W>{};
+                    Cells<W> y;
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        y.v[e] = to_odd((double)f[i].v[e] * rstd64 * (double)g.v[e]);
+                    q[i] = encode<W>(y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                store_bytes<W, WHOLE>(codes, scales, t + TPR * i, D, q[i]);
+        }
     }
 }
 
@@ -289,7 +412,8 @@ __global__ __launch_bounds__(kBlock) void k_to_bytes(RmsArgs a) {
         const int c = (int)(b % blocks) * kCells + threadIdx.x % kCells;
         const Cells<W> f =
             W * c < D ? load_cells<W, WHOLE>(static_cast<const E*>(a.x) + r * a.ld_x, c, D) : Cells<W>{};
-        store_bytes<W, WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D, f);
+        store_bytes<W, WHOLE>(a.codes + r * a.ld_codes, a.scales + r * a.ld_scales, c, D,
+                              encode<W>(f));
     }
 }
 

@@ -115,6 +115,27 @@ __device__ __forceinline__ f32x16 product(const Operand<E>& a, const Operand<E>&
     return Kind<E>::mfma(a.p[0], b.p[0], c);
 }
 
+// The second product of answers' bf16 gradients: halves, whose bits take the place of an
+// operand's.
+template <typename E, bool HALF_BITS>
+__device__ __forceinline__ f32x16 second_product(const Operand<E>& a, const Operand<E>& b, f32x16 c) {
+    if constexpr (HALF_BITS)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.p[0]),
+                                                      __builtin_bit_cast(f16x8, b.p[0]), c, 0, 0, 0);
+    else
+        return product<E>(a, b, c);
+}
+template <typename E, bool HALF_BITS>
+__device__ __forceinline__ Operand<E> second_split(f32x8 v) {
+    if constexpr (HALF_BITS) {
+        Operand<E> r;
+        r.p[0] = __builtin_bit_cast(typename Kind<E>::Vec, __builtin_convertvector(v, f16x8));
+        return r;
+    } else {
+        return split<E>(v);
+    }
+}
+
 // Row of a product's register i in lane half h (the column is lane % 32).
 __device__ __forceinline__ int tile_row(int i, int h) { return 8 * (i / 4) + 4 * h + i % 4; }
 
@@ -123,7 +144,7 @@ constexpr int kHeader = 1024;
 enum Field : int {
     kTerm = 0,    // classes: bias, -inf where the class is out
     kTerm2 = 1,   // the same times log2(e); rows: (log weight - lse) log2(e), -inf without a loss
-    kMul = 2,     // fp32: what the packed row is to be multiplied by
+    kMul = 2,     // fp32, and the T form of answers: what the packed row is to be multiplied by
     kLabel = 3,   // rows: label (int32), -1 without a loss
     kWeight = 4,  // rows: weight
     kSlope = 5,   // rows of weights of either sign: an element is p (kSlope log2 p + kCoef),
@@ -189,6 +210,12 @@ __device__ __forceinline__ void set_status(int32_t* status, int32_t code) {
 // ---------------------------------------------------------------------------
 // Packing
 // ---------------------------------------------------------------------------
+// The largest magnitude of p (slope log2 p + coef), less weight, over p in 0 .. 1: p log2 p
+// is within 1 / (e ln 2) = 0.5307.
+__device__ __forceinline__ float element_bound(float slope, float coef, float weight) {
+    return 0.54f * fabsf(slope) + fabsf(coef) + fabsf(weight);
+}
+
 struct PackArgs {
     const void* m;
     int64_t ld, first, count;  // rows first .. first + count of the matrix
@@ -327,21 +354,40 @@ __global__ __launch_bounds__(kBlock) void k_sm_pack(SoftmaxArgs a, PackArgs w, P
                                       k.scales + at * k.ld_scales, col, a.dim, k.vec);
         return load_cols(m, col, a.dim, k.vec);
     };
-    if constexpr (Kind<E>::kScaled) {
+    // answers' T form is halves of rows under a scale that a record shares: G's elements then
+    // need one factor for a tile, where a scale per row would be one for each
+    constexpr bool kHalfT = ANSWER && !Kind<E>::kScaled;
+    float half_mul = 1.f;
+    if (Kind<E>::kScaled || (kHalfT && forms == 2)) {
         float big = 0.f;
         if (!out)
             for (int col = j0; col < a.dim; col += 32) big = max4(big, cols(col));
         big = fmaxf(big, __shfl_xor(big, 1));
         big = fmaxf(big, __shfl_xor(big, 2));
         big = fmaxf(big, __shfl_xor(big, 4));
-        if ((threadIdx.x & 7) == 0) {
-            // big < 2^e: scaled by 2^(15 - e) the row is below 2^15
-            int e = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
-            e = e < -100 ? -100 : e;
-            s_mul[row] = ldexpf(1.f, 15 - e);
-            head[32 * kMul + row] = ldexpf(1.f, e - 15);
+        auto exponent = [](float v) {
+            // v < 2^e: scaled by 2^(15 - e) the row is below 2^15
+            const int e = v > 0.f && v < INFINITY ? __builtin_amdgcn_frexp_expf(v) : 0;
+            return e < -100 ? -100 : e;
+        };
+        if constexpr (Kind<E>::kScaled) {
+            if ((threadIdx.x & 7) == 0) {
+                const int e = exponent(big);
+                s_mul[row] = ldexpf(1.f, 15 - e);
+                head[32 * kMul + row] = ldexpf(1.f, e - 15);
+            }
+            __syncthreads();
+        } else {
+            if ((threadIdx.x & 7) == 0) s_mul[row] = big;
+            __syncthreads();
+            // an infinity counts for nothing: its row's products are no numbers in any scale
+            float most = 0.f;
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r) most = s_mul[r] < INFINITY ? fmaxf(most, s_mul[r]) : most;
+            const int e = exponent(most);
+            half_mul = ldexpf(1.f, 15 - e);
+            if (threadIdx.x < 32) head[32 * kMul + threadIdx.x] = ldexpf(1.f, e - 15);
         }
-        __syncthreads();
     }
     const float mul = Kind<E>::kScaled ? s_mul[row] : 1.f;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
@@ -367,9 +413,12 @@ __global__ __launch_bounds__(kBlock) void k_sm_pack(SoftmaxArgs a, PackArgs w, P
             if (forms == 2 && db < nd) {
                 f32x8 v;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    v[j] = s[16 * t + tile_row(j, half)][32 * (q >> 1) + (lane & 31)];
-                const Operand<E> p = split<E>(v);
+                for (int j = 0; j < 8; ++j) {
+                    const int r = 16 * t + tile_row(j, half);
+                    v[j] = s[r][32 * (q >> 1) + (lane & 31)];
+                    if constexpr (kHalfT) v[j] *= half_mul;
+                }
+                const Operand<E> p = second_split<E, kHalfT>(v);
 #pragma unroll
                 for (int part = 0; part < kParts; ++part)
                     form[((kParts + part) * nfrag + t * nd + db) * 64 + lane] = p.p[part];
@@ -1271,6 +1320,10 @@ __device__ __forceinline__ void store_out(E* p, float4 v, float scale, bool vec)
 template <typename E, int ND, int XB, int WAVES, bool STAGED, bool ROWS, bool ANSWER>
 __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uint8_t* lds) {
     constexpr bool kScaled = Kind<E>::kScaled;
+    // bf16 rows of answers: G in halves under a scale, as fp32 rows' G, not in bf16
+    constexpr bool kHalfBits = ANSWER && !kScaled;
+    // one wave per SIMD
+    constexpr bool kKeepsSums = STAGED && (kScaled ? ND > 4 : kHalfBits && ND > 8);
     constexpr bool HALVES = STAGED && Shape<E, ND, true>::kHalves;
     const Place at = place(a, block);
     if (at.none) return;
@@ -1285,7 +1338,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
     // per X row: the factor and the term of its exponents (a class's bias is the
     // initial value of its column where that is not scaled), the label (for
     // classes: the class itself) and the weight
-    float xmul[XB], xterm[XB], xw[XB], bias[XB], pscale[XB], xslope[XB], xcoef[XB];
+    float xmul[XB], xterm[XB], xw[XB], bias[XB], pscale[XB], xslope[XB], xcoef[XB], xbound[XB];
     int32_t xl[XB];
     f32x16 acc[XB][ND];
 #pragma unroll
@@ -1301,6 +1354,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
         xw[b] = ROWS ? field(xt.rec[b], kWeight)[r] : 0.f;
         xslope[b] = ROWS && ANSWER ? field(xt.rec[b], kSlope)[r] : 0.f;
         xcoef[b] = ROWS && ANSWER ? field(xt.rec[b], kCoef)[r] : 0.f;
+        xbound[b] = ROWS && ANSWER ? element_bound(xslope[b], xcoef[b], xw[b]) : 0.f;
         const int32_t label = lane_label(xt.rec[b], lane);
         // classes fit 31 bits; a label of an earlier piece is below 0 here
         xl[b] = (int32_t)(ROWS ? (label < 0 ? -1 : label - a.class0)
@@ -1414,6 +1468,25 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
                 }
             }
         }
+        // a new scale for the sums of X's row b, whose next element is up to `big`
+        auto scale_sums = [&](int b, float big, bool anew, int below) {
+            // big is below 2^e: it is brought below 2^below
+            float ratio = 1.f;
+            if (anew) {
+                const int e = __builtin_amdgcn_frexp_expf(big);
+                const float s = ldexpf(1.f, e < below - 120 ? 120 : below - e);
+                ratio = pscale[b] > 0.f ? fminf(s / pscale[b], 1.f) : 0.f;
+                pscale[b] = pscale[b] > 0.f ? fminf(s, pscale[b]) : s;
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                // a wave alone on its SIMD keeps the sums in accumulation registers; unless
+                // that is said here, the compiler copies them for this product in every tile
+                if constexpr (kKeepsSums) asm volatile("" : "+a"(acc[b][d]));
+                acc[b][d] *= ratio;
+                if constexpr (kKeepsSums) asm volatile("" : "+a"(acc[b][d]));
+            }
+        };
         if constexpr (kScaled) {
             const f32x16 ymul = row_values(rec, kMul, half);
 #pragma unroll
@@ -1426,28 +1499,29 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
                 }
                 // the halves share the sums of a row: they share its scale
                 big = fmaxf(big, __shfl_xor(big, 32));
-                const bool scale_anew = big * pscale[b] > 0x1p15f ||
-                                        (pscale[b] == 0.f && big > 0.f);
-                if (__ballot(scale_anew) != 0) {
-                    // big is below 2^e: the largest element is brought below 2^15
-                    float ratio = 1.f;
-                    if (scale_anew) {
-                        const int e = __builtin_amdgcn_frexp_expf(big);
-                        const float s = ldexpf(1.f, e < -105 ? 120 : 15 - e);
-                        ratio = pscale[b] > 0.f ? fminf(s / pscale[b], 1.f) : 0.f;
-                        pscale[b] = pscale[b] > 0.f ? fminf(s, pscale[b]) : s;
-                    }
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        // a wave alone on its SIMD keeps the sums in accumulation
-                        // registers; unless that is said here, the compiler copies
-                        // them for this product in every tile
-                        if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
-                        acc[b][d] *= ratio;
-                        if constexpr (STAGED && ND > 4) asm volatile("" : "+a"(acc[b][d]));
-                    }
-                }
+                const bool anew = big * pscale[b] > 0x1p15f || (pscale[b] == 0.f && big > 0.f);
+                if (__ballot(anew) != 0) scale_sums(b, big, anew, 15);
                 c[b] *= pscale[b];
+            }
+        } else if constexpr (kHalfBits) {
+            // A row's elements are scaled by what they can be: its label's is about that large.
+            // A class may have small ones alone, and is scaled by those that it has.  Either
+            // way the largest is brought below 2^11 or 2^12, so that few later ones are too large
+            const float record_mul = row_four(rec, kMul, 0, 0)[0];
+#pragma unroll
+            for (int b = 0; b < XB; ++b) {
+                float big = xbound[b];
+                if constexpr (!ROWS) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(c[b][i]));
+                    const int v = __float_as_int(big);
+                    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+                    big = fmaxf(__int_as_float(both[0]), __int_as_float(both[1]));
+                }
+                big *= record_mul;
+                const bool anew = big * pscale[b] > 0x1p15f || (pscale[b] == 0.f && big > 0.f);
+                if (__ballot(anew) != 0) scale_sums(b, big, anew, ROWS ? 12 : 11);
+                c[b] *= record_mul * pscale[b];
             }
         }
         Operand<E> p[XB][2];
@@ -1458,7 +1532,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
                 f32x8 v;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = c[b][8 * t + j];
-                p[b][t] = split<E>(v);
+                p[b][t] = second_split<E, kHalfBits>(v);
             }
         if constexpr (HALVES) {
             between();
@@ -1468,7 +1542,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
         y.template run<kProducts<E> * XB>(load, [&](int f, const Operand<E>& q) {
 #pragma unroll
             for (int b = 0; b < XB; ++b)
-                acc[b][f % ND] = product<E>(q, p[b][f / ND], acc[b][f % ND]);
+                acc[b][f % ND] = second_product<E, kHalfBits>(q, p[b][f / ND], acc[b][f % ND]);
         });
     };
     if constexpr (HALVES) {
@@ -1493,7 +1567,8 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
         const int64_t xi = xt.t[b] * 32 + (lane & 31);
         const int64_t row = ((int64_t)at.split * yw + yg) * a.part_rows + xi - a.part_first;
         const bool direct = at.whole || a.part == nullptr;
-        const float back = kScaled && pscale[b] > 0.f ? 1.f / pscale[b] : kScaled ? 0.f : 1.f;
+        constexpr bool kBack = kScaled || kHalfBits;
+        const float back = kBack && pscale[b] > 0.f ? 1.f / pscale[b] : kBack ? 0.f : 1.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -1501,7 +1576,7 @@ __device__ __forceinline__ void grad_block(const PassArgs& a, int32_t block, uin
                 const int col = 32 * (db0 + d) + 8 * g + 4 * half;
                 float4 v = make_float4(acc[b][d][4 * g], acc[b][d][4 * g + 1],
                                        acc[b][d][4 * g + 2], acc[b][d][4 * g + 3]);
-                if constexpr (kScaled) v = scale4(back, v);
+                if constexpr (kBack) v = scale4(back, v);
                 if (!direct) {
                     float4* p = reinterpret_cast<float4*>(a.part + row * a.dp + col);
                     *p = a.first ? v : add4(*p, v);

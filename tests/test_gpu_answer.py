@@ -73,7 +73,11 @@ def test_rms_norm_and_its_gradient(n, dim, dtype):
         within(y, wy, ey + half * np.abs(wy) + 1e-30, "y")
         q, _, rstd8 = P.rms_norm(x, g, r, 1e-5, q8=True)
         assert torch.equal(rstd, rstd8)
-        check_q8(q, wy, ey, "y in 8 bits")
+        check_q8(q, wy, np.abs(wy) * 2.0 ** -48, "y in 8 bits")
+        codes, scales = ref.q8_rows(wy) if wy.size < 40_000 else (None, None)
+        if codes is not None:  # the formula's own codes
+            np.testing.assert_array_equal(q.scales.cpu().numpy(), scales)
+            np.testing.assert_array_equal(q.codes.view(torch.uint8).cpu().numpy(), codes)
         # the backward pass from the oracle's rstd as float32
         r32 = vec(wr)
         rv32 = r32.double().cpu().numpy()
@@ -288,9 +292,10 @@ def check_grad(k, op, a, el, elow, eh, lp, h0):
         rel = (el + elow + 16 * U)[:, None] + 4 * U * np.abs(lp)
         eg = size * rel + soft * (el + elow + eh)[:, None] + soft * 4 * U * (np.abs(lp) + h0[:, None])
         half = BF if dtype == "bf16" else 0.0
-        # in two fp16 parts an element is held within 2^-21 of its row's (column's) largest
-        split = 0.0 if dtype == "bf16" else 2.0 ** -21
-        eh_, ew_ = (eg + half * size + split * size.max(ax, keepdims=True) for ax in (1, 0)) \
+        # an element is held in fp16, half a step of 2^-10 off (fp32 rows: in two parts, within
+        # 2^-21 of its row's (column's) largest)
+        part, split = (2.0 ** -11, 2.0 ** -24) if dtype == "bf16" else (0.0, 2.0 ** -21)
+        eh_, ew_ = (eg + part * size + split * size.max(ax, keepdims=True) for ax in (1, 0)) \
             if n else (eg, eg)
         s = size @ np.abs(wc)
         within(got[0], wants[0], eh_ @ np.abs(wc) + (classes ** 0.5 + 64) * U * s
