@@ -269,18 +269,33 @@ __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
-                    for (int e = 0; e < W; ++e)
+                    for (int e = 0; e < W; ++e) {
                         sq64 = fma((double)f[i].v[e], (double)f[i].v[e], sq64);
-                const double rstd64 =
-                    1.0 / sqrt(row_sum64<TPR>(sq64, s_sum64) / (double)D + (double)a.eps);
+                        asm volatile("" : "+v"(f[i].v[e]));
+                    }
+                // 1 / D and the root by Newton's method from what the hardware has.  Few registers:
+                // what is widened is not kept, and gamma is read here again
+                double inv64 = (double)inv;
+                inv64 = fma(inv64, fma(-(double)D, inv64, 1.0), inv64);
+                const double x64 = fma(row_sum64<TPR>(sq64, s_sum64), inv64, (double)a.eps);
+                double rstd64 = __builtin_amdgcn_rsq(x64);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    rstd64 = fma(0.5 * rstd64, fma(-x64 * rstd64, rstd64, 1.0), rstd64);
+                uint64_t gamma_at = reinterpret_cast<uint64_t>(a.gamma);
+                asm volatile("" : "+s"(gamma_at));
+                const float* gamma = (const float*)(const __attribute__((address_space(1))) float*)gamma_at;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int c = t + TPR * i;
-                    const Cells<W> g = c < chunks ? load_cells<W, WHOLE>(a.gamma, c, D) : Cells<W>{};
+                    const Cells<W> g = c < chunks ? load_cells<W, WHOLE>(gamma, c, D) : Cells<W>{};
                     Cells<W> y;
 #pragma unroll
-                    for (int e = 0; e < W; ++e)
-                        y.v[e] = to_odd((double)f[i].v[e] * rstd64 * (double)g.v[e]);
+                    for (int e = 0; e < W; ++e) {
+                        float ge = g.v[e];
+                        asm volatile("" : "+v"(ge));  // one after the other
+                        y.v[e] = to_odd((double)f[i].v[e] * rstd64 * (double)ge);
+                    }
                     q[i] = encode<W>(y);
                 }
             }
