@@ -5,7 +5,9 @@
 // of either type is exact and cannot overflow or vanish; its sum is one entry of
 // `part`.  A second kernel adds the entries, always in the same order, and writes the
 // norm and the factor, which stay on the device: what applies it (AdamW's step, or
-// k_scale in place) reads it there.  Bound by memory: each gradient is read once.
+// k_scale in place) reads it there.  Bound by memory, each gradient being read once: 129e6
+// fp32 elements 118 to 132 us (3.9 to 4.4 TB/s; a read reaches 4.0), 20e6 bf16 ones in
+// 400 tensors 24 us in three launches of up to 150 tensors.
 #include "device.hpp"
 #include "head.hpp"
 

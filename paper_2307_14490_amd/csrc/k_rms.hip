@@ -4,13 +4,20 @@
 // A group of threads holds a row in registers, as in layer norm: the sum of the two
 // inputs is rounded to the rows' type, stored and normalised as it was stored, so that
 // the backward pass, which reads it again, sees the same row.  One reduction over the
-// group, the sum of squares; every array is moved once.  Bound by memory.
+// group, the sum of squares; every array is moved once.  Bound by memory (a copy reaches
+// 4.75 TB/s): 60417 x 761 fp32 with a residual 131 us forward (5.6 TB/s), 155 us backward
+// (4.7) and 5 us for the sums of the weight gradients; 65536 x 128 bf16, which stays in the
+// caches, 13, 13 and 4 us.
+//
+// bf16 rows of whole aligned eights go 16 bytes a thread: 8 bits back to bf16, 1e6
+// x 128, took 103 us with 8 bytes a thread where it takes 64 to 69.
 //
 // 8 bits: e4m3 codes under a power of two for each 32 columns, which eight threads
 // hold: the largest of their absolute values, as integers, so that a NaN is above
 // everything, gives the smallest power under which no code is above 448.  A code
 // times a power of two is a bf16 number, so that what reads such rows widens them
-// without another rounding.
+// without another rounding.  1e6 x 128 bf16 into codes that are the formula's own (below):
+// 102 us, 3.8 TB/s.
 #include <type_traits>
 
 #include "rows.hpp"
