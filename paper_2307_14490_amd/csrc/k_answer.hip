@@ -13,8 +13,8 @@
 // 4096 x 1e6 x 128 bf16, ten best: the pass 1265 to 1380 us by the clock (0.76 to 0.83 PFLOP/s;
 // the loss, which needs no moment and no tile's largest, takes 960 to 1040), the search 107
 // (0.5 GB of largest logits at 4.8 TB/s), the best classes 92 (470 MB of table rows).  The pass
-// is bound by the vector units: 16 exponentials of 16 clocks and about 70 other instructions
-// of 4 for a tile of 32 x 32, where its products take 256; they are busy 81% of the time.
+// is bound by the vector units: 16 exponentials of 16 clocks and about 55 other instructions
+// of 4 for a tile of 32 x 32, where its products take 256; they are busy 74% of the time.
 // One row over 1e6 x 128 in 8 bits: 30 us (132 MB at 4.4 TB/s), 11 and 9.
 #include "softmax.hpp"
 

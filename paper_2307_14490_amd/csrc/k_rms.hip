@@ -17,7 +17,7 @@
 // everything, gives the smallest power under which no code is above 448.  A code
 // times a power of two is a bf16 number, so that what reads such rows widens them
 // without another rounding.  1e6 x 128 bf16 into codes that are the formula's own (below):
-// 102 us, 3.8 TB/s.
+// 87 to 95 us, 4.1 to 4.5 TB/s.
 #include <type_traits>
 
 #include "rows.hpp"
@@ -134,9 +134,10 @@ __device__ __forceinline__ Bytes<W> encode_near(const Cells<W>& r, float near, b
     const uint32_t big = largest_of_block<W>(r);
     Bytes<W> o;
     o.x = scale_exponent(big);
-    const float most = __uint_as_float(big);
-    doubt |= scale_exponent(__float_as_uint(most * (1.f - near))) !=
-             scale_exponent(__float_as_uint(most * (1.f + near)));
+    // near 1.75 times a power of two, or the first that is no number
+    const uint32_t steps = (uint32_t)(near * 0x1p24f) + 2u;  // floats within `near`
+    doubt |= (big & 0x7FFFFFu) - 0x600000u + steps <= 2u * steps;
+    doubt |= 0x7F800000u - big <= 2u * steps;
     uint32_t low[W / 4];
     const float mul = power(o.x == kNone ? 0 : -o.x);
     codes_of<W>(r, mul * (1.f + near), o.q);
@@ -167,10 +168,26 @@ __device__ __forceinline__ void store_bytes(uint8_t* codes, uint8_t* scales, int
     if (c % kCells == 0) scales[c / kCells] = (uint8_t)(o.x + 127);
 }
 
-template <typename E>
-__device__ __forceinline__ float rounded(float v) {
-    if constexpr (sizeof(E) == 4) return v;
-    else return __uint_as_float(float_to_bf16_bits(v) << 16);
+// r + o, rounded to the rows' type.
+template <typename E, int W>
+__device__ __forceinline__ void add_rounded(Cells<W>& r, const Cells<W>& o) {
+    typedef float Wide __attribute__((ext_vector_type(W)));
+    Wide v;
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = r.v[e] + o.v[e];
+    if constexpr (sizeof(E) == 2) {
+        typedef __bf16 Near __attribute__((ext_vector_type(W)));
+        v = __builtin_convertvector(__builtin_convertvector(v, Near), Wide);
+    }
+#pragma unroll
+    for (int e = 0; e < W; ++e) r.v[e] = v[e];
+}
+
+// Row r0 + sub of rows at a stride: what all lanes share first, where 64-bit products are cheap;
+// the lane's part is the same from turn to turn.
+template <typename T>
+__device__ __forceinline__ T* row_at(T* p, int64_t ld, int64_t r0, int sub) {
+    return p + r0 * ld + sub * ld;
 }
 
 // The float next to v, towards zero where v is none, with its last bit set: rounded from
@@ -197,6 +214,17 @@ __device__ __forceinline__ double row_sum64(double v, double* s) {
     return v;
 }
 
+// 1 / sqrt(x), x > 0, from the hardware's within one unit by a Newton step, whose roundings
+// are one and a half: half of that of x r0, and the last.  What the hardware takes for 0 is
+// scaled before; an infinity's is 0 as it is.
+__device__ __forceinline__ float inverse_root(float x) {
+    const bool tiny = x < 0x1p-96f;
+    const float v = tiny ? x * 0x1p64f : x;
+    const float r0 = __builtin_amdgcn_rsqf(v);
+    const float r = fmaf(0.5f * r0, fmaf(-(v * r0), r0, 1.f), r0);
+    return x < INFINITY ? (tiny ? r * 0x1p32f : r) : r0;
+}
+
 // BYTES: a code that is next to where it changes would change with the last bits of fp32.
 // Where one of a wave's is that near, its rows are formed in fp64 once more, so that all codes
 // are those of the formula.  How near: n squares in sequence and over lanes are summed within
@@ -220,28 +248,29 @@ __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
     const E* res = static_cast<const E*>(a.res);
     E* total = static_cast<E*>(a.total);
     const float inv = 1.0f / (float)D;
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.n;
-         r += (int64_t)gridDim.x * kRows) {
+    const int sub = TPR == kBlock ? 0 : threadIdx.x / TPR;
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.n; r0 += (int64_t)gridDim.x * kRows) {
+        const int64_t r = r0 + sub;
+        if (r >= a.n) break;
         Cells<W> f[NV], o[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
-            f[i] = c < chunks ? load_cells<W, WHOLE>(x + r * a.ld_x, c, D) : Cells<W>{};
-            if (res != nullptr) o[i] = c < chunks ? load_cells<W, WHOLE>(res + r * a.ld_res, c, D) : Cells<W>{};
+            f[i] = c < chunks ? load_cells<W, WHOLE>(row_at(x, a.ld_x, r0, sub), c, D) : Cells<W>{};
+            if (res != nullptr) o[i] = c < chunks ? load_cells<W, WHOLE>(row_at(res, a.ld_res, r0, sub), c, D) : Cells<W>{};
         }
         float sq = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = t + TPR * i;
             if (res != nullptr) {
-#pragma unroll
-                for (int e = 0; e < W; ++e) f[i].v[e] = rounded<E>(f[i].v[e] + o[i].v[e]);
-                if (c < chunks) store_cells<W, WHOLE>(total + r * a.ld_total, c, D, f[i]);
+                add_rounded<E>(f[i], o[i]);
+                if (c < chunks) store_cells<W, WHOLE>(row_at(total, a.ld_total, r0, sub), c, D, f[i]);
             }
 #pragma unroll
             for (int e = 0; e < W; ++e) sq = fmaf(f[i].v[e], f[i].v[e], sq);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s_sum, turn) * inv + a.eps);
+        const float rstd = inverse_root(row_sum<TPR>(sq, s_sum, turn) * inv + a.eps);
         if (t == 0 && a.rstd != nullptr) a.rstd[r] = rstd;
         if constexpr (!BYTES) {
 #pragma unroll
@@ -251,11 +280,11 @@ __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
                 const Cells<W> g = load_cells<W, WHOLE>(a.gamma, c, D);
 #pragma unroll
                 for (int e = 0; e < W; ++e) f[i].v[e] = f[i].v[e] * rstd * g.v[e];
-                store_cells<W, WHOLE>(static_cast<E*>(a.y) + r * a.ld_y, c, D, f[i]);
+                store_cells<W, WHOLE>(row_at(static_cast<E*>(a.y), a.ld_y, r0, sub), c, D, f[i]);
             }
         } else {
-            uint8_t* codes = a.codes + r * a.ld_codes;
-            uint8_t* scales = a.scales + r * a.ld_scales;
+            uint8_t* codes = row_at(a.codes, a.ld_codes, r0, sub);
+            uint8_t* scales = row_at(a.scales, a.ld_scales, r0, sub);
             Bytes<W> q[NV];
             constexpr float kNear = near_of<W, TPR, NV>();
             bool doubt = false;
@@ -477,7 +506,11 @@ __global__ __launch_bounds__(kBlock) void k_from_bytes(RmsArgs a) {
 template <typename E, int W, int TPR, int NV, bool WHOLE>
 void rms_one(const RmsArgs& a, bool backward, hipStream_t s) {
     const int64_t rows = kBlock / TPR, need = (a.n + rows - 1) / rows;
-    const dim3 grid((uint32_t)(need < 65536 ? need : 65536));
+    // into 8 bits vector instructions show, and what comes before the loop is done for several
+    // rows (1e6 x 128 bf16 and back: 158 us, 168 with up to 65536 workgroups); else memory
+    // bounds, and one row a group is a little faster (200000 x 256 fp32 both ways 303 and 310)
+    const int64_t most = a.codes != nullptr ? 8192 : 65536;
+    const dim3 grid((uint32_t)(need < most ? need : most));
     if (backward)
         k_rms_backward<E, W, TPR, NV, WHOLE>
             <<<dim3((uint32_t)norm_blocks(a.n, a.dim)), kBlock, 0, s>>>(a);
