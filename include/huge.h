@@ -757,14 +757,15 @@ huge_status huge_grad_norm(const huge_grad_tensor* h_tensors, int32_t count, flo
 
 /* Scales all elements by max_norm / norm where the norm is above max_norm > 0 (which may
    be infinite), in place; d_norm, or NULL, receives the norm before.  The tensors must
-   not overlap, and stay as they are where the norm is not finite. */
+   not overlap, and stay as they are where an element is not finite.  (A norm above
+   the largest float is written as infinity; finite elements are scaled by what it is.) */
 huge_status huge_clip_grads(const huge_grad_tensor* h_tensors, int32_t count, double max_norm,
                             float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
 
 /* huge_adamw_step with gradients so clipped: in place of grad_scale they are multiplied
    by grad_scale or, where the norm of all grad_scale g is above max_norm > 0, by grad_scale
    max_norm / norm.  The gradients are not written.  d_norm, or NULL, receives the
-   norm of grad_scale g.  Where that is not finite no element moves, and
+   norm of grad_scale g.  Where a gradient is not finite no element moves, and
    HUGE_ERR_NOT_FINITE is written to d_status.  d_workspace as for huge_grad_norm. */
 huge_status huge_adamw_step_clipped(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
                                     int32_t count, double max_norm, float* d_norm,

@@ -318,8 +318,8 @@ def grad_norm(grads, stream=None):
 
 def clip_grads(grads, max_norm, stream=None):
     """Scales a list of gradients in place so that their norm is at most max_norm, by
-    huge_clip_grads, and returns the norm before.  They stay as they are where it is
-    not finite.  The tensors must share no memory."""
+    huge_clip_grads, and returns the norm before.  They stay as they are where one of them
+    is not finite.  The tensors must share no memory."""
     import torch
     grads, device, table, _keep = _grads(grads, "clip_grads")
     if not float(max_norm) > 0:

@@ -381,8 +381,8 @@ class AdamW(_Status):
         a graph's capture its learning rate and bias corrections are recorded too.
         max_norm: the step takes the gradients (which stay as they are) scaled so that the
         norm over all of them, times grad_scale, is at most that; it returns the norm
-        before (one float32 element).  Where that is not finite nothing moves, though the
-        step counts."""
+        before (one float32 element).  Where a gradient is not finite nothing moves, though
+        the step counts."""
         if max_norm is not None and not float(max_norm) > 0:
             raise ValueError(f"AdamW.step: max_norm {max_norm}")
         grads = self._list(grads, ("float32", "bfloat16"), "AdamW.step grads")
