@@ -318,6 +318,7 @@ __global__ __launch_bounds__(kBlock) void k_rms(RmsArgs a) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     rstd64 = fma(0.5 * rstd64, fma(-x64 * rstd64, rstd64, 1.0), rstd64);
+                if (rstd == 0.f) rstd64 = 0.0;  // the sum passed fp32, whatever row calls for fp64
                 uint64_t gamma_at = reinterpret_cast<uint64_t>(a.gamma);
                 asm volatile("" : "+s"(gamma_at));
                 const float* gamma = (const float*)(const __attribute__((address_space(1))) float*)gamma_at;
