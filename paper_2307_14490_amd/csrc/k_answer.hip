@@ -10,7 +10,7 @@
 // that decide, and k_lp_top forms the logits of their classes again in fp64, in which
 // products of bf16 or fp32 numbers are exact, and orders those.
 //
-// 4096 x 1e6 x 128 bf16, ten best: the pass 1265 to 1380 us by the clock (0.76 to 0.83 PFLOP/s;
+// 4096 x 1e6 x 128 bf16, ten best: the pass 1257 to 1380 us by the clock (0.76 to 0.83 PFLOP/s;
 // the loss, which needs no moment and no tile's largest, takes 960 to 1040), the search 107
 // (0.5 GB of largest logits at 4.8 TB/s), the best classes 92 (470 MB of table rows).  The pass
 // is bound by the vector units: 16 exponentials of 16 clocks and about 55 other instructions
