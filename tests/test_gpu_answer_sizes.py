@@ -119,3 +119,23 @@ def test_rms_norm_of_more_than_2_to_the_31_elements():
     q, _, _ = P.rms_norm(x, g, q8=True)
     assert torch.equal(q.codes[-1].view(torch.uint8), q.codes[0].view(torch.uint8))
     assert torch.equal(P.q8_values(q, "bf16")[-1], P.q8_values(P.Q8Rows(q.codes[:1], q.scales[:1]), "bf16")[0])
+
+
+@pytest.mark.parametrize("dim,dtype,n", [(32, "f32", 270_000), (128, "bf16", 140_001),
+                                         (257, "f32", 40_003), (1500, "f32", 9001),
+                                         (2000, "bf16", 17_000)])
+def test_rms_norm_in_8_bits_of_several_rows_a_workgroup(dim, dtype, n):
+    """More rows than workgroups take at once: the same as in parts that are not."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn((n, dim), device="cuda", generator=gen)
+    x = x.to(torch.bfloat16) if dtype == "bf16" else x
+    res = x.flip(0)
+    gamma = torch.linspace(0.5, 1.5, dim, device="cuda")
+    y, total, rstd = P.rms_norm(x, gamma, residual=res, q8=True)
+    step = 4000
+    for a in range(0, n, step):
+        part = slice(a, a + step)
+        y1, total1, rstd1 = P.rms_norm(x[part], gamma, residual=res[part], q8=True)
+        assert torch.equal(y1.codes.view(torch.uint8), y.codes[part].view(torch.uint8))
+        assert torch.equal(y1.scales, y.scales[part])
+        assert torch.equal(total1, total[part]) and torch.equal(rstd1, rstd[part])
