@@ -727,7 +727,7 @@ huge_status huge_log_probs(const huge_log_probs_config* cfg, const void* d_h, in
                         be NULL without d_dentropy)
      d_dlogp          : n floats, or NULL (zeros; labels may then be NULL).  Counts as 0 for
                         a row without a label or whose label is out
-     d_dentropy       : n floats, or NULL (zeros)
+     d_dentropy       : n floats of at most 1e18 in magnitude, or NULL (zeros)
      d_dh, d_dw, d_dbias : as in huge_softmax_grad
    A row whose weights are 0, or which has no class, has no gradient, whatever its h
    holds.  Time and the status are those of huge_softmax_grad, and so are the roundings of

@@ -44,8 +44,9 @@
 // row, as those of fp32 rows do: weights of either sign cancel in the sums, where the
 // rounding to bf16 would show (2.3e-3 to 2.5e-3 of the norm, 1.7e-3 with fp16, which is the
 // result's own rounding; 100003 x 1000 x 128 149 us and 168).  There a class that is out has the finite term
-// kFloor, so that the product of a vanishing probability and its logarithm is 0, and
-// the running maximum starts at kLeast, far above that: a row without classes sums to 0.
+// kFloor (in gradients kGradFloor), so that the product of a vanishing probability and its
+// logarithm is 0, and the running maximum starts at kLeast, far above that: a row without
+// classes sums to 0.
 #pragma once
 
 #include <math.h>
@@ -67,6 +68,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kFloor = -1e30f, kLeast = -1e28f;
+// The term in gradients, where an element is a vanishing probability times its logarithm
+// times a weight: 0 for weights up to 1e18, as that product stays finite.  Far below what logits
+// may be (1e9) all the same.
+constexpr float kGradFloor = -1e20f;
 
 // Element types: how rows are split, and the product of two operands.
 template <typename E>
@@ -291,7 +296,7 @@ __global__ __launch_bounds__(kBlock) void k_sm_pack(SoftmaxArgs a, PackArgs w, P
             if (!out) term = a.bias == nullptr ? 0.f : a.bias[k.first + i];
             if constexpr (ANSWER) {
                 out = term < kLeast;
-                if (out) term = kFloor;
+                if (out) term = forms == 2 ? kGradFloor : kFloor;
             } else {
                 out = term == -INFINITY;
             }
