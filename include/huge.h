@@ -758,7 +758,8 @@ huge_status huge_grad_norm(const huge_grad_tensor* h_tensors, int32_t count, flo
 /* Scales all elements by max_norm / norm where the norm is above max_norm > 0 (which may
    be infinite), in place; d_norm, or NULL, receives the norm before.  The tensors must
    not overlap, and stay as they are where an element is not finite.  (A norm above
-   the largest float is written as infinity; finite elements are scaled by what it is.) */
+   the largest float is written as infinity; finite elements are scaled by what it is, also by
+   factors that no float holds.) */
 huge_status huge_clip_grads(const huge_grad_tensor* h_tensors, int32_t count, double max_norm,
                             float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
 

@@ -24,8 +24,8 @@ inline bool fours(const void* p, int64_t ld, int32_t dtype) {
     return on(p, 4 * elem(dtype)) && ld % 4 == 0;
 }
 
-// AdamW: the checks of a step, and the step, whose gradients are multiplied by *d_factor
-// where that is given, and by cfg->grad_scale otherwise.
+// AdamW: the checks of a step, and the step, whose gradients are multiplied by d_factor[0]
+// d_factor[1] where that is given, and by cfg->grad_scale otherwise.
 huge_status adamw_args(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,
                        int32_t count, const int32_t* d_status);
 huge_status adamw_step(const huge_adamw_config* cfg, const huge_adamw_tensor* h_tensors,

@@ -86,7 +86,8 @@ struct ClipArgs {
 };
 // The sums of squares of a launch's tensors: *parts entries of `part`.
 hipError_t launch_squares(const ClipArgs& a, double* part, int* parts, hipStream_t s);
-// The norm of `scale` times the elements behind `parts` entries, and the factor for them.
+// The norm of `scale` times the elements behind `parts` entries, and the factor for them, the
+// product of two floats.
 hipError_t launch_norm_factor(const double* part, int parts, double scale, double max_norm,
                               float* norm, float* factor, hipStream_t s);
 // Both at once, of up to kClipSmall chunks.
@@ -114,7 +115,7 @@ struct AdamArgs {
     AdamTensor t[kAdamTensors];
     int32_t count;
     float beta1, one_beta1, beta2, one_beta2, rate, fix, eps, keep, grad_scale;
-    const float* factor;  // in place of grad_scale, or null
+    const float* factor;  // two floats whose product is in place of grad_scale, or null
     int32_t* status;
 };
 // Offsets in a state: m, then v, then (8 bits) the two scales of each block.

@@ -141,12 +141,16 @@ __global__ __launch_bounds__(kBlock) void k_squares(ClipArgs a, double* __restri
 }
 
 // The norm of `scale` times the elements from the sum of their squares, and the factor
-// for them: scale, or less so that the norm is max_norm.  NaN where the norm is not finite.
+// for them: scale, or less so that the norm is max_norm.  NaN where the norm is not finite.  It is the product of two
+// floats, one after the other: behind a norm of 1e38 or more one alone would lose digits or be 0.
 __device__ __forceinline__ void write_factor(double square, double scale, double max_norm,
                                              float* norm, float* factor) {
     const double r = fabs(scale) * sqrt(square);
     if (norm != nullptr) *norm = (float)r;
-    *factor = !(r < INFINITY) ? NAN : (float)(r > max_norm ? scale * (max_norm / r) : scale);
+    const double f = r > max_norm ? scale * (max_norm / r) : scale;
+    const bool small = fabs(f) < 0x1p-126;
+    factor[0] = !(r < INFINITY) ? NAN : (float)(small ? f * 0x1p126 : f);
+    factor[1] = small ? 0x1p-126f : 1.0f;
 }
 
 __global__ __launch_bounds__(1024) void k_norm_factor(const double* __restrict__ part, int n,
@@ -175,22 +179,25 @@ __global__ __launch_bounds__(1024) void k_norm_small(ClipArgs a, double scale, d
 }
 
 template <typename E>
-__device__ __forceinline__ void scale_chunk(E* p, int64_t left, float f) {
+__device__ __forceinline__ void scale_chunk(E* p, int64_t left, float f, float f2) {
     each<E>(
         p, left,
         [&](E* at) {
             const Sixteen<E> q = load_sixteen(at);
             if constexpr (sizeof(E) == 4) {
-                *reinterpret_cast<f32x4*>(at) = f32x4{q.v[0] * f, q.v[1] * f, q.v[2] * f, q.v[3] * f};
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = q.v[e] * f * f2;
+                *reinterpret_cast<f32x4*>(at) = v;
             } else {
                 f32x8 v;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = q.v[e] * f;
+                for (int e = 0; e < 8; ++e) v[e] = q.v[e] * f * f2;
                 *reinterpret_cast<bf16x8*>(at) = __builtin_convertvector(v, bf16x8);
             }
         },
         [&](E* at) {
-            const float v = load_one(at) * f;
+            const float v = load_one(at) * f * f2;
             if constexpr (sizeof(E) == 4) *at = v;
             else *at = (bf16_t)float_to_bf16_bits(v);
         });
@@ -198,12 +205,12 @@ __device__ __forceinline__ void scale_chunk(E* p, int64_t left, float f) {
 
 // Nothing is read or written where the factor is 1, or no number.
 __global__ __launch_bounds__(kBlock) void k_scale(ClipArgs a, const float* __restrict__ factor) {
-    const float f = *factor;
-    if (f == 1.0f || f != f) return;
+    const float f = factor[0], f2 = factor[1];
+    if ((f == 1.0f && f2 == 1.0f) || f != f) return;
     for (uint32_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
         const Chunk c = chunk_of(a, k);
-        if (c.bf16) scale_chunk(static_cast<bf16_t*>(c.p), c.left, f);
-        else scale_chunk(static_cast<float*>(c.p), c.left, f);
+        if (c.bf16) scale_chunk(static_cast<bf16_t*>(c.p), c.left, f, f2);
+        else scale_chunk(static_cast<float*>(c.p), c.left, f, f2);
     }
 }
 

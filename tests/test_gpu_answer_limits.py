@@ -38,3 +38,49 @@ def test_gradients_scale_with_large_weights(n, classes, dim, dtype):
             say(f"weights times {power:.3g}, {n} x {classes} x {dim} {dtype}, bias {b is not None}")
             for got, want in zip(op.grad(h, w, a, labels, dl * power, de * power, b), one):
                 assert torch.equal(got.float(), want.float() * power)
+
+
+# norms beyond the largest float, or so far above the largest wanted that the factor is below
+# the smallest: an element of 1000 equal ones becomes max_norm / sqrt(1000)
+FAR = [(3e38, 1.0), (3e38, 1e-3), (1e38, 1e-2), (3e38, 1e-6), (3e38, 1e-12), (2e30, 1e-12)]
+U = 2.0 ** -24
+
+
+def equal_gradients(value, dtype, offset):
+    return torch.full((1003,), value, device="cuda", dtype=TYPES[dtype])[offset:offset + 1000]
+
+
+@pytest.mark.parametrize("value,most", FAR)
+@pytest.mark.parametrize("dtype,offset", [("f32", 0), ("f32", 3), ("bf16", 0), ("bf16", 1)])
+def test_clipping_by_factors_that_no_float_holds(value, most, dtype, offset):
+    g = equal_gradients(value, dtype, offset)
+    v = g[0].double().item()
+    norm = P.clip_grads([g], most)
+    full = v * 1000 ** 0.5
+    assert norm.item() == (math.inf if full > 3.4028235e38 else pytest.approx(full, rel=2 * U))
+    # the factor's rounding, the product's, and half a step of bf16
+    want = most / 1000 ** 0.5
+    rel = 3 * U + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    assert ((g.double() - want).abs() <= rel * want).all(), (g[0].item(), want)
+
+
+@pytest.mark.parametrize("states", ["f32", "q8"])
+@pytest.mark.parametrize("value,most", FAR)
+@pytest.mark.parametrize("dtype,offset", [("f32", 0), ("f32", 3), ("bf16", 0)])
+def test_clipped_steps_by_factors_that_no_float_holds(value, most, dtype, offset, states):
+    """As steps with the scaled gradients themselves, beta1 and beta2 0: the moments are a
+    gradient and its square."""
+    g = equal_gradients(value, dtype, offset)
+    p = normal(1000, seed=4)
+    opt = P.AdamW([p], betas=(0.0, 0.0), states=states, weight_decay=0.0, lr=0.25)
+    before = p.clone()
+    opt.step([g], max_norm=most)
+    opt.check()
+    m, v = opt.values()
+    want = most / 1000 ** 0.5
+    # 8 bits: 7 bits of a square root, whose largest (here: every) element is a code itself
+    assert ((m[0].double() - want).abs() <= 8 * U * want).all()
+    assert ((v[0].double() - want ** 2).abs() <= 16 * U * want ** 2 + 2.0 ** -149).all()
+    # m / (sqrt v + eps) = 1 / (1 + eps / want)
+    moved = 0.25 / (1 + 1e-8 / want)
+    assert ((before - p).double() - moved).abs().max().item() <= 8 * U * (0.25 + 4)
