@@ -682,8 +682,8 @@ typedef struct huge_log_probs_config {
 
 /* Bytes of device workspace of the two calls below (256-byte aligned); 0 if the
    config is invalid.  It holds what huge_softmax_loss packs and, with top > 0, the
-   largest logit of each tile of 16 or 32 classes, for as many rows and classes at a time as
-   take 1 GiB. */
+   largest logit of each tile of 16 or 32 classes and lists of the best tiles, for as many rows
+   and classes at a time as take 1 GiB (and up to 18 MiB of lists of parts of the classes). */
 size_t huge_log_probs_workspace_bytes(const huge_log_probs_config* cfg);
 
 /* Log probabilities, entropies and the most likely classes of n rows h (n x D) over
@@ -732,8 +732,10 @@ huge_status huge_log_probs(const huge_log_probs_config* cfg, const void* d_h, in
    A row whose weights are 0, or which has no class, has no gradient, whatever its h
    holds.  Time and the status are those of huge_softmax_grad, and so are the roundings of
    fp32 rows.  With bf16 rows each g_ij is rounded to fp16 under a scale per row of the
-   result that follows its largest element, 2^-11 of it (or 2^-39 of that largest), and the
-   rows that it multiplies are exact there (within 2^-40 of the largest of 32 rows): what is
+   result: within 2^-11 of it, or where that is more, for dw within 2^-35 of its class's
+   largest, for dh within 2^-36 of what its row's can be, |dlogp| + |dlogp + dentropy entropy|
+   + 0.4 |dentropy| (both times the power of two that scales the 32 rows it multiplies).  Those rows
+   are exact there (within 2^-40 of the largest of the 32): unless only far smaller elements count, what is
    left is the rounding of the result, 1.7e-3 of the norm of dh and dw. */
 huge_status huge_log_probs_grad(const huge_log_probs_config* cfg, const void* d_h, int64_t ld_h,
                                 int64_t n, const void* d_w, int64_t ld_w, const float* d_bias,

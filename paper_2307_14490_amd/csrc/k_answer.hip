@@ -26,7 +26,7 @@ typedef unsigned long long u64;
 
 constexpr int kSlack = 4;                          // tiles looked at beyond `top`
 constexpr int kTopThreads = 256;
-constexpr int64_t kBestFloats = (int64_t)1 << 28;  // tile maxima at a time: 1 GiB
+constexpr int64_t kBestBytes = (int64_t)1 << 30;   // tile maxima and lists at a time
 constexpr int kThirdsFrom = 3;                     // blocks of 16 fp32 rows that go in thirds
 constexpr int64_t kBestRows = 8192;                // rows that have room for any piece
 constexpr int64_t kListRows = 32768;               // rows times splits of k_lp_select
@@ -699,19 +699,21 @@ AnswerPlan answer_plan(int64_t classes, int64_t n, int32_t dim, int32_t dtype, b
     const int64_t all = div_up(classes, p.group);
     const int64_t pad = p.few != 0 ? 16 * p.few : p.sm.rows_pad;
     const int64_t rec = record_bytes(p.sm.dp / 16, p.sm.parts, 1);
+    p.keep = (int32_t)(all < top + kSlack ? all : top + kSlack);
     int64_t piece = all;  // tiles at a time
     p.rows = pad;         // rows at a time
     if (p.few == 0 && piece > kSmPieceBytes / rec) piece = kSmPieceBytes / rec;
     if (top > 0) {
         // the same piece for every number of rows, so that fewer never need more memory
         const int64_t least = p.few != 0 ? pad : kBestRows;
-        if (piece > kBestFloats / least) piece = kBestFloats / least;
-        int64_t most = round_down(kBestFloats / piece, kSmTile);
+        const int64_t lists = 16 * (int64_t)p.keep;  // of a row, and those of earlier pieces
+        const int64_t fits = (kBestBytes / least - lists) / 4;
+        if (piece > fits) piece = fits;
+        int64_t most = round_down(kBestBytes / (4 * piece + lists), kSmTile);
         if (most > kMostRows) most = kMostRows;
         if (p.few == 0 && p.rows > most) p.rows = most;
     }
     p.piece = piece * p.group;
-    p.keep = (int32_t)(all < top + kSlack ? all : top + kSlack);
     size_t off = 0;
     auto take = [&](int64_t bytes) {
         const size_t o = off;
