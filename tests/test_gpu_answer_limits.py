@@ -84,3 +84,58 @@ def test_clipped_steps_by_factors_that_no_float_holds(value, most, dtype, offset
     # m / (sqrt v + eps) = 1 / (1 + eps / want)
     moved = 0.25 / (1 + 1e-8 / want)
     assert ((before - p).double() - moved).abs().max().item() <= 8 * U * (0.25 + 4)
+
+
+def by_bias(bias):
+    """Probabilities, their logarithms and the entropy of logits that are the bias, in fp64."""
+    x = bias.double()
+    logp = x - torch.logsumexp(x, 0)
+    p = logp.exp()
+    return p, logp, -(p * logp).sum()
+
+
+def test_elements_of_the_rows_gradient_are_within_what_is_stated():
+    """Elements far below what their row's can be, one in each column of dh: rows whose logits
+    are the bias alone, and classes whose rows have a single 1."""
+    classes, dim = 64, 32
+    bias = torch.full((classes,), -40.0, device="cuda")
+    bias[0] = 0.0
+    bias[1:32] = -torch.linspace(18, 34, 31, device="cuda")
+    w = torch.zeros(classes, dim, device="cuda", dtype=torch.bfloat16)
+    w[1:32, :31] = torch.eye(31, device="cuda", dtype=torch.bfloat16)
+    h = torch.zeros(40, dim, device="cuda", dtype=torch.bfloat16)
+    h[:, 31] = 1.0
+    op = P.LogProbs(40, classes, dim, dtype="bf16", grad=True)
+    a = op.log_probs(h, w, bias=bias)
+    de = torch.linspace(0.5, 2.0, 40, device="cuda")
+    dh = op.grad(h, w, a, dentropy=de, bias=bias)[0].double()
+    p, logp, entropy = by_bias(bias)
+    g = (-p * (logp + entropy) * de.double()[:, None])[:, 1:32]
+    most = 0.4 * de.double()[:, None] + (entropy * de.double()[:, None]).abs()
+    # the logarithm's and the exponent's roundings, at logits of 40; of fp16, of bf16
+    err = (dh[:, :31] - g).abs()
+    assert (err <= g.abs() * (2.0 ** -8 + 2.0 ** -11 + 256 * U) + most * 2.0 ** -36).all()
+    # and there they show
+    assert (err > g.abs() * 2.0 ** -6).any()
+
+
+def test_elements_of_the_classes_gradient_are_within_what_is_stated():
+    """Rows whose weights fall by 2^-31, each in a column of dw of its own."""
+    classes, dim, n = 40, 32, 31
+    bias = torch.linspace(-3, 0, classes, device="cuda")
+    w = torch.zeros(classes, dim, device="cuda", dtype=torch.bfloat16)
+    h = torch.eye(dim, device="cuda", dtype=torch.bfloat16)[:n].contiguous()
+    op = P.LogProbs(n, classes, dim, dtype="bf16", grad=True)
+    a = op.log_probs(h, w, bias=bias)
+    de = torch.tensor([2.0 ** -i * (1 + i / 37) for i in range(n)], device="cuda")
+    dw = op.grad(h, w, a, dentropy=de, bias=bias)[1].double()
+    p, logp, entropy = by_bias(bias)
+    at = -p * (logp + entropy)
+    g = at[:, None] * de.double()[None, :]
+    size = (p * (logp.abs() + entropy))[:, None] * de.double()[None, :]  # terms that cancel
+    err = (dw[:, :n] - g).abs()
+    assert (err <= g.abs() * (2.0 ** -8 + 2.0 ** -11) + 64 * U * size
+            + g.abs().max(1, keepdim=True).values * 2.0 ** -35).all()
+    # and there they show: up to 2^-35 of the first of an element 2^-30 (1 + 30 / 37) of it, which is
+    # 2^-5.86, where bf16 and fp16 alone round by 2^-7.83 at most
+    assert (err > g.abs() * 2.0 ** -7.5).any()
