@@ -627,10 +627,11 @@ huge_status huge_adamw_set_state(const huge_adamw_tensor* h_tensors, int32_t cou
      d_gamma            : dim floats
      d_y                : rows of `dtype`, which may be the array of d_x if there
                           is no residual; or NULL, and y in 8 bits to
-     d_codes, d_scales  : as huge_quantise_rows says, those of a y in fp64
+     d_codes, d_scales  : as huge_quantise_rows says, those of a y in fp64 (beyond the
+                          largest float: of an infinity)
      d_rstd             : n floats, or NULL
    eps > 0.  Squares are summed in fp32: a row whose sum of them passes 3.4e38 has
-   rstd 0. */
+   rstd 0, and one whose squares are below 1e-38 few digits of it if eps is below 1e-30. */
 huge_status huge_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual,
                           int64_t n, int32_t dim, int32_t dtype, const float* d_gamma, float eps,
                           void* d_total, int64_t ld_total, void* d_y, int64_t ld_y,
@@ -705,7 +706,9 @@ size_t huge_log_probs_workspace_bytes(const huge_log_probs_config* cfg);
    Logits are below 1e9 in magnitude (the exponentials' arguments are taken from fp32
    products).  Where every class is out, lse is -inf, the entropy 0
    and no class is found; where lse is no finite number (a NaN or an infinity in h, or in a
-   class that counts) ids are -1 and the rest NaN.
+   class that counts) ids are -1 and the rest NaN.  An infinity in a class that counts may leave
+   a logit of -inf beside finite ones: the entropy is NaN then, lse NaN or that of the other
+   classes.
    Sums, maxima and exponentials are fp32 on logits as in huge_softmax_loss.  The classes
    found, and the order among them, are those of logits in fp64 (from the stored values), formed
    again for all classes of the top + 4 tiles of 16 or 32 classes with the largest logits:

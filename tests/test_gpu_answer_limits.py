@@ -139,3 +139,65 @@ def test_elements_of_the_classes_gradient_are_within_what_is_stated():
     # and there they show: up to 2^-35 of the first of an element 2^-30 (1 + 30 / 37) of it, which is
     # 2^-5.86, where bf16 and fp16 alone round by 2^-7.83 at most
     assert (err > g.abs() * 2.0 ** -7.5).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [5, 40, 80])
+def test_a_logit_of_minus_infinity_beside_finite_ones(n, dtype):
+    """An infinity in the row of a class that counts: no entropy, and lse and classes either
+    those of the others or none."""
+    h = normal(n, 16, seed=5).abs().add_(0.1).to(TYPES[dtype])
+    w = normal(200, 16, seed=6).to(TYPES[dtype])
+    op = P.LogProbs(n, 200, 16, dtype=dtype, top=4)
+    out = torch.zeros(200, device="cuda")
+    out[7] = -math.inf
+    want = op.log_probs(h, w, bias=out)
+    w[7, 3] = -math.inf
+    a = op.log_probs(h, w)
+    assert a.entropy.isnan().all()
+    for i in range(n):
+        if a.lse[i].isnan():
+            assert (a.ids[i] == -1).all() and a.top_logp[i].isnan().all()
+        else:
+            assert torch.equal(a.ids[i], want.ids[i])
+            assert torch.allclose(a.lse[i], want.lse[i], rtol=1e-5, atol=1e-5)
+            assert torch.allclose(a.top_logp[i], want.top_logp[i], rtol=1e-5, atol=1e-5)
+
+
+def test_rows_in_8_bits_beyond_the_largest_float():
+    """A norm times gamma that no float holds makes its block NaN, as an infinity does."""
+    x = torch.ones(3, 64, device="cuda")
+    x[1, 40] = 8.0
+    gamma = torch.ones(64, device="cuda")
+    gamma[40] = 3e38
+    y, _, _ = P.rms_norm(x, gamma, q8=True)
+    v = P.q8_values(y)
+    # row 1: squares of 63 ones and 64: 8 / sqrt(127 / 64) = 5.7 times 3e38
+    assert v[1, 32:].isnan().all() and not v[1, :32].isnan().any()
+    assert not v[[0, 2]].isnan().any()
+    near = (v[0, 40].double() / 3e38 - 1).abs().item()
+    assert near <= 2.0 ** -4 + 1e-5  # half a step of e4m3; eps
+
+
+@pytest.mark.parametrize("states", ["f32", "q8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_clipped_steps_leave_the_moments_of_scaled_gradients(states, dtype):
+    """Moments, not parameters, which hardly show the factor.  In 8 bits a moment is a code under
+    its block's scale: the scales follow the factor, and the codes are the same but where its
+    last bit moves one across a border."""
+    sizes = [300, 5000, 16385, 1]
+    gs = [normal(n, seed=n).mul_(10.0 ** (k - 2)).to(TYPES[dtype]) for k, n in enumerate(sizes)]
+    norm = math.sqrt(sum(g.double().square().sum().item() for g in gs))
+    for most, scale in ((0.25 * norm, 1.0), (0.03 * norm, -2.0), (10 * norm, 0.5)):
+        a, b, c = (P.AdamW([torch.zeros(n, device="cuda") for n in sizes], states=states)
+                   for _ in range(3))
+        f = scale * min(1.0, most / (abs(scale) * norm))
+        a.step(gs, max_norm=most, grad_scale=scale)
+        b.step(gs, grad_scale=f)
+        c.step(gs, grad_scale=1.01 * f)
+        for x, y, z in zip(*([*o.values()[0], *o.values()[1]] for o in (a, b, c))):
+            # the factor's rounding, and some each of the moment's and the scale's
+            far = ((x - y).abs() > 16 * U * y.abs()).double().mean().item()
+            assert far <= (0.0 if states == "f32" else 0.002), far
+            if x.numel() > 1:  # a hundredth more does not pass
+                assert ((z - y).abs() > 16 * U * y.abs()).double().mean().item() > 0.5
