@@ -201,3 +201,17 @@ def test_clipped_steps_leave_the_moments_of_scaled_gradients(states, dtype):
             assert far <= (0.0 if states == "f32" else 0.002), far
             if x.numel() > 1:  # a hundredth more does not pass
                 assert ((z - y).abs() > 16 * U * y.abs()).double().mean().item() > 0.5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q8"])
+@pytest.mark.parametrize("n", [5, 40, 80])
+def test_zeros_of_either_sign_are_equals(n, dtype):
+    """Rows of zeros and biases of -0 in the first half: the lowest classes all the same."""
+    classes, dim, top = 4000, 32, 20
+    h = torch.zeros(n, dim, device="cuda", dtype=TYPES["bf16" if dtype == "q8" else dtype])
+    w = normal(classes, dim, seed=8).abs().neg().to(h.dtype)
+    bias = torch.zeros(classes, device="cuda")
+    bias[: classes // 2] = -0.0
+    op = P.LogProbs(n, classes, dim, dtype=dtype, top=top)
+    a = op.log_probs(h, P.q8_rows(w) if dtype == "q8" else w, bias=bias)
+    assert (a.ids == torch.arange(top, device="cuda", dtype=torch.int32)).all()
