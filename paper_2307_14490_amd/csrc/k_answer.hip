@@ -15,7 +15,9 @@
 // (0.5 GB of largest logits at 4.8 TB/s), the best classes 92 (470 MB of table rows).  The pass
 // is bound by the vector units: 16 exponentials of 16 clocks and about 55 other instructions
 // of 4 for a tile of 32 x 32, where its products take 256; they are busy 74% of the time.
-// One row over 1e6 x 128 in 8 bits: 30 us (132 MB at 4.4 TB/s), 11 and 9.
+// One row over 1e6 x 128 in 8 bits: 30 us (132 MB at 4.4 TB/s), 11 and 9.  More than 64 rows
+// widen a table in 8 bits into records in every call, 118 to 125 us of that: 128 rows 240 us in all, in
+// bf16 120; 4096 rows 1652 and 1618.
 #include "softmax.hpp"
 
 namespace huge {
@@ -191,6 +193,12 @@ __global__ __launch_bounds__(kBlock) void k_lp_rows(SoftmaxArgs a, Parts part, i
 //
 // Without the bar every list filled and was cut in each round's turn: 4096 x 31250 tiles 375 us,
 // 107 with it; the 62500 tiles of one row 47 us, 11.
+//
+// There is none where the bar's `keep` = top + 4 values are not to be had: from as many threads of
+// a row (32, of few rows 64: top above 28, 60) and slots of the pass (about kSmPartRows / rows:
+// rows (top + 4) above 131072 at a time).  Lists then go in rounds.  bf16, D = 128: 4096 x 1e6, 28 best
+// 134 us, 29 best 576, 64 best 697; 250000 classes, ten best of 8192 rows 71, of 9376 467; of 16384 rows
+// three best 129, ten best 515.
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectKeys = 10496;
 template <int RW>

@@ -6,8 +6,9 @@
 // `part`.  A second kernel adds the entries, always in the same order, and writes the
 // norm and the factor, which stay on the device: what applies it (AdamW's step, or
 // k_scale in place) reads it there.  Bound by memory, each gradient being read once: 129e6
-// fp32 elements 118 to 132 us (3.9 to 4.4 TB/s; a read reaches 4.0), 20e6 bf16 ones in
-// 400 tensors 24 us in three launches of up to 150 tensors.
+// fp32 elements 118 to 132 us (3.9 to 4.4 TB/s; a read reaches 4.0), 40e6 bf16 ones in
+// 400 tensors 24 us in three launches of up to 150 tensors.  In place 129e6 fp32 elements take 159 us
+// more (6.5 TB/s), 285 in all.
 #include "device.hpp"
 #include "head.hpp"
 

@@ -17,7 +17,8 @@
 // everything, gives the smallest power under which no code is above 448.  A code
 // times a power of two is a bf16 number, so that what reads such rows widens them
 // without another rounding.  1e6 x 128 bf16 into codes that are the formula's own (below):
-// 87 to 95 us, 4.1 to 4.5 TB/s.
+// 87 to 95 us, 4.1 to 4.5 TB/s.  Rows as they are into codes: 1e6 x 128 bf16 68 to 71 us (5.5 TB/s),
+// fp32 108 to 114 (5.8).
 #include <type_traits>
 
 #include "rows.hpp"

@@ -443,7 +443,9 @@ struct Shape {
     static constexpr bool kTwo = sizeof(E) == 4;  // fp32: two parts
     // answers hold more beside a tile: at four blocks two tiles of X and four waves per SIMD do
     // not fit (4096 x 1e6 x 128: 1427 us with one tile, 1496 with two and registers in
-    // memory, 1845 with two and three waves)
+    // memory, 1845 with two and three waves).  At three blocks two, with 12 bytes in memory, are
+    // as fast or faster (4096 x 1e6 x 96: log probabilities alone 978 us and 992, with a bias and
+    // ten best 1376 and 1400)
     static constexpr int kXB = !GRAD && !kTwo && ND <= (ANSWER ? 3 : 4) ? 2 : 1;
     static constexpr int loss_occ() {
         if (kTwo) return ND <= 4 ? 4 : ND <= 8 ? 2 : 1;

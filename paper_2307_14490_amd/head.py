@@ -463,7 +463,8 @@ class SoftmaxHead:
     norm: "layer", or "rms" (no beta).  max_norm: steps clip the gradients of all
     parameters together to that norm, and norm_before holds what it was.  top: with a
     number the head also answers (that many of the most likely classes) and trains by
-    log probabilities.
+    log probabilities.  It then holds a second workspace, for answers and for policy_step, of
+    the size of step's (0.8 GB for 1e6 x 128 bf16); a head that only answers is a LogProbs.
 
     step(x, labels) trains the head on rows x (n x dim) and returns the mean loss
     (device) and the gradient of x, for a caller that trains the rows too.  Steps,
