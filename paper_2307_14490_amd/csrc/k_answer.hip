@@ -15,9 +15,9 @@
 // (0.5 GB of largest logits at 4.8 TB/s), the best classes 92 (470 MB of table rows).  The pass
 // is bound by the vector units: 16 exponentials of 16 clocks and about 55 other instructions
 // of 4 for a tile of 32 x 32, where its products take 256; they are busy 74% of the time.
-// One row over 1e6 x 128 in 8 bits: 30 us (132 MB at 4.4 TB/s), 11 and 9.  More than 64 rows
-// widen a table in 8 bits into records in every call, 118 to 125 us of that: 128 rows 240 us in all, in
-// bf16 120; 4096 rows 1652 and 1618.
+// One row over 1e6 x 128 in 8 bits: 30 us (132 MB at 4.4 TB/s), 11 and 9.  With more than 64 rows a
+// table in 8 bits is widened into records in every call, 115 to 127 us for this one: 128 rows 240 us
+// in all, in bf16 120; 4096 rows 1652 and 1618.
 #include "softmax.hpp"
 
 namespace huge {

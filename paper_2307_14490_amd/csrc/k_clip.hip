@@ -142,8 +142,9 @@ __global__ __launch_bounds__(kBlock) void k_squares(ClipArgs a, double* __restri
 }
 
 // The norm of `scale` times the elements from the sum of their squares, and the factor
-// for them: scale, or less so that the norm is max_norm.  NaN where the norm is not finite.  It is the product of two
-// floats, one after the other: behind a norm of 1e38 or more one alone would lose digits or be 0.
+// for them: scale, or less so that the norm is max_norm.  NaN where the norm is not finite.  It is
+// the product of two floats, one after the other: below 2^-126 (a norm of 1e38 brought to 1) one
+// alone would lose digits or be 0.
 __device__ __forceinline__ void write_factor(double square, double scale, double max_norm,
                                              float* norm, float* factor) {
     const double r = fabs(scale) * sqrt(square);

@@ -464,7 +464,7 @@ class SoftmaxHead:
     parameters together to that norm, and norm_before holds what it was.  top: with a
     number the head also answers (that many of the most likely classes) and trains by
     log probabilities.  It then holds a second workspace, for answers and for policy_step, of
-    the size of step's (0.8 GB for 1e6 x 128 bf16); a head that only answers is a LogProbs.
+    the size of step's (0.8 GB for 1e6 x 128 bf16); LogProbs by itself answers without that.
 
     step(x, labels) trains the head on rows x (n x dim) and returns the mean loss
     (device) and the gradient of x, for a caller that trains the rows too.  Steps,
